@@ -484,6 +484,137 @@ mist_status mist_measure_eta(const mist_model_desc* m, const int32_t* mb, int32_
 mist_status mist_probe_fp64(int32_t kind, const double* in, uint64_t* out, int64_t n_threads, int32_t reps,
                             uint64_t* n_instructions, void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of a training step's two ends, on the current device: the first stage's embedding
+ * with its gradient, the global gradient norm with clipping, and the optimizer step.  A plan of
+ * this tuner places them (the cost model's first-stage table of ceil(V/TP) rows and learned
+ * positions, 16-bit weights and gradients, fp32 master weights with Adam's m and v, each
+ * layer's step before its first forward pass, Sec. 5.1) and the operator database, which times
+ * GEMMs, does not cover them.
+ *
+ * Each call enqueues on hip_stream (NULL = the null stream) and returns without waiting.  It
+ * reads nothing back, so it can be captured into a graph, and it keeps nothing between calls.
+ * Buffers are device memory of the caller; scratch memory is passed in and belongs to the call
+ * until its work has finished.  Values are computed in fp32 or wider and rounded once, to
+ * nearest even, where they are stored.  The same inputs give the same bits on every run.
+ * --------------------------------------------------------------------------------------- */
+
+#define MIST_F32 0
+#define MIST_BF16 1
+#define MIST_F16 2
+
+/* A lookup of batch sequences of seq tokens in rows [vocab_begin, vocab_begin + rows) of a
+ * vocabulary-parallel table: this rank's shard.  An id outside them (another rank's, or padding
+ * such as -1) finds the zero row and gives no gradient.  Strides are in elements; the hidden
+ * dimension is contiguous. */
+typedef struct mist_embed_desc {
+  int64_t batch, seq;      /* >= 0; batch * seq < 2^31 */
+  int64_t hidden;          /* 1..2^24 */
+  int64_t rows;            /* 1..2^31 - 2 */
+  int64_t vocab_begin;     /* id of the shard's first row, in [0, 2^31) */
+  int64_t ids_stride;      /* between sequences' ids (ids of one sequence are contiguous) */
+  int64_t act_batch_stride, act_stride; /* of the activations, between sequences and between positions */
+  int64_t table_stride;    /* between rows of the table, >= hidden */
+  int64_t pos_stride;      /* between rows of the learned positions, >= hidden; unused without them */
+  int32_t ids_bytes;       /* 4 or 8: signed ids */
+  int32_t act_type;        /* MIST_F32, MIST_BF16 or MIST_F16: looked-up rows, or their gradient */
+  int32_t table_type;      /* of the table and the positions, or of their gradients */
+  float scale;             /* finite */
+} mist_embed_desc;
+
+/* out[b, s, :] = scale * table[id - vocab_begin, :] + pos[s, :] (the first term 0 for an id
+ * outside the shard; pos may be NULL: no positions).  The positions of out must not overlap.
+ * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const void* table, const void* pos, void* out,
+                               void* hip_stream);
+
+/* Scratch bytes that mist_embed_backward needs for *d.  Errors: MIST_E_INVALID. */
+mist_status mist_embed_workspace(const mist_embed_desc* d, size_t* bytes);
+
+/* The lookup's gradients from grad (laid out as the activations; sequences or positions may share
+ * memory, stride 0): dtable[v, :] = scale * sum of grad[b, s, :] over the tokens of row v, and
+ * dpos[s, :] = sum over b of grad[b, s, :] (dpos may be NULL).  Sums are in fp32 in an order that
+ * depends on the ids and sizes alone.  accumulate = 0 writes every row, zeros where no token is; accumulate
+ * = 1 adds to what dtable and dpos hold and touches only the rows of the tokens.  workspace: at
+ * least mist_embed_workspace bytes, aligned to 256.  Errors: MIST_E_INVALID, MIST_E_RANGE
+ * (workspace too small), MIST_E_DEVICE. */
+mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const void* grad, void* dtable, void* dpos,
+                                int32_t accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* A list of tensors of one type, e.g. the gradients of a stage: their addresses and sizes in
+ * tables on the device.  It holds no values; the tensors stay the caller's and must stay where
+ * they are.  It may be used on several streams at a time. */
+typedef struct mist_tensors mist_tensors;
+
+/* Host ptrs[0..n-1] are device addresses (each aligned to its element) of sizes[0..n-1]
+ * contiguous elements of the given type; a tensor may be empty, then its address is not used.  alloc as in
+ * mist_space_create (NULL: hipMalloc/hipFree).  Errors: MIST_E_INVALID, MIST_E_NOMEM,
+ * MIST_E_DEVICE. */
+mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, int64_t n, int32_t type,
+                                const mist_allocator* alloc, mist_tensors** out);
+
+/* Waits for the device's work and frees the tables.  NULL is accepted. */
+mist_status mist_tensors_destroy(mist_tensors* T);
+
+#define MIST_NORM_L2 0
+#define MIST_NORM_MAX 1
+
+/* State of a step, in device memory of the caller (aligned to 8): what the norm leaves for the calls
+ * after it, so that the host need not wait between them. */
+typedef struct mist_step_record {
+  double total;    /* sum of squares (or largest magnitude) of the gradients as stored */
+  int64_t step;    /* updates applied so far, this one included */
+  float norm;      /* |grad_scale| * sqrt(total) (or |grad_scale| * total) */
+  float coef;      /* factor of the stored gradients: grad_scale, times max_norm / norm where norm > max_norm */
+  int32_t applied; /* 1; 0 when the norm is inf or NaN: the step changes nothing */
+  int32_t skipped; /* steps so far that changed nothing */
+} mist_step_record;
+
+typedef struct mist_clip_desc {
+  int32_t kind;      /* MIST_NORM_L2 or MIST_NORM_MAX */
+  float grad_scale;  /* factor of the stored gradients (1 / loss scale, 1 / microbatches), finite, not 0 */
+  double max_norm;   /* > 0; +inf: no clipping */
+} mist_clip_desc;
+
+/* Scratch bytes of mist_grad_norm.  Errors: MIST_E_INVALID. */
+mist_status mist_norm_workspace(const mist_tensors* g, size_t* bytes);
+
+/* record->total = the gradients' sum of squares (kind MIST_NORM_L2) or largest magnitude
+ * (MIST_NORM_MAX), in 64 bits, joined with the total already there if accumulate = 1 (a step whose
+ * gradients are in several lists).  finish = 1 also does what mist_grad_finish does.  workspace: at least
+ * mist_norm_workspace bytes, aligned to 8.  Errors: MIST_E_INVALID, MIST_E_RANGE (workspace
+ * too small), MIST_E_DEVICE. */
+mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32_t accumulate, int32_t finish,
+                           mist_step_record* record, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Forms norm, coef and applied from record->total and counts the step.  Ranks that each hold a
+ * part of the gradients add up (or take the largest of) their totals first.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_grad_finish(const mist_clip_desc* c, mist_step_record* record, void* hip_stream);
+
+/* out = coef * g, tensor by tensor (the same count and sizes; of any type; out may be g).  With
+ * applied = 0 the values are carried over as they are, rounded to out's type.  Errors:
+ * MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record, const mist_tensors* out,
+                           void* hip_stream);
+
+typedef struct mist_adam_desc {
+  double lr;             /* >= 0 */
+  double beta1, beta2;   /* in [0, 1) */
+  double eps;            /* >= 0 */
+  double weight_decay;   /* >= 0, decoupled */
+} mist_adam_desc;
+
+/* The Adam step with decoupled weight decay, tensor by tensor: with t = record->step,
+ *     g' = coef * g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *     p = p - lr * ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay * p);
+ *     w = p rounded to w's type.
+ * p, m and v are MIST_F32 (bytes_opt = 12), g is of any type, w may be NULL (no 16-bit weights); all
+ * with g's count and sizes.  One step may be made in several calls, e.g. one per layer.  With applied = 0 (gradients
+ * with inf or NaN) it changes nothing.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const mist_tensors* v, const mist_tensors* g,
+                           const mist_tensors* w, const mist_step_record* record, const mist_adam_desc* a,
+                           void* hip_stream);
+
 /* Frees every buffer of the space (through its allocator).  NULL is accepted. */
 mist_status mist_space_destroy(mist_space* S);
 

@@ -1,0 +1,363 @@
+// Lists of tensors, the global gradient norm, clipping and the Adam step.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "mist_ops.h"
+
+using mist::hip_failed;
+using mist::lib_fail;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kChunk = 8192;     // elements a block takes at a time, of one tensor
+constexpr int64_t kMostPieces = (int64_t)1 << 23;  // a grid of a block each stays below 2^32 threads
+constexpr int kNormBlocks = 2048;    // partial results of the norm, at most
+
+// A block's piece of work: elements [part * kChunk, ...) of a tensor.
+struct Piece {
+  int32_t tensor, part;
+};
+
+// The tables as kernels see them.
+struct List {
+  const uint64_t* ptr;    // [n] addresses
+  const int64_t* size;    // [n] elements
+  const Piece* piece;     // [n_pieces]
+};
+
+}  // namespace
+
+struct mist_tensors {
+  int device = 0;
+  int32_t type = 0;
+  std::vector<int64_t> size;
+  int64_t n_pieces = 0;
+  List list{};
+  void* block = nullptr;  // the device tables
+  mist_allocator alloc{};
+  bool own_alloc = false;
+};
+
+namespace {
+
+struct Span {
+  uint64_t ptr;
+  int64_t begin, end;  // elements
+};
+
+__device__ __forceinline__ Span span_of(const List& l, const Piece p) {
+  const int64_t begin = (int64_t)p.part * kChunk, size = l.size[p.tensor];
+  return Span{l.ptr[p.tensor], begin, begin + kChunk < size ? begin + kChunk : size};
+}
+
+// Sum, or largest with NaN above everything, over a block; the result is in thread 0.
+template <bool MAX>
+__device__ __forceinline__ double join(double a, double b) {
+  if (!MAX) return a + b;
+  return a > b || a != a ? a : b;
+}
+template <bool MAX>
+__device__ double block_join(double x) {
+  __shared__ double part[kThreads / 64];
+  for (int d = 32; d; d >>= 1) x = join<MAX>(x, __shfl_down(x, d));
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
+  __syncthreads();
+  x = part[0];
+  for (int k = 1; k < kThreads / 64; ++k) x = join<MAX>(x, part[k]);
+  return x;
+}
+
+template <class G, bool MAX>
+__global__ __launch_bounds__(kThreads) void k_norm(List l, int64_t n_pieces, double* __restrict__ part) {
+  double sum = 0.0;
+  for (int64_t k = blockIdx.x; k < n_pieces; k += gridDim.x) {
+    const Span s = span_of(l, l.piece[k]);
+    const G* g = (const G*)s.ptr;
+    for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
+      const double x = (double)(float)g[i];
+      sum = MAX ? join<true>(sum, fabs(x)) : fma(x, x, sum);
+    }
+  }
+  sum = block_join<MAX>(sum);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+__device__ void finish(const mist_clip_desc& c, mist_step_record* r, double total) {
+  const double scale = fabs((double)c.grad_scale);
+  const double norm = scale * (c.kind == MIST_NORM_L2 ? sqrt(total) : total);
+  const bool fine = norm < HUGE_VAL;  // false for NaN
+  r->norm = (float)norm;
+  r->coef = fine ? (float)(c.grad_scale * (norm > c.max_norm ? c.max_norm / norm : 1.0)) : c.grad_scale;
+  r->applied = fine;
+  r->step += fine;
+  r->skipped += !fine;
+}
+
+// One block: joins the partial results in order.
+template <bool MAX>
+__global__ __launch_bounds__(kThreads) void k_total(const double* __restrict__ part, int32_t n, mist_clip_desc c, int32_t accumulate,
+                                                    int32_t do_finish, mist_step_record* r) {
+  double x = 0.0;
+  for (int32_t k = threadIdx.x; k < n; k += kThreads) x = join<MAX>(x, part[k]);
+  x = block_join<MAX>(x);
+  if (threadIdx.x) return;
+  if (accumulate) x = join<MAX>(r->total, x);
+  r->total = x;
+  if (do_finish) finish(c, r, x);
+}
+
+__global__ void k_finish(mist_clip_desc c, mist_step_record* r) { finish(c, r, r->total); }
+
+template <class G, class O>
+__global__ __launch_bounds__(kThreads) void k_clip(List g, List out, const mist_step_record* __restrict__ r) {
+  const Piece p = g.piece[blockIdx.x];
+  const Span s = span_of(g, p);
+  const float coef = r->applied ? r->coef : 1.0f;
+  const G* x = (const G*)s.ptr;
+  O* y = (O*)out.ptr[p.tensor];
+  for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) y[i] = (O)(coef * (float)x[i]);
+}
+
+struct AdamArgs {
+  List p, m, v, g, w;
+  double beta1, beta2;
+  float b1, b2, one_b1, one_b2, lr, keep, eps;  // keep = 1 - lr * weight_decay
+};
+
+__device__ double power(double x, int64_t n) {
+  double y = 1.0;
+  for (; n > 0; n >>= 1, x *= x)
+    if (n & 1) y *= x;
+  return y;
+}
+
+template <class G, class W, bool WEIGHTS>
+__global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, const mist_step_record* __restrict__ r) {
+  if (!r->applied) return;
+  const Piece piece = a.g.piece[blockIdx.x];
+  const Span s = span_of(a.g, piece);
+  const float coef = r->coef;
+  const float ibc1 = (float)(1.0 / (1.0 - power(a.beta1, r->step))), ibc2 = (float)(1.0 / (1.0 - power(a.beta2, r->step)));
+  const G* g = (const G*)s.ptr;
+  float* p = (float*)a.p.ptr[piece.tensor];
+  float* m = (float*)a.m.ptr[piece.tensor];
+  float* v = (float*)a.v.ptr[piece.tensor];
+  W* w = WEIGHTS ? (W*)a.w.ptr[piece.tensor] : nullptr;
+  for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
+    const float x = coef * (float)g[i];
+    const float mi = fmaf(a.b1, m[i], a.one_b1 * x);
+    const float vi = fmaf(a.b2, v[i], a.one_b2 * x * x);
+    float pi = fmaf(-a.lr, mi * ibc1 / (sqrtf(vi * ibc2) + a.eps), a.keep * p[i]);
+    asm("" : "+v"(pi));  // w is the stored p rounded, not the sum rounded once to 16 bits
+    m[i] = mi;
+    v[i] = vi;
+    p[i] = pi;
+    if (WEIGHTS) w[i] = (W)pi;
+  }
+}
+
+void release(mist_tensors* T) {
+  if (!T) return;
+  int cur = 0;
+  const bool known = hipGetDevice(&cur) == hipSuccess;
+  if (known && cur != T->device) (void)hipSetDevice(T->device);
+  if (T->block) {
+    (void)hipDeviceSynchronize();
+    if (T->own_alloc) (void)hipFree(T->block);
+    else T->alloc.free(T->block, T->alloc.ctx);
+  }
+  if (known && cur != T->device) (void)hipSetDevice(cur);
+  delete T;
+}
+
+mist_status on_device(const mist_tensors* T, const char* what) {
+  int dev = -1;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_failed(e, what);
+  if (dev != T->device) return lib_fail(MIST_E_INVALID, "tensor list: another device is current than the list's");
+  return MIST_OK;
+}
+
+mist_status like(const mist_tensors* a, const mist_tensors* b) {
+  if (a == b) return MIST_OK;
+  if (a->device != b->device) return lib_fail(MIST_E_INVALID, "tensor lists are on different devices");
+  if (a->size != b->size) return lib_fail(MIST_E_INVALID, "tensor lists differ in count or sizes");
+  return MIST_OK;
+}
+
+bool clip_ok(const mist_clip_desc* c) {
+  return (c->kind == MIST_NORM_L2 || c->kind == MIST_NORM_MAX) && std::isfinite(c->grad_scale) && c->grad_scale != 0.0f &&
+         c->max_norm > 0.0;
+}
+
+bool aligned8(const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; }
+
+int32_t norm_blocks(const mist_tensors* g) { return (int32_t)(g->n_pieces < kNormBlocks ? g->n_pieces : kNormBlocks); }
+
+}  // namespace
+
+extern "C" {
+
+mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, int64_t n, int32_t type,
+                                const mist_allocator* alloc, mist_tensors** out) {
+  if (!out) return lib_fail(MIST_E_INVALID, "tensor list: null argument");
+  *out = nullptr;
+  if (n < 0 || n > INT32_MAX || (n && (!ptrs || !sizes))) return lib_fail(MIST_E_INVALID, "tensor list: null argument or bad count");
+  if (!mist::type_ok(type)) return lib_fail(MIST_E_INVALID, "tensor list: unknown element type");
+  if (alloc && (!alloc->alloc || !alloc->free)) return lib_fail(MIST_E_INVALID, "tensor list: allocator without functions");
+  const int64_t bytes = mist::type_bytes(type);
+  int64_t pieces = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (sizes[i] < 0 || sizes[i] > ((int64_t)1 << 42)) return lib_fail(MIST_E_INVALID, "tensor list: sizes must be in 0..2^42");
+    if (sizes[i] && (!ptrs[i] || reinterpret_cast<uintptr_t>(ptrs[i]) % bytes))
+      return lib_fail(MIST_E_INVALID, "tensor list: a tensor is null or not aligned to its elements");
+    pieces += (sizes[i] + kChunk - 1) / kChunk;
+    if (pieces > kMostPieces) return lib_fail(MIST_E_INVALID, "tensor list: too many elements (over about 2^36)");
+  }
+  mist_tensors* T = nullptr;
+  try {
+    T = new mist_tensors;
+    T->type = type;
+    T->size.assign(sizes, sizes + n);
+    T->n_pieces = pieces;
+    hipError_t e = hipGetDevice(&T->device);
+    if (e == hipSuccess && pieces) {
+      // one block: addresses, sizes, pieces (8 bytes each)
+      std::vector<uint64_t> table((size_t)(2 * n + pieces));
+      Piece* piece = reinterpret_cast<Piece*>(table.data() + 2 * n);
+      for (int64_t i = 0; i < n; ++i) {
+        table[(size_t)i] = (uint64_t)reinterpret_cast<uintptr_t>(ptrs[i]);
+        table[(size_t)(n + i)] = (uint64_t)sizes[i];
+        for (int64_t k = 0; k * kChunk < sizes[i]; ++k) *piece++ = Piece{(int32_t)i, (int32_t)k};
+      }
+      const size_t total = table.size() * 8;
+      if (alloc) {
+        T->alloc = *alloc;
+        T->block = alloc->alloc(total, nullptr, alloc->ctx);
+      } else {
+        T->own_alloc = true;
+        if (hipMalloc(&T->block, total) != hipSuccess) {
+          (void)hipGetLastError();
+          T->block = nullptr;
+        }
+      }
+      if (!T->block) {
+        release(T);
+        return lib_fail(MIST_E_NOMEM, "tensor list: device memory");
+      }
+      // the copy is on the null stream; callers use other streams, so it is waited for
+      e = hipMemcpy(T->block, table.data(), total, hipMemcpyHostToDevice);
+      if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+      T->list = List{(const uint64_t*)T->block, (const int64_t*)T->block + n, (const Piece*)((const uint64_t*)T->block + 2 * n)};
+    }
+    if (e != hipSuccess) {
+      release(T);
+      return hip_failed(e, "tensor list");
+    }
+  } catch (...) {
+    release(T);
+    return lib_fail(MIST_E_NOMEM, "tensor list: host memory");
+  }
+  *out = T;
+  return MIST_OK;
+}
+
+mist_status mist_tensors_destroy(mist_tensors* T) {
+  release(T);
+  return MIST_OK;
+}
+
+mist_status mist_norm_workspace(const mist_tensors* g, size_t* bytes) {
+  if (!g || !bytes) return lib_fail(MIST_E_INVALID, "gradient norm: null argument");
+  *bytes = (size_t)norm_blocks(g) * 8;
+  return MIST_OK;
+}
+
+mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32_t accumulate, int32_t do_finish,
+                           mist_step_record* record, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!g || !c || !record) return lib_fail(MIST_E_INVALID, "gradient norm: null argument");
+  if (!clip_ok(c)) return lib_fail(MIST_E_INVALID, "gradient norm: unknown kind, or grad_scale or max_norm out of range");
+  if (accumulate != 0 && accumulate != 1) return lib_fail(MIST_E_INVALID, "gradient norm: accumulate must be 0 or 1");
+  if (do_finish != 0 && do_finish != 1) return lib_fail(MIST_E_INVALID, "gradient norm: finish must be 0 or 1");
+  const int32_t blocks = norm_blocks(g);
+  if (blocks && !workspace) return lib_fail(MIST_E_INVALID, "gradient norm: null workspace");
+  if (workspace_bytes < (size_t)blocks * 8) return lib_fail(MIST_E_RANGE, "gradient norm: workspace too small");
+  if (!aligned8(workspace) || !aligned8(record)) return lib_fail(MIST_E_INVALID, "gradient norm: workspace or record not aligned to 8");
+  if (const mist_status st = on_device(g, "gradient norm")) return st;
+  const hipStream_t st = (hipStream_t)stream;
+  double* part = (double*)workspace;
+  if (blocks) {
+    mist::with_type(g->type, [&](auto x) {
+      using G = typename decltype(x)::type;
+      if (c->kind == MIST_NORM_MAX)
+        hipLaunchKernelGGL((k_norm<G, true>), dim3(blocks), dim3(kThreads), 0, st, g->list, g->n_pieces, part);
+      else
+        hipLaunchKernelGGL((k_norm<G, false>), dim3(blocks), dim3(kThreads), 0, st, g->list, g->n_pieces, part);
+    });
+  }
+  if (c->kind == MIST_NORM_MAX)
+    hipLaunchKernelGGL(k_total<true>, dim3(1), dim3(kThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
+  else
+    hipLaunchKernelGGL(k_total<false>, dim3(1), dim3(kThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? MIST_OK : hip_failed(e, "gradient norm");
+}
+
+mist_status mist_grad_finish(const mist_clip_desc* c, mist_step_record* record, void* stream) {
+  if (!c || !record) return lib_fail(MIST_E_INVALID, "gradient norm: null argument");
+  if (!clip_ok(c)) return lib_fail(MIST_E_INVALID, "gradient norm: unknown kind, or grad_scale or max_norm out of range");
+  if (!aligned8(record)) return lib_fail(MIST_E_INVALID, "gradient norm: record not aligned to 8");
+  hipLaunchKernelGGL(k_finish, dim3(1), dim3(1), 0, (hipStream_t)stream, *c, record);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? MIST_OK : hip_failed(e, "gradient norm");
+}
+
+mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record, const mist_tensors* out, void* stream) {
+  if (!g || !record || !out) return lib_fail(MIST_E_INVALID, "clipping: null argument");
+  if (!aligned8(record)) return lib_fail(MIST_E_INVALID, "clipping: record not aligned to 8");
+  if (const mist_status st = like(g, out)) return st;
+  if (const mist_status st = on_device(g, "clipping")) return st;
+  if (!g->n_pieces) return MIST_OK;
+  mist::with_types(g->type, out->type, [&](auto x, auto y) {
+    using G = typename decltype(x)::type;
+    using O = typename decltype(y)::type;
+    hipLaunchKernelGGL((k_clip<G, O>), dim3((unsigned)g->n_pieces), dim3(kThreads), 0, (hipStream_t)stream, g->list, out->list, record);
+  });
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? MIST_OK : hip_failed(e, "clipping");
+}
+
+mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const mist_tensors* v, const mist_tensors* g,
+                           const mist_tensors* w, const mist_step_record* record, const mist_adam_desc* a, void* stream) {
+  if (!p || !m || !v || !g || !record || !a) return lib_fail(MIST_E_INVALID, "Adam step: null argument");
+  if (!aligned8(record)) return lib_fail(MIST_E_INVALID, "Adam step: record not aligned to 8");
+  if (p->type != MIST_F32 || m->type != MIST_F32 || v->type != MIST_F32)
+    return lib_fail(MIST_E_INVALID, "Adam step: master weights, m and v must be MIST_F32");
+  if (p == m || p == v || m == v || p == g || m == g || v == g || (w && (w == p || w == m || w == v || w == g)))
+    return lib_fail(MIST_E_INVALID, "Adam step: the lists must be distinct");
+  if (!(a->lr >= 0.0 && std::isfinite(a->lr)) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0) ||
+      !(a->eps >= 0.0 && std::isfinite(a->eps)) || !(a->weight_decay >= 0.0 && std::isfinite(a->weight_decay)))
+    return lib_fail(MIST_E_INVALID, "Adam step: lr, beta, eps or weight_decay out of range");
+  for (const mist_tensors* t : {p, m, v, w ? w : g})
+    if (const mist_status st = like(g, t)) return st;
+  if (const mist_status st = on_device(g, "Adam step")) return st;
+  if (!g->n_pieces) return MIST_OK;
+  AdamArgs k{p->list, m->list, v->list, g->list, w ? w->list : List{}, a->beta1, a->beta2,
+             (float)a->beta1, (float)a->beta2, (float)(1.0 - a->beta1), (float)(1.0 - a->beta2),
+             (float)a->lr, (float)(1.0 - a->lr * a->weight_decay), (float)a->eps};
+  const dim3 grid((unsigned)g->n_pieces), block(kThreads);
+  mist::with_types(g->type, w ? w->type : MIST_F32, [&](auto x, auto y) {
+    using G = typename decltype(x)::type;
+    using W = typename decltype(y)::type;
+    if (w) hipLaunchKernelGGL((k_adam<G, W, true>), grid, block, 0, (hipStream_t)stream, k, record);
+    else if constexpr (sizeof(W) == 4) hipLaunchKernelGGL((k_adam<G, W, false>), grid, block, 0, (hipStream_t)stream, k, record);
+  });
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? MIST_OK : hip_failed(e, "Adam step");
+}
+
+}  // extern "C"

@@ -29,6 +29,8 @@ EXPORTS = [
     "mist_corun_create", "mist_corun_run", "mist_corun_reduce", "mist_corun_measure", "mist_corun_destroy",
     "mist_fit_phi", "mist_interference", "mist_measure_eta", "mist_probe_fp64",
     "mist_search_info", "mist_tile_info", "mist_debug_eval_tiles", "mist_eval_ids_noalloc", "mist_exact_group_sizes",
+    "mist_embed_forward", "mist_embed_workspace", "mist_embed_backward", "mist_tensors_create", "mist_tensors_destroy",
+    "mist_norm_workspace", "mist_grad_norm", "mist_grad_finish", "mist_grad_clip", "mist_adam_step",
 ]
 
 PROBE_KINDS = {"add": 0, "mul": 1, "fma": 2, "min": 3, "max": 4, "cmp": 5}
@@ -126,6 +128,22 @@ class GroupKey(ctypes.Structure):
                [("base", ctypes.c_uint64), ("size", ctypes.c_uint64)]
 
 
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in
+                ["batch", "seq", "hidden", "rows", "vocab_begin", "ids_stride", "act_batch_stride", "act_stride",
+                 "table_stride", "pos_stride"]] + \
+               [("ids_bytes", ctypes.c_int32), ("act_type", ctypes.c_int32), ("table_type", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class ClipDesc(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("grad_scale", ctypes.c_float), ("max_norm", ctypes.c_double)]
+
+
+class AdamDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ["lr", "beta1", "beta2", "eps", "weight_decay"]]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -181,6 +199,17 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         L.mist_debug_eval_tiles.argtypes = [vp, P(ctypes.c_int32), ctypes.c_int32, P(ctypes.c_double),
                                             ctypes.c_int64, vp]
         L.mist_probe_fp64.argtypes = [ctypes.c_int32, vp, vp, ctypes.c_int64, ctypes.c_int32, P(ctypes.c_uint64), vp]
+        i32, sz = ctypes.c_int32, ctypes.c_size_t
+        L.mist_embed_forward.argtypes = [P(EmbedDesc), vp, vp, vp, vp, vp]
+        L.mist_embed_workspace.argtypes = [P(EmbedDesc), P(sz)]
+        L.mist_embed_backward.argtypes = [P(EmbedDesc), vp, vp, vp, vp, i32, vp, sz, vp]
+        L.mist_tensors_create.argtypes = [P(vp), P(ctypes.c_int64), ctypes.c_int64, i32, P(Allocator), P(vp)]
+        L.mist_tensors_destroy.argtypes = [vp]
+        L.mist_norm_workspace.argtypes = [vp, P(sz)]
+        L.mist_grad_norm.argtypes = [vp, P(ClipDesc), i32, i32, vp, vp, sz, vp]
+        L.mist_grad_finish.argtypes = [P(ClipDesc), vp, vp]
+        L.mist_grad_clip.argtypes = [vp, vp, vp, vp]
+        L.mist_adam_step.argtypes = [vp, vp, vp, vp, vp, vp, P(AdamDesc), vp]
         L.mist_last_error.restype = ctypes.c_char_p
         for name in EXPORTS:
             if name != "mist_last_error":
@@ -219,6 +248,30 @@ def _stream_handle(stream):
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _torch_allocator(failures: list):
+    """PyTorch's caching allocator on the current device as the library's callbacks; the callbacks are
+    returned too, to be kept as long as the library may call them."""
+    import torch
+    device = torch.cuda.current_device()
+
+    def alloc(nbytes, stream, ctx):
+        # the block joins the pool of the stream the library uses it on (NULL: the null stream)
+        try:
+            return torch.cuda.caching_allocator_alloc(int(nbytes), device, int(stream or 0))
+        except Exception as e:  # no exception may cross the C ABI
+            failures.append(e)
+            return None
+
+    def free(ptr, ctx):
+        try:
+            torch.cuda.caching_allocator_delete(ptr)
+        except Exception as e:
+            failures.append(e)
+
+    cb = (ALLOC_FN(alloc), FREE_FN(free))
+    return Allocator(cb[0], cb[1], None), cb
 
 
 class Space:
@@ -270,26 +323,9 @@ class Space:
         self.n_configs, self.n_groups, self.n_buckets = n.value, g.value, nb.value
 
     def _torch_allocator(self):
-        import torch
-        device = torch.cuda.current_device()
-        failures = self._alloc_failures = []
-
-        def alloc(nbytes, stream, ctx):
-            # the block joins the pool of the stream the library uses it on (NULL: the null stream)
-            try:
-                return torch.cuda.caching_allocator_alloc(int(nbytes), device, int(stream or 0))
-            except Exception as e:  # no exception may cross the C ABI
-                failures.append(e)
-                return None
-
-        def free(ptr, ctx):
-            try:
-                torch.cuda.caching_allocator_delete(ptr)
-            except Exception as e:
-                failures.append(e)
-
-        self._cb = (ALLOC_FN(alloc), FREE_FN(free))
-        return Allocator(self._cb[0], self._cb[1], None)
+        self._alloc_failures = []
+        allocator, self._cb = _torch_allocator(self._alloc_failures)
+        return allocator
 
     # -- evaluation ---------------------------------------------------------------
     def eval(self, stream=None) -> None:
@@ -612,3 +648,254 @@ class Corun:
 
     def __exit__(self, *exc):
         self.close()
+
+
+# -- operators of a training step's two ends ---------------------------------------------------
+E_INVALID = -1
+_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_NORMS = {"l2": 0, "max": 1}
+
+
+def _type(t, what: str) -> int:
+    code = _TYPES.get(str(t.dtype))
+    if code is None:
+        raise MistError(E_INVALID, "%s: %s is not float32, bfloat16 or float16" % (what, t.dtype))
+    return code
+
+
+def _need(ok: bool, msg: str) -> None:
+    if not ok:
+        raise MistError(E_INVALID, msg)
+
+
+class _On:
+    """The stream of one call: its handle, scratch memory of its pool, and the note to the caching
+    allocator that tensors are used on it when it is not the current one."""
+
+    def __init__(self, stream, device):
+        import torch
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+        self.stream, self.device = stream, device
+        self.handle = _stream_handle(stream)
+
+    def scratch(self, nbytes: int):
+        import torch
+        if self.stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def use(self, *tensors) -> None:
+        if self.stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+
+def _embed_desc(ids, act, table, scale, pos, vocab_begin) -> EmbedDesc:
+    for name, t in (("ids", ids), ("the activations", act), ("the table", table)) + ((("the positions", pos),) if pos is not None else ()):
+        _need(t.device == act.device and t.is_cuda, "embedding: %s must be on the activations' GPU" % name)
+    _need(str(ids.dtype) in ("torch.int32", "torch.int64"), "embedding: ids must be int32 or int64")
+    _need(ids.dim() in (1, 2) and act.dim() == ids.dim() + 1 and act.shape[:-1] == ids.shape,
+          "embedding: ids must be [seq] or [batch, seq], the activations ids' shape and hidden")
+    seq = ids.shape[-1]
+    batch = ids.shape[0] if ids.dim() == 2 else 1
+    hidden = act.shape[-1]
+    _need(table.dim() == 2 and table.shape[1] == hidden, "embedding: the table must be [rows, hidden]")
+    _need(pos is None or (pos.dim() == 2 and pos.shape[1] == hidden and pos.shape[0] >= seq),
+          "embedding: the positions must be [at least seq, hidden]")
+    _need(pos is None or pos.dtype == table.dtype, "embedding: the positions must have the table's type")
+    for t in (act, table) + (() if pos is None else (pos,)):
+        _need(t.stride(-1) == 1 or hidden == 1 or t.numel() == 0, "embedding: the hidden dimension must be contiguous")
+    _need(seq <= 1 or ids.stride(-1) == 1 or batch == 0, "embedding: the ids of a sequence must be contiguous")
+    d = EmbedDesc()
+    d.batch, d.seq, d.hidden, d.rows, d.vocab_begin = batch, seq, hidden, table.shape[0], int(vocab_begin)
+    d.ids_stride = ids.stride(0) if ids.dim() == 2 else 0
+    d.act_batch_stride = act.stride(0) if ids.dim() == 2 else 0
+    d.act_stride = act.stride(-2)
+    d.table_stride = table.stride(0)
+    d.pos_stride = pos.stride(0) if pos is not None else 0
+    d.ids_bytes = ids.element_size()
+    d.act_type, d.table_type = _type(act, "embedding"), _type(table, "embedding")
+    d.scale = float(scale)
+    return d
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out=None, stream=None):
+    """mist_embed_forward: scale * table[ids - vocab_begin] + pos[position], zero in the first term for ids
+    outside the shard (padding, other ranks' rows).  ids: [seq] or [batch, seq], int32 or int64 (batch strides
+    allowed); table: [rows, hidden]; pos: [at least seq, hidden] or None; out: ids' shape + [hidden], of
+    any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
+    import torch
+    L = load()
+    on = _On(stream, table.device)
+    if out is None:
+        _need(table.dim() == 2, "embedding: the table must be [rows, hidden]")
+        shape = tuple(ids.shape) + (table.shape[1],)
+        with torch.cuda.stream(on.stream):
+            out = torch.empty(shape, dtype=table.dtype, device=table.device)
+    d = _embed_desc(ids, out, table, scale, pos, vocab_begin)
+    with torch.cuda.device(table.device):
+        _check(L, L.mist_embed_forward(ctypes.byref(d), _ptr(ids), _ptr(table), _ptr(pos), _ptr(out), on.handle))
+    on.use(ids, table, pos, out)
+    return out
+
+
+def embed_grad(ids, grad, dtable, *, scale: float = 1.0, dpos=None, vocab_begin: int = 0, accumulate: bool = False,
+               stream=None):
+    """mist_embed_backward: the gradients of embed's table and positions from grad (ids' shape + [hidden]; it
+    may be expanded), written to dtable and dpos (accumulate: added to them)."""
+    import torch
+    L = load()
+    d = _embed_desc(ids, grad, dtable, scale, dpos, vocab_begin)
+    on = _On(stream, grad.device)
+    need = ctypes.c_size_t()
+    with torch.cuda.device(grad.device):
+        _check(L, L.mist_embed_workspace(ctypes.byref(d), ctypes.byref(need)))
+        ws = on.scratch(need.value)
+        _check(L, L.mist_embed_backward(ctypes.byref(d), _ptr(ids), _ptr(grad), _ptr(dtable), _ptr(dpos),
+                                        1 if accumulate else 0, _ptr(ws), need.value, on.handle))
+    on.use(ids, grad, dtable, dpos)
+    return dtable
+
+
+class TensorList:
+    """Tensors of one type on the current GPU as one list (mist_tensors_create), e.g. a stage's gradients.  They
+    must be contiguous and stay where they are; the list keeps them alive."""
+
+    def __init__(self, tensors, allocator: str | None = "torch"):
+        import torch
+        self.h = None
+        self.L = load()
+        self.tensors = list(tensors)
+        _need(len(self.tensors) > 0, "tensor list: no tensors")
+        t0 = self.tensors[0]
+        self.dtype, self.device = t0.dtype, t0.device
+        for t in self.tensors:
+            _need(t.is_cuda and t.device == self.device and t.dtype == self.dtype,
+                  "tensor list: the tensors must be of one type on one GPU")
+            _need(t.is_contiguous(), "tensor list: the tensors must be contiguous")
+        n = len(self.tensors)
+        ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
+        _need(allocator in ("torch", None), "allocator must be 'torch' or None")
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            self._alloc = None
+            if allocator == "torch":
+                self._alloc, self._cb = _torch_allocator([])
+            _check(self.L, self.L.mist_tensors_create(ptrs, sizes, n, _type(t0, "tensor list"),
+                                                      ctypes.byref(self._alloc) if self._alloc else None,
+                                                      ctypes.byref(h)))
+            self.h = h
+            need = ctypes.c_size_t()
+            _check(self.L, self.L.mist_norm_workspace(self.h, ctypes.byref(need)))
+        self._norm_bytes = need.value
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+    def close(self) -> None:
+        if getattr(self, "h", None):
+            self.L.mist_tensors_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+class StepRecord:
+    """A mist_step_record on the GPU; the fields are 0-dimensional tensors that share its memory."""
+
+    def __init__(self, step: int = 0, device=None):
+        import torch
+        self.data = torch.zeros(4, dtype=torch.float64, device="cuda" if device is None else device)
+        self.total = self.data[0]
+        self.step = self.data.view(torch.int64)[1]
+        f, i = self.data.view(torch.float32), self.data.view(torch.int32)
+        self.norm, self.coef = f[4], f[5]
+        self.applied, self.skipped = i[6], i[7]
+        if step:
+            self.step.fill_(int(step))
+
+
+def _clip_desc(kind, grad_scale, max_norm) -> ClipDesc:
+    _need(kind in _NORMS, "gradient norm: kind must be 'l2' or 'max'")
+    return ClipDesc(_NORMS[kind], float(grad_scale), float(max_norm))
+
+
+def _handles(*lists):
+    for x in lists:
+        _need(x is None or x.h is not None, "tensor list: closed")
+    return [None if x is None else x.h for x in lists]
+
+
+def grad_norm(grads, record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
+              accumulate: bool = False, finish: bool = True, stream=None) -> StepRecord:
+    """mist_grad_norm over a TensorList: record.total, and with finish the norm, the clip factor and the count of
+    the step.  Nothing is waited for.  accumulate joins record.total (a step with several lists)."""
+    import torch
+    c = _clip_desc(kind, grad_scale, max_norm)
+    (h,) = _handles(grads)
+    _need(record.data.device == grads.device, "step record: on another device than the gradients")
+    on = _On(stream, grads.device)
+    with torch.cuda.device(grads.device):
+        ws = on.scratch(grads._norm_bytes)
+        _check(grads.L, grads.L.mist_grad_norm(h, ctypes.byref(c), 1 if accumulate else 0, 1 if finish else 0,
+                                               record.data.data_ptr(), _ptr(ws), grads._norm_bytes, on.handle))
+    on.use(record.data)
+    return record
+
+
+def grad_finish(record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
+                stream=None) -> StepRecord:
+    """mist_grad_finish: forms the norm and the clip factor from record.total, e.g. after an all-reduce of it."""
+    import torch
+    L = load()
+    c = _clip_desc(kind, grad_scale, max_norm)
+    on = _On(stream, record.data.device)
+    with torch.cuda.device(record.data.device):
+        _check(L, L.mist_grad_finish(ctypes.byref(c), record.data.data_ptr(), on.handle))
+    on.use(record.data)
+    return record
+
+
+def grad_clip(grads: TensorList, record: StepRecord, out: TensorList | None = None, *, stream=None) -> None:
+    """mist_grad_clip: out = record.coef * grads (out None: in place)."""
+    import torch
+    out = grads if out is None else out
+    g, o = _handles(grads, out)
+    _need(record.data.device == grads.device, "step record: on another device than the gradients")
+    on = _On(stream, grads.device)
+    with torch.cuda.device(grads.device):
+        _check(grads.L, grads.L.mist_grad_clip(g, record.data.data_ptr(), o, on.handle))
+    on.use(record.data, *grads.tensors, *out.tensors)
+
+
+def adam_step(master: TensorList, m: TensorList, v: TensorList, grads: TensorList, record: StepRecord, *, lr: float,
+              betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, weights: TensorList | None = None,
+              stream=None) -> None:
+    """mist_adam_step with record's clip factor and step count; weights receives the rounded master weights."""
+    import torch
+    hp, hm, hv, hg, hw = _handles(master, m, v, grads, weights)
+    _need(record.data.device == grads.device, "step record: on another device than the gradients")
+    a = AdamDesc(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay))
+    on = _On(stream, grads.device)
+    with torch.cuda.device(grads.device):
+        _check(grads.L, grads.L.mist_adam_step(hp, hm, hv, hg, hw, record.data.data_ptr(), ctypes.byref(a), on.handle))
+    if stream is not None:
+        on.use(record.data, *(t for x in (master, m, v, grads, weights) if x is not None for t in x.tensors))
