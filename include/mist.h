@@ -508,7 +508,7 @@ mist_status mist_probe_fp64(int32_t kind, const double* in, uint64_t* out, int64
  * such as -1) finds the zero row and gives no gradient.  Strides are in elements; the hidden
  * dimension is contiguous. */
 typedef struct mist_embed_desc {
-  int64_t batch, seq;      /* >= 0; batch * seq < 2^31 */
+  int64_t batch, seq;      /* >= 0; batch * seq < 2^30 */
   int64_t hidden;          /* 1..2^24 */
   int64_t rows;            /* 1..2^31 - 2 */
   int64_t vocab_begin;     /* id of the shard's first row, in [0, 2^31) */
