@@ -33,6 +33,13 @@ struct Elem<MIST_F16> {
   using type = _Float16;
 };
 
+// N consecutive values, read and written by instructions of up to 16 bytes.  They need only their element's
+// alignment (the device's global memory instructions take any), so that shards and odd rows take the same path.
+template <class T, int N>
+struct Vec {
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
 inline int64_t type_bytes(int32_t type) { return type == MIST_F32 ? 4 : 2; }
 inline bool type_ok(int32_t type) { return type == MIST_F32 || type == MIST_BF16 || type == MIST_F16; }
 

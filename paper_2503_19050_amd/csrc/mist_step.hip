@@ -9,10 +9,12 @@
 
 using mist::hip_failed;
 using mist::lib_fail;
+using mist::Vec;
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kTotalThreads = 1024;
 constexpr int64_t kChunk = 8192;     // elements a block takes at a time, of one tensor
 constexpr int64_t kMostPieces = (int64_t)1 << 23;  // a grid of a block each stays below 2^32 threads
 constexpr int kNormBlocks = 2048;    // partial results of the norm, at most
@@ -60,29 +62,49 @@ __device__ __forceinline__ double join(double a, double b) {
   if (!MAX) return a + b;
   return a > b || a != a ? a : b;
 }
-template <bool MAX>
+template <bool MAX, int THREADS>
 __device__ double block_join(double x) {
-  __shared__ double part[kThreads / 64];
+  __shared__ double part[THREADS / 64];
   for (int d = 32; d; d >>= 1) x = join<MAX>(x, __shfl_down(x, d));
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
   __syncthreads();
   x = part[0];
-  for (int k = 1; k < kThreads / 64; ++k) x = join<MAX>(x, part[k]);
+  for (int k = 1; k < THREADS / 64; ++k) x = join<MAX>(x, part[k]);
   return x;
 }
 
+// Reads only: pieces in turn, four loads of 16 bytes a thread in flight; the next piece's table entries are
+// read ahead.
 template <class G, bool MAX>
 __global__ __launch_bounds__(kThreads) void k_norm(List l, int64_t n_pieces, double* __restrict__ part) {
+  constexpr int kV = 16 / sizeof(G), kLoads = 4;
+  typedef typename Vec<G, kV>::type V;
   double sum = 0.0;
-  for (int64_t k = blockIdx.x; k < n_pieces; k += gridDim.x) {
-    const Span s = span_of(l, l.piece[k]);
-    const G* g = (const G*)s.ptr;
-    for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
-      const double x = (double)(float)g[i];
-      sum = MAX ? join<true>(sum, fabs(x)) : fma(x, x, sum);
+  auto add = [&](G g) {
+    const double x = (double)(float)g;
+    sum = MAX ? join<true>(sum, fabs(x)) : fma(x, x, sum);
+  };
+  int64_t k = blockIdx.x;
+  Span s = span_of(l, l.piece[k]);
+  for (; k < n_pieces; k += gridDim.x) {
+    const G* g = (const G*)s.ptr + s.begin;
+    const int n = (int)(s.end - s.begin), vectors = n / kV;
+    if (k + gridDim.x < n_pieces) s = span_of(l, l.piece[k + gridDim.x]);
+    for (int i0 = 0; i0 < vectors; i0 += kThreads * kLoads) {
+      V x[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int i = i0 + j * kThreads + threadIdx.x;
+        x[j] = i < vectors ? *(const V*)(g + i * kV) : V{};
+      }
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int c = 0; c < kV; ++c) add(x[j][c]);
     }
+    if (const int i = vectors * kV + threadIdx.x; i < n) add(g[i]);
   }
-  sum = block_join<MAX>(sum);
+  sum = block_join<MAX, kThreads>(sum);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -99,11 +121,11 @@ __device__ void finish(const mist_clip_desc& c, mist_step_record* r, double tota
 
 // One block: joins the partial results in order.
 template <bool MAX>
-__global__ __launch_bounds__(kThreads) void k_total(const double* __restrict__ part, int32_t n, mist_clip_desc c, int32_t accumulate,
+__global__ __launch_bounds__(kTotalThreads) void k_total(const double* __restrict__ part, int32_t n, mist_clip_desc c, int32_t accumulate,
                                                     int32_t do_finish, mist_step_record* r) {
   double x = 0.0;
-  for (int32_t k = threadIdx.x; k < n; k += kThreads) x = join<MAX>(x, part[k]);
-  x = block_join<MAX>(x);
+  for (int32_t k = threadIdx.x; k < n; k += kTotalThreads) x = join<MAX>(x, part[k]);
+  x = block_join<MAX, kTotalThreads>(x);
   if (threadIdx.x) return;
   if (accumulate) x = join<MAX>(r->total, x);
   r->total = x;
@@ -112,14 +134,33 @@ __global__ __launch_bounds__(kThreads) void k_total(const double* __restrict__ p
 
 __global__ void k_finish(mist_clip_desc c, mist_step_record* r) { finish(c, r, r->total); }
 
+// Pieces from the last to the first: what the norm has read last is still in the cache.
 template <class G, class O>
 __global__ __launch_bounds__(kThreads) void k_clip(List g, List out, const mist_step_record* __restrict__ r) {
-  const Piece p = g.piece[blockIdx.x];
+  constexpr int kV = sizeof(G) == 2 && sizeof(O) == 2 ? 8 : 4, kLoads = 4;
+  typedef typename Vec<G, kV>::type VG;
+  typedef typename Vec<O, kV>::type VO;
+  typedef typename Vec<float, kV>::type VF;
+  const Piece p = g.piece[gridDim.x - 1 - blockIdx.x];
   const Span s = span_of(g, p);
   const float coef = r->applied ? r->coef : 1.0f;
-  const G* x = (const G*)s.ptr;
-  O* y = (O*)out.ptr[p.tensor];
-  for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) y[i] = (O)(coef * (float)x[i]);
+  const G* x = (const G*)s.ptr + s.begin;
+  O* y = (O*)out.ptr[p.tensor] + s.begin;
+  const int n = (int)(s.end - s.begin), vectors = n / kV;
+  for (int i0 = 0; i0 < vectors; i0 += kThreads * kLoads) {
+    VG v[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = i0 + j * kThreads + threadIdx.x;
+      if (i < vectors) v[j] = *(const VG*)(x + i * kV);
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = i0 + j * kThreads + threadIdx.x;
+      if (i < vectors) *(VO*)(y + i * kV) = __builtin_convertvector(coef * __builtin_convertvector(v[j], VF), VO);
+    }
+  }
+  if (const int i = vectors * kV + threadIdx.x; i < n) y[i] = (O)(coef * (float)x[i]);
 }
 
 struct AdamArgs {
@@ -135,28 +176,68 @@ __device__ double power(double x, int64_t n) {
   return y;
 }
 
+struct AdamScalars {
+  float coef, ibc1, ibc2;
+};
+
+__device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamScalars& c, float g, float& p, float& m, float& v) {
+  const float x = c.coef * g;
+  m = fmaf(a.b1, m, a.one_b1 * x);
+  v = fmaf(a.b2, v, a.one_b2 * x * x);
+  p = fmaf(-a.lr, m * c.ibc1 / (sqrtf(v * c.ibc2) + a.eps), a.keep * p);
+  asm("" : "+v"(p));  // the weights are the stored p rounded, not the sum rounded once to 16 bits
+}
+
+// Pieces from the last to the first, as the clipping takes them.
 template <class G, class W, bool WEIGHTS>
 __global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, const mist_step_record* __restrict__ r) {
+  constexpr int kV = 4, kLoads = 2;
+  typedef typename Vec<G, kV>::type VG;
+  typedef typename Vec<W, kV>::type VW;
+  typedef typename Vec<float, kV>::type VF;
   if (!r->applied) return;
-  const Piece piece = a.g.piece[blockIdx.x];
+  const Piece piece = a.g.piece[gridDim.x - 1 - blockIdx.x];
   const Span s = span_of(a.g, piece);
-  const float coef = r->coef;
-  const float ibc1 = (float)(1.0 / (1.0 - power(a.beta1, r->step))), ibc2 = (float)(1.0 / (1.0 - power(a.beta2, r->step)));
-  const G* g = (const G*)s.ptr;
-  float* p = (float*)a.p.ptr[piece.tensor];
-  float* m = (float*)a.m.ptr[piece.tensor];
-  float* v = (float*)a.v.ptr[piece.tensor];
-  W* w = WEIGHTS ? (W*)a.w.ptr[piece.tensor] : nullptr;
-  for (int64_t i = s.begin + threadIdx.x; i < s.end; i += kThreads) {
-    const float x = coef * (float)g[i];
-    const float mi = fmaf(a.b1, m[i], a.one_b1 * x);
-    const float vi = fmaf(a.b2, v[i], a.one_b2 * x * x);
-    float pi = fmaf(-a.lr, mi * ibc1 / (sqrtf(vi * ibc2) + a.eps), a.keep * p[i]);
-    asm("" : "+v"(pi));  // w is the stored p rounded, not the sum rounded once to 16 bits
-    m[i] = mi;
-    v[i] = vi;
-    p[i] = pi;
-    if (WEIGHTS) w[i] = (W)pi;
+  const AdamScalars c{r->coef, (float)(1.0 / (1.0 - power(a.beta1, r->step))), (float)(1.0 / (1.0 - power(a.beta2, r->step)))};
+  const G* g = (const G*)s.ptr + s.begin;
+  float* p = (float*)a.p.ptr[piece.tensor] + s.begin;
+  float* m = (float*)a.m.ptr[piece.tensor] + s.begin;
+  float* v = (float*)a.v.ptr[piece.tensor] + s.begin;
+  W* w = WEIGHTS ? (W*)a.w.ptr[piece.tensor] + s.begin : nullptr;
+  const int n = (int)(s.end - s.begin), vectors = n / kV;
+  for (int i0 = 0; i0 < vectors; i0 += kThreads * kLoads) {
+    VG vg[kLoads];
+    VF vp[kLoads], vm[kLoads], vv[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = i0 + j * kThreads + threadIdx.x;
+      if (i < vectors) {
+        vg[j] = *(const VG*)(g + i * kV);
+        vp[j] = *(const VF*)(p + i * kV);
+        vm[j] = *(const VF*)(m + i * kV);
+        vv[j] = *(const VF*)(v + i * kV);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = i0 + j * kThreads + threadIdx.x;
+      if (i < vectors) {
+#pragma unroll
+        for (int k = 0; k < kV; ++k) {
+          float pk = vp[j][k], mk = vm[j][k], vk = vv[j][k];
+          adam_one(a, c, (float)vg[j][k], pk, mk, vk);
+          vp[j][k] = pk, vm[j][k] = mk, vv[j][k] = vk;
+        }
+        *(VF*)(p + i * kV) = vp[j];
+        *(VF*)(m + i * kV) = vm[j];
+        *(VF*)(v + i * kV) = vv[j];
+        if (WEIGHTS) *(VW*)(w + i * kV) = __builtin_convertvector(vp[j], VW);
+      }
+    }
+  }
+  if (const int i = vectors * kV + threadIdx.x; i < n) {
+    adam_one(a, c, (float)g[i], p[i], m[i], v[i]);
+    if (WEIGHTS) w[i] = (W)p[i];
   }
 }
 
@@ -300,9 +381,9 @@ mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32
     });
   }
   if (c->kind == MIST_NORM_MAX)
-    hipLaunchKernelGGL(k_total<true>, dim3(1), dim3(kThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
+    hipLaunchKernelGGL(k_total<true>, dim3(1), dim3(kTotalThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
   else
-    hipLaunchKernelGGL(k_total<false>, dim3(1), dim3(kThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
+    hipLaunchKernelGGL(k_total<false>, dim3(1), dim3(kTotalThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "gradient norm");
 }
