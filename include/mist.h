@@ -559,8 +559,9 @@ mist_status mist_tensors_destroy(mist_tensors* T);
 #define MIST_NORM_L2 0
 #define MIST_NORM_MAX 1
 
-/* State of a step, in device memory of the caller (aligned to 8): what the norm leaves for the calls
- * after it, so that the host need not wait between them. */
+/* State of a step, in device memory of the caller (aligned to 8; all zero at first, or with step set):
+ * what the norm leaves for the calls after it, so that the host need not wait between them.  One stream
+ * at a time. */
 typedef struct mist_step_record {
   double total;    /* sum of squares (or largest magnitude) of the gradients as stored */
   int64_t step;    /* updates applied so far, this one included */
@@ -576,7 +577,8 @@ typedef struct mist_clip_desc {
   double max_norm;   /* > 0; +inf: no clipping */
 } mist_clip_desc;
 
-/* Scratch bytes of mist_grad_norm.  Errors: MIST_E_INVALID. */
+/* Scratch bytes of mist_grad_norm, at most MIST_NORM_WORKSPACE.  Errors: MIST_E_INVALID. */
+#define MIST_NORM_WORKSPACE 16384
 mist_status mist_norm_workspace(const mist_tensors* g, size_t* bytes);
 
 /* record->total = the gradients' sum of squares (kind MIST_NORM_L2) or largest magnitude

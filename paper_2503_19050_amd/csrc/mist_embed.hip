@@ -14,13 +14,14 @@ namespace {
 
 using mist::hip_failed;
 using mist::lib_fail;
+using mist::Vec;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kVec = 8;             // values of a lane
 constexpr int kSlab = 64 * kVec;    // columns of a wave
 constexpr int64_t kMostTokens = (int64_t)1 << 30;  // places past the last token stay below 2^31
-constexpr int kChunk = 64;          // ordered tokens of a wave, one a lane
+constexpr int kMaxChunk = 64;       // ordered tokens of a wave, one a lane, at most
 
 struct EmbedArgs {
   int64_t batch, seq, hidden, rows, begin;
@@ -36,37 +37,32 @@ struct Entry {
   uint32_t row, token;
 };
 
-typedef float Float8 __attribute__((ext_vector_type(8), aligned(16)));
+typedef Vec<float, kVec>::type Float8;
 
-// Eight values of one lane.  VEC: consecutive, 16 bytes a load; otherwise 64 columns apart, one by one
-// (for rows that are not aligned to 16 bytes, or of a size that is no multiple of 8).
-template <bool VEC>
-__device__ __forceinline__ int64_t first_col(int32_t slab) {
-  const int lane = threadIdx.x % 64;
-  return (int64_t)slab * kSlab + (VEC ? lane * kVec : lane);
-}
+__device__ __forceinline__ int64_t first_col(int32_t slab) { return (int64_t)slab * kSlab + threadIdx.x % 64 * kVec; }
 
-template <class T, bool VEC>
+// Eight consecutive values of one lane; the last lane of a row may have fewer.
+template <class T>
 struct Lane8 {
-  typedef T type __attribute__((ext_vector_type(8), aligned(16)));
+  typedef typename Vec<T, kVec>::type type;
   type v;
   __device__ __forceinline__ void load(const T* row, int64_t col, int64_t hidden) {
-    if (VEC) {
-      v = col < hidden ? *(const type*)(row + col) : type{};
+    if (col + kVec <= hidden) {
+      v = *(const type*)(row + col);
     } else {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = col + 64 * k < hidden ? row[col + 64 * k] : (T)0.0f;
+      for (int k = 0; k < kVec; ++k) v[k] = col + k < hidden ? row[col + k] : (T)0.0f;
     }
   }
   __device__ __forceinline__ Float8 get() const { return __builtin_convertvector(v, Float8); }
   static __device__ __forceinline__ void store(T* row, int64_t col, int64_t hidden, Float8 x) {
     const type y = __builtin_convertvector(x, type);
-    if (VEC) {
-      if (col < hidden) *(type*)(row + col) = y;
+    if (col + kVec <= hidden) {
+      *(type*)(row + col) = y;
     } else {
 #pragma unroll
       for (int k = 0; k < kVec; ++k)
-        if (col + 64 * k < hidden) row[col + 64 * k] = y[k];
+        if (col + k < hidden) row[col + k] = y[k];
     }
   }
 };
@@ -100,7 +96,7 @@ __device__ __forceinline__ int64_t act_offset(const EmbedArgs& a, uint32_t token
 // the cache.
 constexpr int kAhead = 8;
 
-template <class A, class W, bool VEC, bool POS>
+template <class A, class W, bool POS>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wave, const void* __restrict__ ids,
                                                     const W* __restrict__ table, const W* __restrict__ pos, A* __restrict__ out) {
   const int64_t wave = wave_index();
@@ -115,9 +111,9 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
   const int64_t row_at = row < a.rows ? row * a.table_stride : -1;
   const int64_t out_at = act_offset(a, token);
   const uint32_t s = token % (uint32_t)a.seq;
-  const int64_t col = first_col<VEC>(slab);
+  const int64_t col = first_col(slab);
   for (int k0 = 0; k0 < count; k0 += kAhead) {
-    Lane8<W, VEC> x[kAhead], p[kAhead];
+    Lane8<W> x[kAhead], p[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (k0 + k < count) {
@@ -132,9 +128,47 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
       if (k0 + k < count) {
         Float8 y = a.scale * x[k].get();
         if (POS) y += p[k].get();
-        Lane8<A, VEC>::store(out + lane_value(out_at, k0 + k), col, a.hidden, y);
+        Lane8<A>::store(out + lane_value(out_at, k0 + k), col, a.hidden, y);
       }
     }
+  }
+}
+
+// ---- sums of the positions -------------------------------------------------------------------------
+// A wave takes a position and a slab, and adds up the batch.  The work is spread over the launches
+// that order the tokens, which leave most of the device idle: `block` of `blocks` more blocks takes the
+// waves' worth [begin, end) of the call.
+template <class A, class W>
+struct PosArgs {
+  const A* grad;
+  W* dpos;
+  int64_t begin, end;  // of seq * slabs
+  int32_t accumulate;
+};
+
+template <class A, class W>
+__device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32_t block, uint32_t blocks) {
+  const int32_t waves = blockDim.x / 64;
+  int64_t w = p.begin + __builtin_amdgcn_readfirstlane((int32_t)(block * waves + threadIdx.x / 64));
+  for (; w < p.end; w += (int64_t)blocks * waves) {
+    const int64_t s = w / a.slabs, col = first_col((int32_t)(w % a.slabs));
+    Float8 acc = {};
+    for (int64_t b0 = 0; b0 < a.batch; b0 += kAhead) {
+      Lane8<A> x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (b0 + k < a.batch) x[k].load(p.grad + (b0 + k) * a.act_batch_stride + s * a.act_stride, col, a.hidden);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (b0 + k < a.batch) acc += x[k].get();
+    }
+    W* d = p.dpos + s * a.pos_stride;
+    if (p.accumulate) {
+      Lane8<W> old;
+      old.load(d, col, a.hidden);
+      acc += old.get();
+    }
+    Lane8<W>::store(d, col, a.hidden, acc);
   }
 }
 
@@ -144,14 +178,31 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
 constexpr int32_t kCounted = 8192;   // tokens up to which places are counted
 constexpr int kPlaced = 16;
 
-__global__ __launch_bounds__(kThreads) void k_place(EmbedArgs a, const void* __restrict__ ids, Entry* __restrict__ out) {
-  __shared__ uint32_t row[kCounted];
-  for (int32_t i = threadIdx.x; i < a.n; i += kThreads) row[i] = token_row(a, ids, i);
+template <class A, class W>
+__global__ __launch_bounds__(kThreads) void k_place(EmbedArgs a, PosArgs<A, W> pos, const void* __restrict__ ids, Entry* __restrict__ out) {
+  const int32_t blocks = (a.n + kPlaced - 1) / kPlaced;
+  if ((int32_t)blockIdx.x >= blocks) {
+    sum_positions(a, pos, blockIdx.x - blocks, gridDim.x - blocks);
+    return;
+  }
+  __shared__ uint4 rows[kCounted / 4];
+  uint32_t* row = (uint32_t*)rows;
+  const int32_t steps = (a.n + 63) / 64;   // of 16 lanes by 4 tokens
+#pragma unroll 4
+  for (int32_t i = threadIdx.x; i < steps * 64; i += kThreads) row[i] = i < a.n ? token_row(a, ids, i) : UINT32_MAX;
   __syncthreads();
   const int32_t i = blockIdx.x * kPlaced + threadIdx.x / 16;
   const uint32_t mine = row[i < a.n ? i : 0];
   int32_t place = 0;
-  for (int32_t j = threadIdx.x % 16; j < a.n; j += 16) place += row[j] < mine || (row[j] == mine && j < i);
+#pragma unroll 4
+  for (int32_t t = 0; t < steps; ++t) {
+    const int32_t q = t * 16 + threadIdx.x % 16, j = q * 4;
+    const uint4 r = rows[q];
+    place += r.x < mine + (j < i);       // rows are below 2^31: r < mine, or equal and before
+    place += r.y < mine + (j + 1 < i);
+    place += r.z < mine + (j + 2 < i);
+    place += r.w < mine + (j + 3 < i);
+  }
   for (int d = 8; d; d >>= 1) place += __shfl_xor(place, d);
   if (threadIdx.x % 16 == 0 && i < a.n) out[place] = Entry{mine, (uint32_t)i};
 }
@@ -175,7 +226,12 @@ __device__ __forceinline__ Entry sort_entry(const EmbedArgs& a, const SortArgs& 
   return s.in ? s.in[i] : Entry{token_row(a, ids, i), (uint32_t)i};
 }
 
-__global__ __launch_bounds__(kSortThreads) void k_digits(EmbedArgs a, SortArgs s, const void* __restrict__ ids) {
+template <class A, class W>
+__global__ __launch_bounds__(kSortThreads) void k_digits(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
+  if ((int32_t)blockIdx.x >= s.tiles) {
+    sum_positions(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    return;
+  }
   __shared__ int32_t count[kMaxDigits];
   const int32_t digits = 1 << s.bits;
   for (int32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
@@ -197,29 +253,47 @@ __device__ __forceinline__ uint64_t equals(uint32_t digit, int bits, bool live) 
   return m;
 }
 
-__global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, const void* __restrict__ ids) {
+template <class A, class W>
+__global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
+  if ((int32_t)blockIdx.x >= s.tiles) {
+    sum_positions(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    return;
+  }
   __shared__ int32_t at[kSortWaves][kMaxDigits];  // counts, then places
-  __shared__ int32_t scan[kMaxDigits], before[kMaxDigits];
+  __shared__ int32_t total[kSortThreads], before[kSortThreads], wave_total[kMaxDigits / 64];
   const int32_t digits = 1 << s.bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   for (int32_t d = threadIdx.x; d < kSortWaves * kMaxDigits; d += kSortThreads) (&at[0][0])[d] = 0;
-  // digit d: its tokens in all tiles, and in the tiles before this one
-  if ((int32_t)threadIdx.x < digits) {
-    int32_t total = 0, mine = 0;
-    for (int32_t t = 0; t < s.tiles; ++t) {
-      const int32_t c = s.hist[t * digits + threadIdx.x];
-      total += c;
+  // a digit's tokens in all tiles, and in the tiles before this one; 1024 / digits threads a digit
+  {
+    const int32_t d = threadIdx.x % digits, parts = kSortThreads / digits, share = (s.tiles + parts - 1) / parts;
+    const int32_t t0 = threadIdx.x / digits * share, t1 = min(s.tiles, t0 + share);
+    int32_t all = 0, mine = 0;
+#pragma unroll 8
+    for (int32_t t = t0; t < t1; ++t) {
+      const int32_t c = s.hist[t * digits + d];
+      all += c;
       mine += t < (int32_t)blockIdx.x ? c : 0;
     }
-    scan[threadIdx.x] = total;
+    total[threadIdx.x] = all;
     before[threadIdx.x] = mine;
   }
   __syncthreads();
-  for (int32_t d = 1; d < digits; d <<= 1) {
-    const int32_t x = (int32_t)threadIdx.x < digits && (int32_t)threadIdx.x >= d ? scan[threadIdx.x - d] : 0;
-    __syncthreads();
-    if ((int32_t)threadIdx.x < digits) scan[threadIdx.x] += x;
-    __syncthreads();
+  int32_t sum = 0, mine = 0, scan = 0;  // of digit threadIdx.x
+  if ((int32_t)threadIdx.x < digits) {
+    for (int32_t t = threadIdx.x; t < kSortThreads; t += digits) {
+      sum += total[t];
+      mine += before[t];
+    }
   }
+  scan = sum;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t x = __shfl_up(scan, d);
+    scan += lane >= d ? x : 0;
+  }
+  if (lane == 63 && wave < kMaxDigits / 64) wave_total[wave] = scan;
+  __syncthreads();
+  for (int w = 0; w < wave && w < kMaxDigits / 64; ++w) scan += wave_total[w];
+  const int32_t base = scan - sum + mine;  // place of the tile's first token of digit threadIdx.x
   const int32_t per_wave = s.tile / kSortWaves;   // a multiple of 64
   const int32_t begin = blockIdx.x * s.tile + wave * per_wave, end = min(s.n, begin + per_wave);
   for (int32_t i0 = begin; i0 < end; i0 += 64) {
@@ -232,11 +306,11 @@ __global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, 
   }
   __syncthreads();
   if ((int32_t)threadIdx.x < digits) {
-    int32_t sum = (threadIdx.x ? scan[threadIdx.x - 1] : 0) + before[threadIdx.x];
+    int32_t place = base;
     for (int w = 0; w < kSortWaves; ++w) {
       const int32_t c = at[w][threadIdx.x];
-      at[w][threadIdx.x] = sum;
-      sum += c;
+      at[w][threadIdx.x] = place;
+      place += c;
     }
   }
   __syncthreads();
@@ -255,14 +329,14 @@ __global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, 
 }
 
 // ---- sums of the rows ------------------------------------------------------------------------------
-// A wave takes a chunk of 64 ordered tokens and a slab of columns, and adds up runs of equal rows in
+// A wave takes a chunk of up to 64 ordered tokens and a slab of columns, and adds up runs of equal rows in
 // registers.  A run that crosses one chunk boundary is finished by the chunk where it begins.  A run that
 // touches three chunks or more is long: each chunk leaves its piece in `part`, slot 1 the chunk where
 // the run begins and slot 0 the others, and k_join adds the pieces in order.
 struct RowArgs {
   const Entry* order;
   float* part;          // [chunks][2][slabs][kSlab], in lane order
-  int32_t chunks;
+  int32_t chunk, chunks;  // tokens a chunk, a power of two; chunks
   int32_t accumulate;
   int64_t sum_waves;    // waves that sum chunks; the rest, one a row, clear rows without a token
 };
@@ -271,7 +345,7 @@ __device__ __forceinline__ uint32_t row_at(const RowArgs& r, const EmbedArgs& a,
   return i >= 0 && i < a.n ? r.order[i].row : (uint32_t)a.rows;
 }
 
-template <class A, class W, bool VEC>
+template <class A, class W>
 struct RowSum {
   const EmbedArgs& a;
   const RowArgs& r;
@@ -287,19 +361,19 @@ struct RowSum {
     *(Float8*)p = acc;
   }
 
-  // Tokens [from, to) of the 64 whose rows and offsets the lanes hold.  `next` is the row after the last
+  // Tokens [from, to) of the chunk whose rows and offsets the lanes hold.  `next` is the row after the last
   // lane's.  slot >= 0: the range is one piece of a long run.
   __device__ __forceinline__ void take(uint32_t row, int64_t offset, int from, int to, uint32_t next, int slot) {
     for (int k0 = from; k0 < to; k0 += kGroup) {
-      Lane8<A, VEC> x[kGroup];
-      Lane8<W, VEC> old[kGroup];
+      Lane8<A> x[kGroup];
+      Lane8<W> old[kGroup];
       bool ends[kGroup];
       uint32_t mine[kGroup];
 #pragma unroll
       for (int k = 0; k < kGroup; ++k) {
         if (k0 + k < to) {
           mine[k] = lane_value(row, k0 + k);
-          ends[k] = slot < 0 && mine[k] != (k0 + k < 63 ? lane_value(row, k0 + k + 1) : next);
+          ends[k] = slot < 0 && mine[k] != (k0 + k < r.chunk - 1 ? lane_value(row, k0 + k + 1) : next);
           x[k].load(grad + lane_value(offset, k0 + k), col, a.hidden);
           if (r.accumulate && ends[k]) old[k].load(dtable + mine[k] * a.table_stride, col, a.hidden);
         }
@@ -311,7 +385,7 @@ struct RowSum {
           if (ends[k]) {
             Float8 y = a.scale * acc;
             if (r.accumulate) y += old[k].get();
-            Lane8<W, VEC>::store(dtable + mine[k] * a.table_stride, col, a.hidden, y);
+            Lane8<W>::store(dtable + mine[k] * a.table_stride, col, a.hidden, y);
             acc = Float8{};
           }
         }
@@ -324,12 +398,12 @@ struct RowSum {
   }
 
   __device__ __forceinline__ void run() {
-    const int64_t base = (int64_t)chunk * kChunk;
-    const int lane = threadIdx.x % 64;
+    const int C = r.chunk, lane = threadIdx.x % 64;
+    const int64_t base = (int64_t)chunk * C;
     const uint32_t none = (uint32_t)a.rows;
-    const bool in0 = base + lane < a.n, in1 = base + 64 + lane < a.n;
-    const Entry e0 = in0 ? r.order[base + lane] : Entry{none, 0}, e1 = in1 ? r.order[base + 64 + lane] : Entry{none, 0};
-    const uint32_t first = lane_value(e0.row, 0), last = lane_value(e0.row, 63), after = lane_value(e1.row, 0);
+    const bool in0 = lane < C && base + lane < a.n, in1 = lane < C && base + C + lane < a.n;
+    const Entry e0 = in0 ? r.order[base + lane] : Entry{none, 0}, e1 = in1 ? r.order[base + C + lane] : Entry{none, 0};
+    const uint32_t first = lane_value(e0.row, 0), last = lane_value(e0.row, C - 1), after = lane_value(e1.row, 0);
     if (first == none) return;
     const uint32_t before = row_at(r, a, base - 1);
     const int64_t off0 = act_offset(a, e0.token);
@@ -337,7 +411,7 @@ struct RowSum {
     int from = 0;
     if (chunk > 0 && before == first) {  // the first run began earlier
       const int lead = __popcll(__ballot(e0.row == first));
-      const bool short_run = row_at(r, a, base - 65) != first && after != first;
+      const bool short_run = row_at(r, a, base - 1 - C) != first && after != first;
       if (!short_run) take(e0.row, off0, 0, lead, none, 0);
       from = lead;
     }
@@ -347,14 +421,14 @@ struct RowSum {
       take(e0.row, off0, from, valid, after, -1);
       return;
     }
-    const int tail = 64 - __popcll(__ballot(e0.row == last));  // where it begins
-    if (row_at(r, a, base + 128) != last) {
-      take(e0.row, off0, from, 64, after, -1);
+    const int tail = C - __popcll(__ballot(e0.row == last));  // where it begins
+    if (row_at(r, a, base + 2 * C) != last) {
+      take(e0.row, off0, from, C, after, -1);
       const int more = __popcll(__ballot(e1.row == last));
       take(e1.row, act_offset(a, e1.token), 0, more, none, -1);
     } else {
       take(e0.row, off0, from, tail, after, -1);
-      take(e0.row, off0, tail, 64, after, 1);
+      take(e0.row, off0, tail, C, after, 1);
     }
   }
 };
@@ -375,19 +449,19 @@ __device__ __forceinline__ bool has_token(const RowArgs& r, int32_t n, uint32_t 
   return __ballot(at < n && r.order[at < n ? at : 0].row == row) != 0;
 }
 
-template <class A, class W, bool VEC>
+template <class A, class W>
 __global__ __launch_bounds__(kThreads) void k_rows(EmbedArgs a, RowArgs r, const A* __restrict__ grad, W* __restrict__ dtable) {
   const int64_t waves = (int64_t)gridDim.x * kWaves, all = r.sum_waves + (r.accumulate ? 0 : a.rows);
   for (int64_t w = wave_index(); w < all; w += waves) {
     if (w < r.sum_waves) {
       const int32_t chunk = (int32_t)(w / a.slabs), slab = (int32_t)(w % a.slabs);
-      RowSum<A, W, VEC> s{a, r, grad, dtable, chunk, slab, first_col<VEC>(slab)};
+      RowSum<A, W> s{a, r, grad, dtable, chunk, slab, first_col(slab)};
       s.run();
     } else {
       const uint32_t row = (uint32_t)(w - r.sum_waves);
       if (a.n && has_token(r, a.n, row)) continue;
       for (int32_t slab = 0; slab < a.slabs; ++slab)
-        Lane8<W, VEC>::store(dtable + row * a.table_stride, first_col<VEC>(slab), a.hidden, Float8{});
+        Lane8<W>::store(dtable + row * a.table_stride, first_col(slab), a.hidden, Float8{});
     }
   }
 }
@@ -396,70 +470,48 @@ __global__ __launch_bounds__(kThreads) void k_rows(EmbedArgs a, RowArgs r, const
 // order, and the quarters are added in order.
 constexpr int kJoinChunks = 16;
 
-template <class W, bool VEC>
+template <class W>
 __global__ __launch_bounds__(kThreads) void k_join(EmbedArgs a, RowArgs r, W* __restrict__ dtable) {
   __shared__ Float8 quarter[kWaves][64];
   const int32_t slab = (int32_t)(blockIdx.x % a.slabs), wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int32_t first = (int32_t)(blockIdx.x / a.slabs) * kJoinChunks;
-  for (int32_t c = first; c < first + kJoinChunks && c < r.chunks; ++c) {
-    const int64_t base = (int64_t)c * kChunk;
-    const uint32_t row = row_at(r, a, base + 63);
-    if (row == (uint32_t)a.rows || row_at(r, a, base - 1) == row || row_at(r, a, base + 64) != row || row_at(r, a, base + 128) != row)
-      continue;
+  const int32_t first = (int32_t)(blockIdx.x / a.slabs) * kJoinChunks, C = r.chunk;
+  uint64_t begins;  // chunks where a long run begins
+  {
+    const int64_t base = (int64_t)(first + lane) * C;
+    const uint32_t row = lane < kJoinChunks ? row_at(r, a, base + C - 1) : (uint32_t)a.rows;
+    begins = __ballot(row != (uint32_t)a.rows && row_at(r, a, base - 1) != row && row_at(r, a, base + C) == row &&
+                      row_at(r, a, base + 2 * C) == row);
+  }
+  for (; begins; begins &= begins - 1) {
+    const int32_t c = first + __ffsll((unsigned long long)begins) - 1;
+    const uint32_t row = row_at(r, a, (int64_t)c * C + C - 1);
     int32_t end = c + 2;  // the run's chunks are [c, end)
     for (;;) {
-      const uint64_t in = __ballot(row_at(r, a, (int64_t)(end + lane) * kChunk) == row);
+      const uint64_t in = __ballot(row_at(r, a, (int64_t)(end + lane) * C) == row);
       end += in == ~0ull ? 64 : __ffsll((unsigned long long)~in) - 1;
       if (in != ~0ull) break;
     }
     const int32_t pieces = end - c, share = (pieces + kWaves - 1) / kWaves;
     Float8 acc = {};
     const int32_t to = min(pieces, (wave + 1) * share);
-#pragma unroll 4
+#pragma unroll 8
     for (int32_t k = wave * share; k < to; ++k)
       acc += *(const Float8*)(r.part + (((int64_t)(c + k) * 2 + (k == 0)) * a.slabs + slab) * kSlab + lane * kVec);
     quarter[wave][lane] = acc;
     __syncthreads();
     if (wave == 0) {
       for (int w = 1; w < kWaves; ++w) acc += quarter[w][lane];
-      const int64_t col = first_col<VEC>(slab);
+      const int64_t col = first_col(slab);
       W* d = dtable + row * a.table_stride;
       Float8 y = a.scale * acc;
       if (r.accumulate) {
-        Lane8<W, VEC> old;
+        Lane8<W> old;
         old.load(d, col, a.hidden);
         y += old.get();
       }
-      Lane8<W, VEC>::store(d, col, a.hidden, y);
+      Lane8<W>::store(d, col, a.hidden, y);
     }
     __syncthreads();
-  }
-}
-
-// A wave takes a position and a slab, and adds up the batch.
-template <class A, class W, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_dpos(EmbedArgs a, const A* __restrict__ grad, W* __restrict__ dpos,
-                                                   int32_t accumulate) {
-  const int64_t waves = (int64_t)gridDim.x * kWaves, all = a.seq * a.slabs;
-  for (int64_t w = wave_index(); w < all; w += waves) {
-    const int64_t s = w / a.slabs, col = first_col<VEC>((int32_t)(w % a.slabs));
-    Float8 acc = {};
-    for (int64_t b0 = 0; b0 < a.batch; b0 += kAhead) {
-      Lane8<A, VEC> x[kAhead];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (b0 + k < a.batch) x[k].load(grad + (b0 + k) * a.act_batch_stride + s * a.act_stride, col, a.hidden);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (b0 + k < a.batch) acc += x[k].get();
-    }
-    W* d = dpos + s * a.pos_stride;
-    if (accumulate) {
-      Lane8<W, VEC> old;
-      old.load(d, col, a.hidden);
-      acc += old.get();
-    }
-    Lane8<W, VEC>::store(d, col, a.hidden, acc);
   }
 }
 
@@ -498,30 +550,21 @@ EmbedArgs args(const mist_embed_desc* d) {
                    (int32_t)(d->batch * d->seq), (int32_t)((d->hidden + kSlab - 1) / kSlab)};
 }
 
-// Whether every lane's eight values are one aligned piece of 16 bytes (32 in fp32).
-bool vectors(const mist_embed_desc* d, const void* act, const void* table, const void* pos) {
-  return d->hidden % kVec == 0 && (d->batch == 1 || d->act_batch_stride % kVec == 0) && (d->seq == 1 || d->act_stride % kVec == 0) &&
-         (d->rows == 1 || d->table_stride % kVec == 0) && (!pos || d->seq == 1 || d->pos_stride % kVec == 0) && aligned(act, 16) &&
-         aligned(table, 16) && aligned(pos, 16);
-}
-
-template <class F>
-void with_bool(bool b, F&& f) {
-  if (b) f(std::true_type{});
-  else f(std::false_type{});
-}
-
 // Blocks for a number of waves, capped so that a grid stays below 2^32 threads (kernels loop).
-unsigned blocks_of(int64_t waves) { return (unsigned)std::min<int64_t>((waves + kWaves - 1) / kWaves, 1 << 23); }
+unsigned blocks_of(int64_t waves, int per_block) { return (unsigned)std::min<int64_t>((waves + per_block - 1) / per_block, 1 << 21); }
 
 // Places in the workspace.
 struct Scratch {
+  int32_t chunk;
   int64_t chunks;
   size_t order, other, hist, part, bytes;
 };
 Scratch scratch(const EmbedArgs& a) {
   Scratch s{};
-  s.chunks = ((int64_t)a.n + kChunk - 1) / kChunk;
+  // Smaller chunks where there are too few waves to hide the gather's latency.
+  s.chunk = kMaxChunk;
+  while (s.chunk > 8 && ((int64_t)a.n + s.chunk - 1) / s.chunk * a.slabs < 2048) s.chunk /= 2;
+  s.chunks = ((int64_t)a.n + s.chunk - 1) / s.chunk;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -533,15 +576,19 @@ Scratch scratch(const EmbedArgs& a) {
     s.other = take((size_t)a.n * sizeof(Entry));
     s.hist = take((size_t)kMaxTiles * kMaxDigits * 4);
   }
-  s.part = take(a.n > 2 * kChunk ? (size_t)s.chunks * 2 * a.slabs * kSlab * 4 : 0);
+  s.part = take(s.chunks > 2 ? (size_t)s.chunks * 2 * a.slabs * kSlab * 4 : 0);
   s.bytes = at;
   return s;
 }
 
-void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, char* ws, hipStream_t st) {
+template <class A, class W>
+void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs<A, W> pos, char* ws, hipStream_t st) {
   Entry* order = (Entry*)(ws + s.order);
+  const int64_t pos_waves = pos.dpos ? a.seq * a.slabs : 0;
   if (a.n <= kCounted) {
-    hipLaunchKernelGGL(k_place, dim3((unsigned)((a.n + kPlaced - 1) / kPlaced)), dim3(kThreads), 0, st, a, ids, order);
+    pos.end = pos_waves;
+    const dim3 grid((unsigned)((a.n + kPlaced - 1) / kPlaced) + blocks_of(pos_waves, kWaves));
+    if (grid.x) hipLaunchKernelGGL((k_place<A, W>), grid, dim3(kThreads), 0, st, a, pos, ids, order);
     return;
   }
   int bits = 1;  // of the largest key, rows
@@ -555,12 +602,20 @@ void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, char* w
   p.tiles = (int32_t)(((int64_t)a.n + p.tile - 1) / p.tile);
   p.bits = (bits + passes - 1) / passes;
   Entry* buf[2] = {order, (Entry*)(ws + s.other)};
-  for (int k = 0; k < passes; ++k) {
-    p.out = buf[(passes - 1 - k) % 2];  // the last pass ends in `order`
-    p.shift = k * p.bits;
-    hipLaunchKernelGGL(k_digits, dim3(p.tiles), dim3(kSortThreads), 0, st, a, p, ids);
-    hipLaunchKernelGGL(k_move, dim3(p.tiles), dim3(kSortThreads), 0, st, a, p, ids);
-    p.in = p.out;
+  for (int k = 0; k < 2 * passes; ++k) {
+    if (k % 2 == 0) {
+      p.out = buf[(passes - 1 - k / 2) % 2];  // the last pass ends in `order`
+      p.shift = k / 2 * p.bits;
+    }
+    pos.begin = pos_waves * k / (2 * passes);
+    pos.end = pos_waves * (k + 1) / (2 * passes);
+    const dim3 grid(p.tiles + blocks_of(pos.end - pos.begin, kSortWaves));
+    if (k % 2 == 0) {
+      hipLaunchKernelGGL((k_digits<A, W>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+    } else {
+      hipLaunchKernelGGL((k_move<A, W>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+      p.in = p.out;
+    }
   }
 }
 
@@ -586,12 +641,9 @@ mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const 
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
-    with_bool(vectors(d, out, table, pos), [&](auto vec) {
-      with_bool(pos != nullptr, [&](auto with_pos) {
-        hipLaunchKernelGGL((k_embed<A, W, vec.value, with_pos.value>), dim3(blocks_of(waves)), dim3(kThreads), 0, (hipStream_t)stream, a,
-                           (int32_t)per_wave, ids, (const W*)table, (const W*)pos, (A*)out);
-      });
-    });
+    const auto kernel = pos ? k_embed<A, W, true> : k_embed<A, W, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
+                       (int32_t)per_wave, ids, (const W*)table, (const W*)pos, (A*)out);
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "embedding");
@@ -623,21 +675,16 @@ mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const
   if (join_blocks > 1 << 23) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
   const hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  if (a.n) order_tokens(a, ids, s, ws, st);
-  const RowArgs r{(const Entry*)(ws + s.order), (float*)(ws + s.part), (int32_t)s.chunks, accumulate, s.chunks * a.slabs};
+  const RowArgs r{(const Entry*)(ws + s.order), (float*)(ws + s.part), s.chunk, (int32_t)s.chunks, accumulate, s.chunks * a.slabs};
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
-    with_bool(vectors(d, grad, dtable, dpos), [&](auto vec) {
-      const int64_t waves = r.sum_waves + (accumulate ? 0 : a.rows);
-      if (waves)
-        hipLaunchKernelGGL((k_rows<A, W, vec.value>), dim3(blocks_of(waves)), dim3(kThreads), 0, st, a, r, (const A*)grad, (W*)dtable);
-      if (a.n > 2 * kChunk)
-        hipLaunchKernelGGL((k_join<W, vec.value>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
-      if (dpos && d->seq)
-        hipLaunchKernelGGL((k_dpos<A, W, vec.value>), dim3(blocks_of(a.seq * a.slabs)), dim3(kThreads), 0, st, a, (const A*)grad, (W*)dpos,
-                           accumulate);
-    });
+    const PosArgs<A, W> p{(const A*)grad, (W*)dpos, 0, 0, accumulate};
+    order_tokens(a, ids, s, p, ws, st);
+    const int64_t waves = r.sum_waves + (accumulate ? 0 : a.rows);
+    if (waves)
+      hipLaunchKernelGGL((k_rows<A, W>), dim3(blocks_of(waves, kWaves)), dim3(kThreads), 0, st, a, r, (const A*)grad, (W*)dtable);
+    if (s.chunks > 2) hipLaunchKernelGGL((k_join<W>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "embedding gradient");

@@ -1,6 +1,7 @@
 // Lists of tensors, the global gradient norm, clipping and the Adam step.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -73,8 +74,21 @@ __device__ double block_join(double x) {
   return x;
 }
 
+__device__ void finish(const mist_clip_desc& c, mist_step_record* r, double total) {
+  const double scale = fabs((double)c.grad_scale);
+  const double norm = scale * (c.kind == MIST_NORM_L2 ? sqrt(total) : total);
+  const bool fine = norm < HUGE_VAL;  // false for NaN
+  r->norm = (float)norm;
+  r->coef = fine ? (float)(c.grad_scale * (norm > c.max_norm ? c.max_norm / norm : 1.0)) : c.grad_scale;
+  r->applied = fine;
+  r->step += fine;
+  r->skipped += !fine;
+}
+
 // Reads only: pieces in turn, four loads of 16 bytes a thread in flight; the next piece's table entries are
-// read ahead.
+// read ahead.  The blocks' results are joined by a launch of their own: letting the last block to arrive do
+// it in this one takes a release of the XCD's cache from every block, which measured 85 us more on 302
+// million fp32 gradients (224 us) where the launch takes 5.
 template <class G, bool MAX>
 __global__ __launch_bounds__(kThreads) void k_norm(List l, int64_t n_pieces, double* __restrict__ part) {
   constexpr int kV = 16 / sizeof(G), kLoads = 4;
@@ -85,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void k_norm(List l, int64_t n_pieces, dou
     sum = MAX ? join<true>(sum, fabs(x)) : fma(x, x, sum);
   };
   int64_t k = blockIdx.x;
-  Span s = span_of(l, l.piece[k]);
+  Span s = k < n_pieces ? span_of(l, l.piece[k]) : Span{};
   for (; k < n_pieces; k += gridDim.x) {
     const G* g = (const G*)s.ptr + s.begin;
     const int n = (int)(s.end - s.begin), vectors = n / kV;
@@ -108,22 +122,12 @@ __global__ __launch_bounds__(kThreads) void k_norm(List l, int64_t n_pieces, dou
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-__device__ void finish(const mist_clip_desc& c, mist_step_record* r, double total) {
-  const double scale = fabs((double)c.grad_scale);
-  const double norm = scale * (c.kind == MIST_NORM_L2 ? sqrt(total) : total);
-  const bool fine = norm < HUGE_VAL;  // false for NaN
-  r->norm = (float)norm;
-  r->coef = fine ? (float)(c.grad_scale * (norm > c.max_norm ? c.max_norm / norm : 1.0)) : c.grad_scale;
-  r->applied = fine;
-  r->step += fine;
-  r->skipped += !fine;
-}
-
-// One block: joins the partial results in order.
+// One block: joins the results in order.
 template <bool MAX>
 __global__ __launch_bounds__(kTotalThreads) void k_total(const double* __restrict__ part, int32_t n, mist_clip_desc c, int32_t accumulate,
-                                                    int32_t do_finish, mist_step_record* r) {
+                                                         int32_t do_finish, mist_step_record* r) {
   double x = 0.0;
+#pragma unroll 2
   for (int32_t k = threadIdx.x; k < n; k += kTotalThreads) x = join<MAX>(x, part[k]);
   x = block_join<MAX, kTotalThreads>(x);
   if (threadIdx.x) return;
@@ -277,7 +281,7 @@ bool clip_ok(const mist_clip_desc* c) {
 
 bool aligned8(const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; }
 
-int32_t norm_blocks(const mist_tensors* g) { return (int32_t)(g->n_pieces < kNormBlocks ? g->n_pieces : kNormBlocks); }
+int32_t norm_blocks(const mist_tensors* g) { return (int32_t)std::min<int64_t>(g->n_pieces, kNormBlocks); }
 
 }  // namespace
 
@@ -370,20 +374,15 @@ mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32
   if (!aligned8(workspace) || !aligned8(record)) return lib_fail(MIST_E_INVALID, "gradient norm: workspace or record not aligned to 8");
   if (const mist_status st = on_device(g, "gradient norm")) return st;
   const hipStream_t st = (hipStream_t)stream;
+  const bool max = c->kind == MIST_NORM_MAX;
   double* part = (double*)workspace;
-  if (blocks) {
-    mist::with_type(g->type, [&](auto x) {
-      using G = typename decltype(x)::type;
-      if (c->kind == MIST_NORM_MAX)
-        hipLaunchKernelGGL((k_norm<G, true>), dim3(blocks), dim3(kThreads), 0, st, g->list, g->n_pieces, part);
-      else
-        hipLaunchKernelGGL((k_norm<G, false>), dim3(blocks), dim3(kThreads), 0, st, g->list, g->n_pieces, part);
-    });
-  }
-  if (c->kind == MIST_NORM_MAX)
-    hipLaunchKernelGGL(k_total<true>, dim3(1), dim3(kTotalThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
-  else
-    hipLaunchKernelGGL(k_total<false>, dim3(1), dim3(kTotalThreads), 0, st, part, blocks, *c, accumulate, do_finish, record);
+  mist::with_type(g->type, [&](auto x) {
+    using G = typename decltype(x)::type;
+    const auto kernel = max ? k_norm<G, true> : k_norm<G, false>;
+    if (blocks) hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, g->list, g->n_pieces, part);
+  });
+  hipLaunchKernelGGL(max ? k_total<true> : k_total<false>, dim3(1), dim3(kTotalThreads), 0, st, part, blocks, *c, accumulate, do_finish,
+                     record);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "gradient norm");
 }

@@ -652,15 +652,16 @@ class Corun:
 
 # -- operators of a training step's two ends ---------------------------------------------------
 E_INVALID = -1
-_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
 _NORMS = {"l2": 0, "max": 1}
+NORM_WORKSPACE = 16384
+_TYPES = {}  # torch dtype -> element type
 
 
-def _type(t, what: str) -> int:
-    code = _TYPES.get(str(t.dtype))
-    if code is None:
-        raise MistError(E_INVALID, "%s: %s is not float32, bfloat16 or float16" % (what, t.dtype))
-    return code
+def _torch():
+    import torch
+    if not _TYPES:
+        _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return torch
 
 
 def _need(ok: bool, msg: str) -> None:
@@ -668,58 +669,63 @@ def _need(ok: bool, msg: str) -> None:
         raise MistError(E_INVALID, msg)
 
 
-class _On:
-    """The stream of one call: its handle, scratch memory of its pool, and the note to the caching
-    allocator that tensors are used on it when it is not the current one."""
+def _type(t, what: str) -> int:
+    code = _TYPES.get(t.dtype)
+    _need(code is not None, "%s: %s is not float32, bfloat16 or float16" % (what, t.dtype))
+    return code
 
-    def __init__(self, stream, device):
-        import torch
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
-        self.stream, self.device = stream, device
-        self.handle = _stream_handle(stream)
 
-    def scratch(self, nbytes: int):
-        import torch
-        if self.stream is None:
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+def _stream_of(torch, stream, device):
+    """A caller's stream (None, raw handle or torch stream) as (handle, torch stream or None)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index), None
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    return stream.cuda_stream, stream
 
-    def use(self, *tensors) -> None:
-        if self.stream is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+
+def _on_device(torch, device, fn, *args) -> None:
+    """One call of the library with the tensors' device current."""
+    if torch._C._cuda_getDevice() == device.index:
+        _check(_lib, fn(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(_lib, fn(*args))
+
+
+def _used_on(stream, *tensors) -> None:
+    """Tells the caching allocator that the tensors are used on a stream other than the current one."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def _embed_desc(ids, act, table, scale, pos, vocab_begin) -> EmbedDesc:
-    for name, t in (("ids", ids), ("the activations", act), ("the table", table)) + ((("the positions", pos),) if pos is not None else ()):
-        _need(t.device == act.device and t.is_cuda, "embedding: %s must be on the activations' GPU" % name)
-    _need(str(ids.dtype) in ("torch.int32", "torch.int64"), "embedding: ids must be int32 or int64")
-    _need(ids.dim() in (1, 2) and act.dim() == ids.dim() + 1 and act.shape[:-1] == ids.shape,
+    device = act.device
+    _need(act.is_cuda and ids.device == device and table.device == device and (pos is None or pos.device == device),
+          "embedding: ids, table, positions and activations must be on one GPU")
+    id_bytes = ids.element_size()
+    _need(id_bytes in (4, 8) and not ids.dtype.is_floating_point and not ids.dtype.is_complex and ids.dtype.is_signed,
+          "embedding: ids must be int32 or int64")
+    shape, ashape = ids.shape, act.shape
+    dims = len(shape)
+    _need(dims in (1, 2) and len(ashape) == dims + 1 and ashape[:-1] == shape,
           "embedding: ids must be [seq] or [batch, seq], the activations ids' shape and hidden")
-    seq = ids.shape[-1]
-    batch = ids.shape[0] if ids.dim() == 2 else 1
-    hidden = act.shape[-1]
-    _need(table.dim() == 2 and table.shape[1] == hidden, "embedding: the table must be [rows, hidden]")
-    _need(pos is None or (pos.dim() == 2 and pos.shape[1] == hidden and pos.shape[0] >= seq),
-          "embedding: the positions must be [at least seq, hidden]")
-    _need(pos is None or pos.dtype == table.dtype, "embedding: the positions must have the table's type")
-    for t in (act, table) + (() if pos is None else (pos,)):
-        _need(t.stride(-1) == 1 or hidden == 1 or t.numel() == 0, "embedding: the hidden dimension must be contiguous")
-    _need(seq <= 1 or ids.stride(-1) == 1 or batch == 0, "embedding: the ids of a sequence must be contiguous")
-    d = EmbedDesc()
-    d.batch, d.seq, d.hidden, d.rows, d.vocab_begin = batch, seq, hidden, table.shape[0], int(vocab_begin)
-    d.ids_stride = ids.stride(0) if ids.dim() == 2 else 0
-    d.act_batch_stride = act.stride(0) if ids.dim() == 2 else 0
-    d.act_stride = act.stride(-2)
-    d.table_stride = table.stride(0)
-    d.pos_stride = pos.stride(0) if pos is not None else 0
-    d.ids_bytes = ids.element_size()
-    d.act_type, d.table_type = _type(act, "embedding"), _type(table, "embedding")
-    d.scale = float(scale)
-    return d
+    seq, hidden, tshape = shape[-1], ashape[-1], table.shape
+    _need(len(tshape) == 2 and tshape[1] == hidden, "embedding: the table must be [rows, hidden]")
+    ist, ast, tst = ids.stride(), act.stride(), table.stride()
+    _need(hidden == 1 or ((ast[-1] == 1 or act.numel() == 0) and tst[1] == 1), "embedding: the hidden dimension must be contiguous")
+    _need(seq <= 1 or ist[-1] == 1, "embedding: the ids of a sequence must be contiguous")
+    pos_stride = 0
+    if pos is not None:
+        _need(pos.dim() == 2 and pos.shape[1] == hidden and pos.shape[0] >= seq, "embedding: the positions must be [at least seq, hidden]")
+        _need(pos.dtype == table.dtype, "embedding: the positions must have the table's type")
+        pst = pos.stride()
+        _need(hidden == 1 or pst[1] == 1 or pos.numel() == 0, "embedding: the hidden dimension must be contiguous")
+        pos_stride = pst[0]
+    two = dims == 2
+    return EmbedDesc(shape[0] if two else 1, seq, hidden, tshape[0], int(vocab_begin), ist[0] if two else 0, ast[0] if two else 0,
+                     ast[-2], tst[0], pos_stride, id_bytes, _type(act, "embedding"), _type(table, "embedding"), float(scale))
 
 
 def _ptr(t):
@@ -731,18 +737,18 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     outside the shard (padding, other ranks' rows).  ids: [seq] or [batch, seq], int32 or int64 (batch strides
     allowed); table: [rows, hidden]; pos: [at least seq, hidden] or None; out: ids' shape + [hidden], of
     any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
-    import torch
+    torch = _torch()
     L = load()
-    on = _On(stream, table.device)
+    handle, other = _stream_of(torch, stream, table.device)
     if out is None:
         _need(table.dim() == 2, "embedding: the table must be [rows, hidden]")
-        shape = tuple(ids.shape) + (table.shape[1],)
-        with torch.cuda.stream(on.stream):
-            out = torch.empty(shape, dtype=table.dtype, device=table.device)
+        with torch.cuda.stream(other):
+            out = torch.empty(tuple(ids.shape) + (table.shape[1],), dtype=table.dtype, device=table.device)
     d = _embed_desc(ids, out, table, scale, pos, vocab_begin)
-    with torch.cuda.device(table.device):
-        _check(L, L.mist_embed_forward(ctypes.byref(d), _ptr(ids), _ptr(table), _ptr(pos), _ptr(out), on.handle))
-    on.use(ids, table, pos, out)
+    _on_device(torch, out.device, L.mist_embed_forward, ctypes.byref(d), ids.data_ptr(), table.data_ptr(), _ptr(pos),
+               out.data_ptr(), handle)
+    if other is not None:
+        _used_on(other, ids, table, pos, out)
     return out
 
 
@@ -750,17 +756,22 @@ def embed_grad(ids, grad, dtable, *, scale: float = 1.0, dpos=None, vocab_begin:
                stream=None):
     """mist_embed_backward: the gradients of embed's table and positions from grad (ids' shape + [hidden]; it
     may be expanded), written to dtable and dpos (accumulate: added to them)."""
-    import torch
+    torch = _torch()
     L = load()
     d = _embed_desc(ids, grad, dtable, scale, dpos, vocab_begin)
-    on = _On(stream, grad.device)
+    device = grad.device
+    handle, other = _stream_of(torch, stream, device)
     need = ctypes.c_size_t()
-    with torch.cuda.device(grad.device):
-        _check(L, L.mist_embed_workspace(ctypes.byref(d), ctypes.byref(need)))
-        ws = on.scratch(need.value)
-        _check(L, L.mist_embed_backward(ctypes.byref(d), _ptr(ids), _ptr(grad), _ptr(dtable), _ptr(dpos),
-                                        1 if accumulate else 0, _ptr(ws), need.value, on.handle))
-    on.use(ids, grad, dtable, dpos)
+    _check(L, L.mist_embed_workspace(ctypes.byref(d), ctypes.byref(need)))
+    if other is None:
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(other):  # of that stream's pool
+            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    _on_device(torch, device, L.mist_embed_backward, ctypes.byref(d), ids.data_ptr(), grad.data_ptr(), dtable.data_ptr(), _ptr(dpos),
+               1 if accumulate else 0, ws.data_ptr(), need.value, handle)
+    if other is not None:
+        _used_on(other, ids, grad, dtable, dpos)
     return dtable
 
 
@@ -769,33 +780,30 @@ class TensorList:
     must be contiguous and stay where they are; the list keeps them alive."""
 
     def __init__(self, tensors, allocator: str | None = "torch"):
-        import torch
         self.h = None
+        torch = _torch()
         self.L = load()
         self.tensors = list(tensors)
         _need(len(self.tensors) > 0, "tensor list: no tensors")
+        _need(allocator in ("torch", None), "allocator must be 'torch' or None")
         t0 = self.tensors[0]
         self.dtype, self.device = t0.dtype, t0.device
         for t in self.tensors:
             _need(t.is_cuda and t.device == self.device and t.dtype == self.dtype,
                   "tensor list: the tensors must be of one type on one GPU")
             _need(t.is_contiguous(), "tensor list: the tensors must be contiguous")
+        code = _type(t0, "tensor list")
         n = len(self.tensors)
         ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
-        _need(allocator in ("torch", None), "allocator must be 'torch' or None")
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             self._alloc = None
             if allocator == "torch":
                 self._alloc, self._cb = _torch_allocator([])
-            _check(self.L, self.L.mist_tensors_create(ptrs, sizes, n, _type(t0, "tensor list"),
-                                                      ctypes.byref(self._alloc) if self._alloc else None,
+            _check(self.L, self.L.mist_tensors_create(ptrs, sizes, n, code, ctypes.byref(self._alloc) if self._alloc else None,
                                                       ctypes.byref(h)))
-            self.h = h
-            need = ctypes.c_size_t()
-            _check(self.L, self.L.mist_norm_workspace(self.h, ctypes.byref(need)))
-        self._norm_bytes = need.value
+        self.h = h
 
     def __len__(self) -> int:
         return len(self.tensors)
@@ -819,11 +827,14 @@ class TensorList:
 
 
 class StepRecord:
-    """A mist_step_record on the GPU; the fields are 0-dimensional tensors that share its memory."""
+    """A mist_step_record on the GPU, with the norm's scratch memory behind it; the fields are 0-dimensional tensors
+    that share its memory.  One stream at a time."""
 
     def __init__(self, step: int = 0, device=None):
-        import torch
-        self.data = torch.zeros(4, dtype=torch.float64, device="cuda" if device is None else device)
+        torch = _torch()
+        self.data = torch.zeros(8 + NORM_WORKSPACE // 8, dtype=torch.float64, device="cuda" if device is None else device)
+        self.device = self.data.device
+        self.ptr = self.data.data_ptr()
         self.total = self.data[0]
         self.step = self.data.view(torch.int64)[1]
         f, i = self.data.view(torch.float32), self.data.view(torch.int32)
@@ -835,67 +846,64 @@ class StepRecord:
 
 def _clip_desc(kind, grad_scale, max_norm) -> ClipDesc:
     _need(kind in _NORMS, "gradient norm: kind must be 'l2' or 'max'")
-    return ClipDesc(_NORMS[kind], float(grad_scale), float(max_norm))
+    return ClipDesc(_NORMS[kind], grad_scale, max_norm)
 
 
-def _handles(*lists):
+def _lists_on(record, *lists) -> None:
     for x in lists:
-        _need(x is None or x.h is not None, "tensor list: closed")
-    return [None if x is None else x.h for x in lists]
+        _need(x.h is not None, "tensor list: closed")
+        _need(x.device == record.device, "tensor list: on another device than the step record")
 
 
-def grad_norm(grads, record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
+def grad_norm(grads: TensorList, record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
               accumulate: bool = False, finish: bool = True, stream=None) -> StepRecord:
-    """mist_grad_norm over a TensorList: record.total, and with finish the norm, the clip factor and the count of
+    """mist_grad_norm over a list: record.total, and with finish the norm, the clip factor and the count of
     the step.  Nothing is waited for.  accumulate joins record.total (a step with several lists)."""
-    import torch
+    torch = _torch()
     c = _clip_desc(kind, grad_scale, max_norm)
-    (h,) = _handles(grads)
-    _need(record.data.device == grads.device, "step record: on another device than the gradients")
-    on = _On(stream, grads.device)
-    with torch.cuda.device(grads.device):
-        ws = on.scratch(grads._norm_bytes)
-        _check(grads.L, grads.L.mist_grad_norm(h, ctypes.byref(c), 1 if accumulate else 0, 1 if finish else 0,
-                                               record.data.data_ptr(), _ptr(ws), grads._norm_bytes, on.handle))
-    on.use(record.data)
+    _lists_on(record, grads)
+    handle, other = _stream_of(torch, stream, record.device)
+    _on_device(torch, record.device, grads.L.mist_grad_norm, grads.h, ctypes.byref(c), 1 if accumulate else 0, 1 if finish else 0,
+               record.ptr, record.ptr + 64, NORM_WORKSPACE, handle)
+    if other is not None:
+        _used_on(other, record.data, *grads.tensors)
     return record
 
 
 def grad_finish(record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
                 stream=None) -> StepRecord:
     """mist_grad_finish: forms the norm and the clip factor from record.total, e.g. after an all-reduce of it."""
-    import torch
+    torch = _torch()
     L = load()
     c = _clip_desc(kind, grad_scale, max_norm)
-    on = _On(stream, record.data.device)
-    with torch.cuda.device(record.data.device):
-        _check(L, L.mist_grad_finish(ctypes.byref(c), record.data.data_ptr(), on.handle))
-    on.use(record.data)
+    handle, other = _stream_of(torch, stream, record.device)
+    _on_device(torch, record.device, L.mist_grad_finish, ctypes.byref(c), record.ptr, handle)
+    if other is not None:
+        _used_on(other, record.data)
     return record
 
 
 def grad_clip(grads: TensorList, record: StepRecord, out: TensorList | None = None, *, stream=None) -> None:
     """mist_grad_clip: out = record.coef * grads (out None: in place)."""
-    import torch
+    torch = _torch()
     out = grads if out is None else out
-    g, o = _handles(grads, out)
-    _need(record.data.device == grads.device, "step record: on another device than the gradients")
-    on = _On(stream, grads.device)
-    with torch.cuda.device(grads.device):
-        _check(grads.L, grads.L.mist_grad_clip(g, record.data.data_ptr(), o, on.handle))
-    on.use(record.data, *grads.tensors, *out.tensors)
+    _lists_on(record, grads, out)
+    handle, other = _stream_of(torch, stream, record.device)
+    _on_device(torch, record.device, grads.L.mist_grad_clip, grads.h, record.ptr, out.h, handle)
+    if other is not None:
+        _used_on(other, record.data, *grads.tensors, *out.tensors)
 
 
 def adam_step(master: TensorList, m: TensorList, v: TensorList, grads: TensorList, record: StepRecord, *, lr: float,
               betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, weights: TensorList | None = None,
               stream=None) -> None:
     """mist_adam_step with record's clip factor and step count; weights receives the rounded master weights."""
-    import torch
-    hp, hm, hv, hg, hw = _handles(master, m, v, grads, weights)
-    _need(record.data.device == grads.device, "step record: on another device than the gradients")
-    a = AdamDesc(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay))
-    on = _On(stream, grads.device)
-    with torch.cuda.device(grads.device):
-        _check(grads.L, grads.L.mist_adam_step(hp, hm, hv, hg, hw, record.data.data_ptr(), ctypes.byref(a), on.handle))
-    if stream is not None:
-        on.use(record.data, *(t for x in (master, m, v, grads, weights) if x is not None for t in x.tensors))
+    torch = _torch()
+    lists = (master, m, v, grads) if weights is None else (master, m, v, grads, weights)
+    _lists_on(record, *lists)
+    a = AdamDesc(lr, betas[0], betas[1], eps, weight_decay)
+    handle, other = _stream_of(torch, stream, record.device)
+    _on_device(torch, record.device, grads.L.mist_adam_step, master.h, m.h, v.h, grads.h, None if weights is None else weights.h,
+               record.ptr, ctypes.byref(a), handle)
+    if other is not None:
+        _used_on(other, record.data, *(t for x in lists for t in x.tensors))
