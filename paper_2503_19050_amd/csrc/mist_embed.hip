@@ -20,6 +20,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kVec = 8;             // values of a lane
 constexpr int kSlab = 64 * kVec;    // columns of a wave
+constexpr int kJoinRuns = 128;      // long runs joined at a time
+constexpr int64_t kCache = (int64_t)256 << 20;  // the memory-side cache
 constexpr int64_t kMostTokens = (int64_t)1 << 30;  // places past the last token stay below 2^31
 constexpr int kMaxChunk = 64;       // ordered tokens of a wave, one a lane, at most
 
@@ -39,30 +41,45 @@ struct Entry {
 
 typedef Vec<float, kVec>::type Float8;
 
-__device__ __forceinline__ int64_t first_col(int32_t slab) { return (int64_t)slab * kSlab + threadIdx.x % 64 * kVec; }
+// A lane's eight columns of a slab.  VEC (hidden a multiple of 8): consecutive, one access of 16 bytes for
+// 16-bit values; otherwise 64 apart.  Columns past the row are read as the row's last ones, so that loads
+// need no branch, and not written.
+template <bool VEC>
+struct Cols {
+  int32_t first, hidden;
+  __device__ __forceinline__ Cols(int32_t slab, int64_t h)
+      : first(slab * kSlab + (int32_t)(threadIdx.x % 64) * (VEC ? kVec : 1)), hidden((int32_t)h) {}
+  __device__ __forceinline__ int32_t at(int k) const { return VEC ? min(first, hidden - kVec) : min(first + 64 * k, hidden - 1); }
+  __device__ __forceinline__ bool in(int k) const { return VEC ? first < hidden : first + 64 * k < hidden; }
+};
 
-// Eight consecutive values of one lane; the last lane of a row may have fewer.
-template <class T>
+// ONCE: not wanted again soon, so that it does not displace what is (rows of the table, the
+// gradient between its two uses).
+template <class T, bool VEC>
 struct Lane8 {
   typedef typename Vec<T, kVec>::type type;
   type v;
-  __device__ __forceinline__ void load(const T* row, int64_t col, int64_t hidden) {
-    if (col + kVec <= hidden) {
-      v = *(const type*)(row + col);
+  template <bool ONCE = false>
+  __device__ __forceinline__ void load(const T* row, const Cols<VEC>& c) {
+    if (VEC) {
+      v = ONCE ? __builtin_nontemporal_load((const type*)(row + c.at(0))) : *(const type*)(row + c.at(0));
     } else {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = col + k < hidden ? row[col + k] : (T)0.0f;
+      for (int k = 0; k < kVec; ++k) v[k] = row[c.at(k)];
     }
   }
   __device__ __forceinline__ Float8 get() const { return __builtin_convertvector(v, Float8); }
-  static __device__ __forceinline__ void store(T* row, int64_t col, int64_t hidden, Float8 x) {
+  template <bool ONCE = false>
+  static __device__ __forceinline__ void store(T* row, const Cols<VEC>& c, Float8 x) {
     const type y = __builtin_convertvector(x, type);
-    if (col + kVec <= hidden) {
-      *(type*)(row + col) = y;
+    if (VEC) {
+      if (!c.in(0)) return;
+      if (ONCE) __builtin_nontemporal_store(y, (type*)(row + c.at(0)));
+      else *(type*)(row + c.at(0)) = y;
     } else {
 #pragma unroll
       for (int k = 0; k < kVec; ++k)
-        if (col + k < hidden) row[col + k] = y[k];
+        if (c.in(k)) row[c.at(k)] = y[k];
     }
   }
 };
@@ -80,8 +97,7 @@ __device__ __forceinline__ int32_t wave_index() {
 
 // Row of the shard that token (b, s) finds; args.rows if none.
 __device__ __forceinline__ uint32_t token_row(const EmbedArgs& a, const void* ids, uint32_t token) {
-  const uint32_t b = token / (uint32_t)a.seq, s = token % (uint32_t)a.seq;
-  const int64_t at = b * a.ids_stride + s;
+  const int64_t at = a.ids_stride == a.seq ? token : token / (uint32_t)a.seq * a.ids_stride + token % (uint32_t)a.seq;
   const int64_t id = a.ids_bytes == 4 ? (int64_t)((const int32_t*)ids)[at] : ((const int64_t*)ids)[at];
   return id >= a.begin && id - a.begin < a.rows ? (uint32_t)(id - a.begin) : (uint32_t)a.rows;
 }
@@ -91,12 +107,12 @@ __device__ __forceinline__ int64_t act_offset(const EmbedArgs& a, uint32_t token
 }
 
 // ---- lookup ----------------------------------------------------------------------------------------
-// A wave takes `per_wave` (at most 64) tokens and one slab of columns, kAhead rows in flight.  With
-// positions the tokens are taken position by position, so that the batch shares a position's row in
-// the cache.
+// A wave takes `per_wave` (at most kAhead) tokens and one slab of columns, all rows in flight.  With
+// positions the tokens are taken position by position, so that a wave reads a position's row once for
+// its part of the batch.
 constexpr int kAhead = 8;
 
-template <class A, class W, bool POS>
+template <class A, class W, bool VEC, bool POS>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wave, const void* __restrict__ ids,
                                                     const W* __restrict__ table, const W* __restrict__ pos, A* __restrict__ out) {
   const int64_t wave = wave_index();
@@ -111,33 +127,38 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
   const int64_t row_at = row < a.rows ? row * a.table_stride : -1;
   const int64_t out_at = act_offset(a, token);
   const uint32_t s = token % (uint32_t)a.seq;
-  const int64_t col = first_col(slab);
-  for (int k0 = 0; k0 < count; k0 += kAhead) {
-    Lane8<W> x[kAhead], p[kAhead];
+  const Cols<VEC> col(slab, a.hidden);
+  Lane8<W, VEC> x[kAhead], p[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (k0 + k < count) {
-        const int64_t at = lane_value(row_at, k0 + k);
-        if (at >= 0) x[k].load(table + at, col, a.hidden);
-        else x[k].v = {};
-        if (POS) p[k].load(pos + lane_value(s, k0 + k) * a.pos_stride, col, a.hidden);
-      }
+  for (int k = 0; k < kAhead; ++k) {
+    if (k < count) {
+      const int64_t at = lane_value(row_at, k);
+      if (at >= 0) x[k].load(table + at, col);
+      else x[k].v = {};
+      if (POS && (k == 0 || lane_value(s, k) != lane_value(s, k - 1))) p[k].load(pos + lane_value(s, k) * a.pos_stride, col);
     }
+  }
+  Float8 at_s = {};
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (k0 + k < count) {
-        Float8 y = a.scale * x[k].get();
-        if (POS) y += p[k].get();
-        Lane8<A>::store(out + lane_value(out_at, k0 + k), col, a.hidden, y);
+  for (int k = 0; k < kAhead; ++k) {
+    if (k < count) {
+      Float8 y = a.scale * x[k].get();
+      if (POS) {
+        if (k == 0 || lane_value(s, k) != lane_value(s, k - 1)) at_s = p[k].get();
+        y += at_s;
       }
+      Lane8<A, VEC>::template store<true>(out + lane_value(out_at, k), col, y);
     }
   }
 }
 
 // ---- sums of the positions -------------------------------------------------------------------------
-// A wave takes a position and a slab, and adds up the batch.  The work is spread over the launches
-// that order the tokens, which leave most of the device idle: `block` of `blocks` more blocks takes the
-// waves' worth [begin, end) of the call.
+// A wave takes a position and a slab, and adds up the batch.  The work is spread over the launches that order
+// the tokens, which leave most of the device idle: `block` of `blocks` more blocks takes the items [begin, end).
+// The reads reach 4.2 TB/s (32 x 2048 tokens of 2560 columns, 16 bits); more loads at once, several
+// positions a wave, or several waves a position measured the same or worse.
+constexpr int kPosAhead = 8;
+
 template <class A, class W>
 struct PosArgs {
   const A* grad;
@@ -146,65 +167,68 @@ struct PosArgs {
   int32_t accumulate;
 };
 
-template <class A, class W>
+template <bool VEC, class A, class W>
 __device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32_t block, uint32_t blocks) {
   const int32_t waves = blockDim.x / 64;
-  int64_t w = p.begin + __builtin_amdgcn_readfirstlane((int32_t)(block * waves + threadIdx.x / 64));
-  for (; w < p.end; w += (int64_t)blocks * waves) {
-    const int64_t s = w / a.slabs, col = first_col((int32_t)(w % a.slabs));
+  int64_t item = p.begin + __builtin_amdgcn_readfirstlane((int32_t)(block * waves + threadIdx.x / 64));
+  for (; item < p.end; item += (int64_t)blocks * waves) {
+    const int64_t s = item / a.slabs;
+    const Cols<VEC> col((int32_t)(item % a.slabs), a.hidden);
     Float8 acc = {};
-    for (int64_t b0 = 0; b0 < a.batch; b0 += kAhead) {
-      Lane8<A> x[kAhead];
+    for (int64_t b0 = 0; b0 < a.batch; b0 += kPosAhead) {
+      Lane8<A, VEC> x[kPosAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (b0 + k < a.batch) x[k].load(p.grad + (b0 + k) * a.act_batch_stride + s * a.act_stride, col, a.hidden);
+      for (int k = 0; k < kPosAhead; ++k)
+        if (b0 + k < a.batch) x[k].load(p.grad + (b0 + k) * a.act_batch_stride + s * a.act_stride, col);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
+      for (int k = 0; k < kPosAhead; ++k)
         if (b0 + k < a.batch) acc += x[k].get();
     }
     W* d = p.dpos + s * a.pos_stride;
     if (p.accumulate) {
-      Lane8<W> old;
-      old.load(d, col, a.hidden);
+      Lane8<W, VEC> old;
+      old.load(d, col);
       acc += old.get();
     }
-    Lane8<W>::store(d, col, a.hidden, acc);
+    Lane8<W, VEC>::store(d, col, acc);
   }
 }
 
 // ---- order of the tokens ---------------------------------------------------------------------------
 // Short inputs: a token's place is the number of tokens before it by (row, token), counted directly;
-// one launch.  A block places 16 tokens against all of them, 16 lanes a token.
+// one launch.  A block's 16 waves place a token each against all of them.
 constexpr int32_t kCounted = 8192;   // tokens up to which places are counted
-constexpr int kPlaced = 16;
+constexpr int kPlaceThreads = 1024, kPlaced = kPlaceThreads / 64;
 
-template <class A, class W>
-__global__ __launch_bounds__(kThreads) void k_place(EmbedArgs a, PosArgs<A, W> pos, const void* __restrict__ ids, Entry* __restrict__ out) {
+template <class A, class W, bool VEC>
+__global__ __launch_bounds__(kPlaceThreads) void k_place(EmbedArgs a, PosArgs<A, W> pos, const void* __restrict__ ids, Entry* __restrict__ out,
+                                                         int32_t* __restrict__ longs) {
   const int32_t blocks = (a.n + kPlaced - 1) / kPlaced;
   if ((int32_t)blockIdx.x >= blocks) {
-    sum_positions(a, pos, blockIdx.x - blocks, gridDim.x - blocks);
+    sum_positions<VEC>(a, pos, blockIdx.x - blocks, gridDim.x - blocks);
     return;
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *longs = 0;
   __shared__ uint4 rows[kCounted / 4];
   uint32_t* row = (uint32_t*)rows;
-  const int32_t steps = (a.n + 63) / 64;   // of 16 lanes by 4 tokens
+  const int32_t steps = (a.n + 255) / 256;   // of 64 lanes by 4 tokens
 #pragma unroll 4
-  for (int32_t i = threadIdx.x; i < steps * 64; i += kThreads) row[i] = i < a.n ? token_row(a, ids, i) : UINT32_MAX;
+  for (int32_t i = threadIdx.x; i < steps * 256; i += kPlaceThreads) row[i] = i < a.n ? token_row(a, ids, i) : UINT32_MAX;
   __syncthreads();
-  const int32_t i = blockIdx.x * kPlaced + threadIdx.x / 16;
+  const int32_t i = blockIdx.x * kPlaced + threadIdx.x / 64, lane = threadIdx.x % 64;
   const uint32_t mine = row[i < a.n ? i : 0];
   int32_t place = 0;
 #pragma unroll 4
   for (int32_t t = 0; t < steps; ++t) {
-    const int32_t q = t * 16 + threadIdx.x % 16, j = q * 4;
+    const int32_t q = t * 64 + lane, j = q * 4;
     const uint4 r = rows[q];
     place += r.x < mine + (j < i);       // rows are below 2^31: r < mine, or equal and before
     place += r.y < mine + (j + 1 < i);
     place += r.z < mine + (j + 2 < i);
     place += r.w < mine + (j + 3 < i);
   }
-  for (int d = 8; d; d >>= 1) place += __shfl_xor(place, d);
-  if (threadIdx.x % 16 == 0 && i < a.n) out[place] = Entry{mine, (uint32_t)i};
+  for (int d = 32; d; d >>= 1) place += __shfl_xor(place, d);
+  if (lane == 0 && i < a.n) out[place] = Entry{mine, (uint32_t)i};
 }
 
 // Long inputs: radix order, least significant digit first, each pass stable.  A pass counts the digits
@@ -219,6 +243,7 @@ struct SortArgs {
   const Entry* in;    // nullptr: the tokens themselves
   Entry* out;
   int32_t* hist;      // [tiles][digits]
+  int32_t* longs;     // cleared
   int32_t n, tile, tiles, shift, bits;
 };
 
@@ -226,12 +251,13 @@ __device__ __forceinline__ Entry sort_entry(const EmbedArgs& a, const SortArgs& 
   return s.in ? s.in[i] : Entry{token_row(a, ids, i), (uint32_t)i};
 }
 
-template <class A, class W>
+template <class A, class W, bool VEC>
 __global__ __launch_bounds__(kSortThreads) void k_digits(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
   if ((int32_t)blockIdx.x >= s.tiles) {
-    sum_positions(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    sum_positions<VEC>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     return;
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *s.longs = 0;
   __shared__ int32_t count[kMaxDigits];
   const int32_t digits = 1 << s.bits;
   for (int32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
@@ -253,10 +279,10 @@ __device__ __forceinline__ uint64_t equals(uint32_t digit, int bits, bool live) 
   return m;
 }
 
-template <class A, class W>
+template <class A, class W, bool VEC>
 __global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
   if ((int32_t)blockIdx.x >= s.tiles) {
-    sum_positions(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    sum_positions<VEC>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     return;
   }
   __shared__ int32_t at[kSortWaves][kMaxDigits];  // counts, then places
@@ -335,6 +361,7 @@ __global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, 
 // the run begins and slot 0 the others, and k_join adds the pieces in order.
 struct RowArgs {
   const Entry* order;
+  int32_t* longs;       // count of long runs, then the chunks where they begin, in any order
   float* part;          // [chunks][2][slabs][kSlab], in lane order
   int32_t chunk, chunks;  // tokens a chunk, a power of two; chunks
   int32_t accumulate;
@@ -345,14 +372,14 @@ __device__ __forceinline__ uint32_t row_at(const RowArgs& r, const EmbedArgs& a,
   return i >= 0 && i < a.n ? r.order[i].row : (uint32_t)a.rows;
 }
 
-template <class A, class W>
+template <class A, class W, bool VEC, bool ONCE>
 struct RowSum {
   const EmbedArgs& a;
   const RowArgs& r;
   const A* grad;
   W* dtable;
   int32_t chunk, slab;
-  int64_t col;
+  Cols<VEC> col;
   Float8 acc = {};
   static constexpr int kGroup = sizeof(A) == 2 ? 8 : 4;
 
@@ -365,8 +392,8 @@ struct RowSum {
   // lane's.  slot >= 0: the range is one piece of a long run.
   __device__ __forceinline__ void take(uint32_t row, int64_t offset, int from, int to, uint32_t next, int slot) {
     for (int k0 = from; k0 < to; k0 += kGroup) {
-      Lane8<A> x[kGroup];
-      Lane8<W> old[kGroup];
+      Lane8<A, VEC> x[kGroup];
+      Lane8<W, VEC> old[kGroup];
       bool ends[kGroup];
       uint32_t mine[kGroup];
 #pragma unroll
@@ -374,8 +401,8 @@ struct RowSum {
         if (k0 + k < to) {
           mine[k] = lane_value(row, k0 + k);
           ends[k] = slot < 0 && mine[k] != (k0 + k < r.chunk - 1 ? lane_value(row, k0 + k + 1) : next);
-          x[k].load(grad + lane_value(offset, k0 + k), col, a.hidden);
-          if (r.accumulate && ends[k]) old[k].load(dtable + mine[k] * a.table_stride, col, a.hidden);
+          x[k].template load<ONCE>(grad + lane_value(offset, k0 + k), col);
+          if (r.accumulate && ends[k]) old[k].load(dtable + mine[k] * a.table_stride, col);
         }
       }
 #pragma unroll
@@ -384,8 +411,9 @@ struct RowSum {
           acc += x[k].get();
           if (ends[k]) {
             Float8 y = a.scale * acc;
-            if (r.accumulate) y += old[k].get();
-            Lane8<W>::store(dtable + mine[k] * a.table_stride, col, a.hidden, y);
+            W* d = dtable + mine[k] * a.table_stride;
+            if (r.accumulate) Lane8<W, VEC>::store(d, col, y + old[k].get());
+            else Lane8<W, VEC>::template store<true>(d, col, y);
             acc = Float8{};
           }
         }
@@ -429,6 +457,7 @@ struct RowSum {
     } else {
       take(e0.row, off0, from, tail, after, -1);
       take(e0.row, off0, tail, C, after, 1);
+      if (slab == 0 && lane == 0) r.longs[1 + atomicAdd(r.longs, 1)] = chunk;
     }
   }
 };
@@ -449,67 +478,57 @@ __device__ __forceinline__ bool has_token(const RowArgs& r, int32_t n, uint32_t 
   return __ballot(at < n && r.order[at < n ? at : 0].row == row) != 0;
 }
 
-template <class A, class W>
+template <class A, class W, bool VEC, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_rows(EmbedArgs a, RowArgs r, const A* __restrict__ grad, W* __restrict__ dtable) {
   const int64_t waves = (int64_t)gridDim.x * kWaves, all = r.sum_waves + (r.accumulate ? 0 : a.rows);
   for (int64_t w = wave_index(); w < all; w += waves) {
     if (w < r.sum_waves) {
       const int32_t chunk = (int32_t)(w / a.slabs), slab = (int32_t)(w % a.slabs);
-      RowSum<A, W> s{a, r, grad, dtable, chunk, slab, first_col(slab)};
+      RowSum<A, W, VEC, ONCE> s{a, r, grad, dtable, chunk, slab, Cols<VEC>(slab, a.hidden)};
       s.run();
     } else {
       const uint32_t row = (uint32_t)(w - r.sum_waves);
       if (a.n && has_token(r, a.n, row)) continue;
       for (int32_t slab = 0; slab < a.slabs; ++slab)
-        Lane8<W>::store(dtable + row * a.table_stride, first_col(slab), a.hidden, Float8{});
+        Lane8<W, VEC>::template store<true>(dtable + row * a.table_stride, Cols<VEC>(slab, a.hidden), Float8{});
     }
   }
 }
 
-// Long runs that begin in the block's chunks: the waves add up a quarter of the pieces each, in
-// order, and the quarters are added in order.
-constexpr int kJoinChunks = 16;
-
-template <class W>
+// Long runs: a block takes a run and a slab, its waves add up a share of the pieces each, in order, and the
+// shares are added in order.
+template <class W, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_join(EmbedArgs a, RowArgs r, W* __restrict__ dtable) {
-  __shared__ Float8 quarter[kWaves][64];
-  const int32_t slab = (int32_t)(blockIdx.x % a.slabs), wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int32_t first = (int32_t)(blockIdx.x / a.slabs) * kJoinChunks, C = r.chunk;
-  uint64_t begins;  // chunks where a long run begins
-  {
-    const int64_t base = (int64_t)(first + lane) * C;
-    const uint32_t row = lane < kJoinChunks ? row_at(r, a, base + C - 1) : (uint32_t)a.rows;
-    begins = __ballot(row != (uint32_t)a.rows && row_at(r, a, base - 1) != row && row_at(r, a, base + C) == row &&
-                      row_at(r, a, base + 2 * C) == row);
-  }
-  for (; begins; begins &= begins - 1) {
-    const int32_t c = first + __ffsll((unsigned long long)begins) - 1;
-    const uint32_t row = row_at(r, a, (int64_t)c * C + C - 1);
+  __shared__ Float8 shares[kWaves][64];
+  const int32_t slab = (int32_t)(blockIdx.x % a.slabs), wave = threadIdx.x / 64, lane = threadIdx.x % 64, C = r.chunk;
+  const Cols<VEC> col(slab, a.hidden);
+  const int32_t runs = r.longs[0];
+  for (int32_t i = (int32_t)(blockIdx.x / a.slabs); i < runs; i += (int32_t)(gridDim.x / a.slabs)) {
+    const int32_t c = r.longs[1 + i];
+    const uint32_t row = r.order[(int64_t)c * C + C - 1].row;
     int32_t end = c + 2;  // the run's chunks are [c, end)
     for (;;) {
       const uint64_t in = __ballot(row_at(r, a, (int64_t)(end + lane) * C) == row);
       end += in == ~0ull ? 64 : __ffsll((unsigned long long)~in) - 1;
       if (in != ~0ull) break;
     }
-    const int32_t pieces = end - c, share = (pieces + kWaves - 1) / kWaves;
+    const int32_t pieces = end - c, share = (pieces + kWaves - 1) / kWaves, to = min(pieces, (wave + 1) * share);
     Float8 acc = {};
-    const int32_t to = min(pieces, (wave + 1) * share);
 #pragma unroll 8
     for (int32_t k = wave * share; k < to; ++k)
       acc += *(const Float8*)(r.part + (((int64_t)(c + k) * 2 + (k == 0)) * a.slabs + slab) * kSlab + lane * kVec);
-    quarter[wave][lane] = acc;
+    shares[wave][lane] = acc;
     __syncthreads();
     if (wave == 0) {
-      for (int w = 1; w < kWaves; ++w) acc += quarter[w][lane];
-      const int64_t col = first_col(slab);
+      for (int w = 1; w < kWaves; ++w) acc += shares[w][lane];
       W* d = dtable + row * a.table_stride;
       Float8 y = a.scale * acc;
       if (r.accumulate) {
-        Lane8<W> old;
-        old.load(d, col, a.hidden);
+        Lane8<W, VEC> old;
+        old.load(d, col);
         y += old.get();
       }
-      Lane8<W>::store(d, col, a.hidden, y);
+      Lane8<W, VEC>::store(d, col, y);
     }
     __syncthreads();
   }
@@ -550,6 +569,12 @@ EmbedArgs args(const mist_embed_desc* d) {
                    (int32_t)(d->batch * d->seq), (int32_t)((d->hidden + kSlab - 1) / kSlab)};
 }
 
+template <class F>
+void with_bool(bool b, F&& f) {
+  if (b) f(std::true_type{});
+  else f(std::false_type{});
+}
+
 // Blocks for a number of waves, capped so that a grid stays below 2^32 threads (kernels loop).
 unsigned blocks_of(int64_t waves, int per_block) { return (unsigned)std::min<int64_t>((waves + per_block - 1) / per_block, 1 << 21); }
 
@@ -557,7 +582,7 @@ unsigned blocks_of(int64_t waves, int per_block) { return (unsigned)std::min<int
 struct Scratch {
   int32_t chunk;
   int64_t chunks;
-  size_t order, other, hist, part, bytes;
+  size_t order, other, hist, longs, part, bytes;
 };
 Scratch scratch(const EmbedArgs& a) {
   Scratch s{};
@@ -576,19 +601,20 @@ Scratch scratch(const EmbedArgs& a) {
     s.other = take((size_t)a.n * sizeof(Entry));
     s.hist = take((size_t)kMaxTiles * kMaxDigits * 4);
   }
+  s.longs = take((size_t)(s.chunks / 2 + 2) * 4);
   s.part = take(s.chunks > 2 ? (size_t)s.chunks * 2 * a.slabs * kSlab * 4 : 0);
   s.bytes = at;
   return s;
 }
 
-template <class A, class W>
+template <bool VEC, class A, class W>
 void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs<A, W> pos, char* ws, hipStream_t st) {
   Entry* order = (Entry*)(ws + s.order);
-  const int64_t pos_waves = pos.dpos ? a.seq * a.slabs : 0;
+  const int64_t items = pos.dpos ? a.seq * a.slabs : 0;  // of the positions
   if (a.n <= kCounted) {
-    pos.end = pos_waves;
-    const dim3 grid((unsigned)((a.n + kPlaced - 1) / kPlaced) + blocks_of(pos_waves, kWaves));
-    if (grid.x) hipLaunchKernelGGL((k_place<A, W>), grid, dim3(kThreads), 0, st, a, pos, ids, order);
+    pos.end = items;
+    const dim3 grid((unsigned)((a.n + kPlaced - 1) / kPlaced) + blocks_of(items, kPlaced));
+    if (grid.x) hipLaunchKernelGGL((k_place<A, W, VEC>), grid, dim3(kPlaceThreads), 0, st, a, pos, ids, order, (int32_t*)(ws + s.longs));
     return;
   }
   int bits = 1;  // of the largest key, rows
@@ -596,6 +622,7 @@ void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs
   const int passes = (bits + 8) / 9;
   SortArgs p{};
   p.hist = (int32_t*)(ws + s.hist);
+  p.longs = (int32_t*)(ws + s.longs);
   p.n = a.n;
   const int64_t tile = ((int64_t)a.n + kMaxTiles - 1) / kMaxTiles;
   p.tile = (int32_t)((tile + kSortThreads - 1) / kSortThreads * kSortThreads);
@@ -607,13 +634,13 @@ void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs
       p.out = buf[(passes - 1 - k / 2) % 2];  // the last pass ends in `order`
       p.shift = k / 2 * p.bits;
     }
-    pos.begin = pos_waves * k / (2 * passes);
-    pos.end = pos_waves * (k + 1) / (2 * passes);
+    pos.begin = items * k / (2 * passes);
+    pos.end = items * (k + 1) / (2 * passes);
     const dim3 grid(p.tiles + blocks_of(pos.end - pos.begin, kSortWaves));
     if (k % 2 == 0) {
-      hipLaunchKernelGGL((k_digits<A, W>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+      hipLaunchKernelGGL((k_digits<A, W, VEC>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
     } else {
-      hipLaunchKernelGGL((k_move<A, W>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+      hipLaunchKernelGGL((k_move<A, W, VEC>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
       p.in = p.out;
     }
   }
@@ -635,15 +662,17 @@ mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const 
     return lib_fail(MIST_E_INVALID, "embedding: a buffer is not aligned to its elements");
   const EmbedArgs a = args(d);
   // enough tokens a wave to keep several rows in flight, few enough to fill the device
-  int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 8192, 1, 64);
+  const int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 32768, 1, kAhead);
   const int64_t waves = (a.n + per_wave - 1) / per_wave * a.slabs;
   if (waves > (int64_t)kWaves << 23) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
-    const auto kernel = pos ? k_embed<A, W, true> : k_embed<A, W, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
-                       (int32_t)per_wave, ids, (const W*)table, (const W*)pos, (A*)out);
+    with_bool(d->hidden % kVec == 0, [&](auto vec) {
+      const auto kernel = pos ? k_embed<A, W, vec.value, true> : k_embed<A, W, vec.value, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
+                         (int32_t)per_wave, ids, (const W*)table, (const W*)pos, (A*)out);
+    });
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "embedding");
@@ -671,20 +700,24 @@ mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const
       !aligned(dtable, mist::type_bytes(d->table_type)) || !aligned(dpos, mist::type_bytes(d->table_type)) ||
       !aligned(workspace, 256))
     return lib_fail(MIST_E_INVALID, "embedding: a buffer is not aligned to its elements, or the workspace to 256");
-  const int64_t join_blocks = (s.chunks + kJoinChunks - 1) / kJoinChunks * a.slabs;
-  if (join_blocks > 1 << 23) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
+  const int64_t join_blocks = std::min<int64_t>(s.chunks / 2, kJoinRuns) * a.slabs;
+  if (join_blocks > 1 << 23 || (int64_t)a.slabs * kSlab > INT32_MAX) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
   const hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
-  const RowArgs r{(const Entry*)(ws + s.order), (float*)(ws + s.part), s.chunk, (int32_t)s.chunks, accumulate, s.chunks * a.slabs};
+  const RowArgs r{(const Entry*)(ws + s.order), (int32_t*)(ws + s.longs), (float*)(ws + s.part), s.chunk, (int32_t)s.chunks, accumulate, s.chunks * a.slabs};
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
     const PosArgs<A, W> p{(const A*)grad, (W*)dpos, 0, 0, accumulate};
-    order_tokens(a, ids, s, p, ws, st);
-    const int64_t waves = r.sum_waves + (accumulate ? 0 : a.rows);
-    if (waves)
-      hipLaunchKernelGGL((k_rows<A, W>), dim3(blocks_of(waves, kWaves)), dim3(kThreads), 0, st, a, r, (const A*)grad, (W*)dtable);
-    if (s.chunks > 2) hipLaunchKernelGGL((k_join<W>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
+    with_bool(d->hidden % kVec == 0, [&](auto vec) {
+      order_tokens<vec.value>(a, ids, s, p, ws, st);
+      const int64_t waves = r.sum_waves + (accumulate ? 0 : a.rows);
+      const bool once = a.n * a.hidden * (int64_t)sizeof(A) > kCache;
+      const auto rows = once ? k_rows<A, W, vec.value, true> : k_rows<A, W, vec.value, false>;
+      if (waves) hipLaunchKernelGGL(rows, dim3(blocks_of(waves, kWaves)), dim3(kThreads), 0, st, a, r, (const A*)grad, (W*)dtable);
+      if (s.chunks > 2)
+        hipLaunchKernelGGL((k_join<W, vec.value>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
+    });
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "embedding gradient");

@@ -738,7 +738,7 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     allowed); table: [rows, hidden]; pos: [at least seq, hidden] or None; out: ids' shape + [hidden], of
     any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
     torch = _torch()
-    L = load()
+    L = _lib or load()
     handle, other = _stream_of(torch, stream, table.device)
     if out is None:
         _need(table.dim() == 2, "embedding: the table must be [rows, hidden]")
@@ -757,7 +757,7 @@ def embed_grad(ids, grad, dtable, *, scale: float = 1.0, dpos=None, vocab_begin:
     """mist_embed_backward: the gradients of embed's table and positions from grad (ids' shape + [hidden]; it
     may be expanded), written to dtable and dpos (accumulate: added to them)."""
     torch = _torch()
-    L = load()
+    L = _lib or load()
     d = _embed_desc(ids, grad, dtable, scale, dpos, vocab_begin)
     device = grad.device
     handle, other = _stream_of(torch, stream, device)
@@ -874,7 +874,7 @@ def grad_finish(record: StepRecord, *, max_norm: float = float("inf"), grad_scal
                 stream=None) -> StepRecord:
     """mist_grad_finish: forms the norm and the clip factor from record.total, e.g. after an all-reduce of it."""
     torch = _torch()
-    L = load()
+    L = _lib or load()
     c = _clip_desc(kind, grad_scale, max_norm)
     handle, other = _stream_of(torch, stream, record.device)
     _on_device(torch, record.device, L.mist_grad_finish, ctypes.byref(c), record.ptr, handle)
