@@ -41,45 +41,61 @@ struct Entry {
 
 typedef Vec<float, kVec>::type Float8;
 
-// A lane's eight columns of a slab.  VEC (hidden a multiple of 8): consecutive, one access of 16 bytes for
-// 16-bit values; otherwise 64 apart.  Columns past the row are read as the row's last ones, so that loads
-// need no branch, and not written.
-template <bool VEC>
+// Which eight columns of a slab a lane holds:
+//   kWide   eight in a row: one access of 16 bytes (both types of 16 bits, hidden a multiple of 8)
+//   kSplit  two fours 256 apart: accesses of 16 bytes for fp32, 8 for 16 bits (hidden a multiple of 4).  Eight in
+//           a row would leave every other 16 bytes of a store to a second instruction: 2.4 TB/s where this
+//           reaches 4.9 (64365 tokens, 5440 columns)
+//   kOdd    one by one, 64 apart (any hidden)
+// Columns past the row are read as the row's last ones, so that loads need no branch, and not written.
+enum Layout { kWide, kSplit, kOdd };
+
+template <int L>
 struct Cols {
+  static constexpr int kRun = L == kWide ? 8 : L == kSplit ? 4 : 1, kRuns = kVec / kRun;
   int32_t first, hidden;
   __device__ __forceinline__ Cols(int32_t slab, int64_t h)
-      : first(slab * kSlab + (int32_t)(threadIdx.x % 64) * (VEC ? kVec : 1)), hidden((int32_t)h) {}
-  __device__ __forceinline__ int32_t at(int k) const { return VEC ? min(first, hidden - kVec) : min(first + 64 * k, hidden - 1); }
-  __device__ __forceinline__ bool in(int k) const { return VEC ? first < hidden : first + 64 * k < hidden; }
+      : first(slab * kSlab + (int32_t)(threadIdx.x % 64) * kRun), hidden((int32_t)h) {}
+  __device__ __forceinline__ bool in(int k) const { return first + 64 * kRun * k < hidden; }
+  // Run k of a row of T.  The offset is a 32-bit one to a uniform address, which takes no registers of its own.
+  template <class T>
+  __device__ __forceinline__ T* at(T* row, int k) const {
+    const uint32_t offset = (uint32_t)min(first + 64 * kRun * k, hidden - kRun) * (uint32_t)sizeof(T);
+    return (T*)((uintptr_t)row + offset);
+  }
 };
 
 // ONCE: not wanted again soon, so that it does not displace what is (rows of the table, the
 // gradient between its two uses).
-template <class T, bool VEC>
+template <class T, int L>
 struct Lane8 {
-  typedef typename Vec<T, kVec>::type type;
-  type v;
+  static constexpr int kRun = Cols<L>::kRun, kRuns = Cols<L>::kRuns;
+  typedef typename Vec<T, kRun>::type Run;
+  Run v[kRuns];
   template <bool ONCE = false>
-  __device__ __forceinline__ void load(const T* row, const Cols<VEC>& c) {
-    if (VEC) {
-      v = ONCE ? __builtin_nontemporal_load((const type*)(row + c.at(0))) : *(const type*)(row + c.at(0));
-    } else {
+  __device__ __forceinline__ void load(const T* row, const Cols<L>& c) {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = row[c.at(k)];
+    for (int k = 0; k < kRuns; ++k) {
+      const Run* p = (const Run*)c.at(row, k);
+      v[k] = ONCE ? __builtin_nontemporal_load(p) : *p;
     }
   }
-  __device__ __forceinline__ Float8 get() const { return __builtin_convertvector(v, Float8); }
-  template <bool ONCE = false>
-  static __device__ __forceinline__ void store(T* row, const Cols<VEC>& c, Float8 x) {
-    const type y = __builtin_convertvector(x, type);
-    if (VEC) {
-      if (!c.in(0)) return;
-      if (ONCE) __builtin_nontemporal_store(y, (type*)(row + c.at(0)));
-      else *(type*)(row + c.at(0)) = y;
-    } else {
+  __device__ __forceinline__ Float8 get() const {
+    Float8 x;
 #pragma unroll
-      for (int k = 0; k < kVec; ++k)
-        if (c.in(k)) row[c.at(k)] = y[k];
+    for (int k = 0; k < kVec; ++k) x[k] = (float)v[k / kRun][k % kRun];
+    return x;
+  }
+  template <bool ONCE = false>
+  static __device__ __forceinline__ void store(T* row, const Cols<L>& c, Float8 x) {
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k) {
+      Run y;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) y[i] = (T)x[k * kRun + i];
+      if (!c.in(k)) continue;
+      if (ONCE) __builtin_nontemporal_store(y, (Run*)c.at(row, k));
+      else *(Run*)c.at(row, k) = y;
     }
   }
 };
@@ -107,12 +123,14 @@ __device__ __forceinline__ int64_t act_offset(const EmbedArgs& a, uint32_t token
 }
 
 // ---- lookup ----------------------------------------------------------------------------------------
-// A wave takes `per_wave` (at most kAhead) tokens and one slab of columns, all rows in flight.  With
-// positions the tokens are taken position by position, so that a wave reads a position's row once for
+// A wave takes `per_wave` (at most kAhead) tokens and one slab of columns, all rows in flight: 4 (32768 tokens
+// of 8192 columns: 88 us; 8 tokens 98, 16 102), or 16 with positions (65536 of 2560: 94 us; 8 tokens 99,
+// 4 106).  With positions the tokens are taken position by position, so that a wave reads a position's row once for
 // its part of the batch.
-constexpr int kAhead = 8;
+template <bool POS>
+constexpr int kAhead = POS ? 16 : 4;
 
-template <class A, class W, bool VEC, bool POS>
+template <class A, class W, int L, bool POS>
 __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wave, const void* __restrict__ ids,
                                                     const W* __restrict__ table, const W* __restrict__ pos, A* __restrict__ out) {
   const int64_t wave = wave_index();
@@ -127,27 +145,27 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
   const int64_t row_at = row < a.rows ? row * a.table_stride : -1;
   const int64_t out_at = act_offset(a, token);
   const uint32_t s = token % (uint32_t)a.seq;
-  const Cols<VEC> col(slab, a.hidden);
-  Lane8<W, VEC> x[kAhead], p[kAhead];
+  const Cols<L> col(slab, a.hidden);
+  Lane8<W, L> x[kAhead<POS>], p[kAhead<POS>];
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) {
+  for (int k = 0; k < kAhead<POS>; ++k) {
     if (k < count) {
       const int64_t at = lane_value(row_at, k);
       if (at >= 0) x[k].load(table + at, col);
-      else x[k].v = {};
+      else x[k] = {};
       if (POS && (k == 0 || lane_value(s, k) != lane_value(s, k - 1))) p[k].load(pos + lane_value(s, k) * a.pos_stride, col);
     }
   }
   Float8 at_s = {};
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) {
+  for (int k = 0; k < kAhead<POS>; ++k) {
     if (k < count) {
       Float8 y = a.scale * x[k].get();
       if (POS) {
         if (k == 0 || lane_value(s, k) != lane_value(s, k - 1)) at_s = p[k].get();
         y += at_s;
       }
-      Lane8<A, VEC>::template store<true>(out + lane_value(out_at, k), col, y);
+      Lane8<A, L>::template store<true>(out + lane_value(out_at, k), col, y);
     }
   }
 }
@@ -157,7 +175,8 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
 // the tokens, which leave most of the device idle: `block` of `blocks` more blocks takes the items [begin, end).
 // The reads reach 4.2 TB/s (32 x 2048 tokens of 2560 columns, 16 bits); more loads at once, several
 // positions a wave, or several waves a position measured the same or worse.
-constexpr int kPosAhead = 8;
+template <int L>
+constexpr int kPosAhead = L == kOdd ? 2 : 8;  // one by one, eight take more registers than a block of 1024 threads has
 
 template <class A, class W>
 struct PosArgs {
@@ -167,30 +186,30 @@ struct PosArgs {
   int32_t accumulate;
 };
 
-template <bool VEC, class A, class W>
+template <int L, class A, class W>
 __device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32_t block, uint32_t blocks) {
   const int32_t waves = blockDim.x / 64;
   int64_t item = p.begin + __builtin_amdgcn_readfirstlane((int32_t)(block * waves + threadIdx.x / 64));
   for (; item < p.end; item += (int64_t)blocks * waves) {
     const int64_t s = item / a.slabs;
-    const Cols<VEC> col((int32_t)(item % a.slabs), a.hidden);
+    const Cols<L> col((int32_t)(item % a.slabs), a.hidden);
     Float8 acc = {};
-    for (int64_t b0 = 0; b0 < a.batch; b0 += kPosAhead) {
-      Lane8<A, VEC> x[kPosAhead];
+    for (int64_t b0 = 0; b0 < a.batch; b0 += kPosAhead<L>) {
+      Lane8<A, L> x[kPosAhead<L>];
 #pragma unroll
-      for (int k = 0; k < kPosAhead; ++k)
+      for (int k = 0; k < kPosAhead<L>; ++k)
         if (b0 + k < a.batch) x[k].load(p.grad + (b0 + k) * a.act_batch_stride + s * a.act_stride, col);
 #pragma unroll
-      for (int k = 0; k < kPosAhead; ++k)
+      for (int k = 0; k < kPosAhead<L>; ++k)
         if (b0 + k < a.batch) acc += x[k].get();
     }
     W* d = p.dpos + s * a.pos_stride;
     if (p.accumulate) {
-      Lane8<W, VEC> old;
+      Lane8<W, L> old;
       old.load(d, col);
       acc += old.get();
     }
-    Lane8<W, VEC>::store(d, col, acc);
+    Lane8<W, L>::store(d, col, acc);
   }
 }
 
@@ -200,12 +219,12 @@ __device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32
 constexpr int32_t kCounted = 8192;   // tokens up to which places are counted
 constexpr int kPlaceThreads = 1024, kPlaced = kPlaceThreads / 64;
 
-template <class A, class W, bool VEC>
+template <class A, class W, int L>
 __global__ __launch_bounds__(kPlaceThreads) void k_place(EmbedArgs a, PosArgs<A, W> pos, const void* __restrict__ ids, Entry* __restrict__ out,
                                                          int32_t* __restrict__ longs) {
   const int32_t blocks = (a.n + kPlaced - 1) / kPlaced;
   if ((int32_t)blockIdx.x >= blocks) {
-    sum_positions<VEC>(a, pos, blockIdx.x - blocks, gridDim.x - blocks);
+    sum_positions<L>(a, pos, blockIdx.x - blocks, gridDim.x - blocks);
     return;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *longs = 0;
@@ -251,10 +270,10 @@ __device__ __forceinline__ Entry sort_entry(const EmbedArgs& a, const SortArgs& 
   return s.in ? s.in[i] : Entry{token_row(a, ids, i), (uint32_t)i};
 }
 
-template <class A, class W, bool VEC>
+template <class A, class W, int L>
 __global__ __launch_bounds__(kSortThreads) void k_digits(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
   if ((int32_t)blockIdx.x >= s.tiles) {
-    sum_positions<VEC>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    sum_positions<L>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     return;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *s.longs = 0;
@@ -279,10 +298,10 @@ __device__ __forceinline__ uint64_t equals(uint32_t digit, int bits, bool live) 
   return m;
 }
 
-template <class A, class W, bool VEC>
+template <class A, class W, int L>
 __global__ __launch_bounds__(kSortThreads) void k_move(EmbedArgs a, SortArgs s, PosArgs<A, W> pos, const void* __restrict__ ids) {
   if ((int32_t)blockIdx.x >= s.tiles) {
-    sum_positions<VEC>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    sum_positions<L>(a, pos, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     return;
   }
   __shared__ int32_t at[kSortWaves][kMaxDigits];  // counts, then places
@@ -365,21 +384,21 @@ struct RowArgs {
   float* part;          // [chunks][2][slabs][kSlab], in lane order
   int32_t chunk, chunks;  // tokens a chunk, a power of two; chunks
   int32_t accumulate;
-  int64_t sum_waves;    // waves that sum chunks; the rest, one a row, clear rows without a token
+  int64_t sum_waves;    // waves that sum chunks; the rest clear rows without a token
 };
 
 __device__ __forceinline__ uint32_t row_at(const RowArgs& r, const EmbedArgs& a, int64_t i) {
   return i >= 0 && i < a.n ? r.order[i].row : (uint32_t)a.rows;
 }
 
-template <class A, class W, bool VEC, bool ONCE>
+template <class A, class W, int L, bool ONCE>
 struct RowSum {
   const EmbedArgs& a;
   const RowArgs& r;
   const A* grad;
   W* dtable;
   int32_t chunk, slab;
-  Cols<VEC> col;
+  Cols<L> col;
   Float8 acc = {};
   static constexpr int kGroup = sizeof(A) == 2 ? 8 : 4;
 
@@ -392,8 +411,8 @@ struct RowSum {
   // lane's.  slot >= 0: the range is one piece of a long run.
   __device__ __forceinline__ void take(uint32_t row, int64_t offset, int from, int to, uint32_t next, int slot) {
     for (int k0 = from; k0 < to; k0 += kGroup) {
-      Lane8<A, VEC> x[kGroup];
-      Lane8<W, VEC> old[kGroup];
+      Lane8<A, L> x[kGroup];
+      Lane8<W, L> old[kGroup];
       bool ends[kGroup];
       uint32_t mine[kGroup];
 #pragma unroll
@@ -412,8 +431,8 @@ struct RowSum {
           if (ends[k]) {
             Float8 y = a.scale * acc;
             W* d = dtable + mine[k] * a.table_stride;
-            if (r.accumulate) Lane8<W, VEC>::store(d, col, y + old[k].get());
-            else Lane8<W, VEC>::template store<true>(d, col, y);
+            if (r.accumulate) Lane8<W, L>::store(d, col, y + old[k].get());
+            else Lane8<W, L>::template store<true>(d, col, y);
             acc = Float8{};
           }
         }
@@ -462,46 +481,50 @@ struct RowSum {
   }
 };
 
-// Whether a token has the row: a search with 64 probes a step.
-__device__ __forceinline__ bool has_token(const RowArgs& r, int32_t n, uint32_t row) {
+// Rows [first, first + kClear) without a token are cleared; a lane looks for each.
+constexpr int kClear = 16;
+
+template <class W, int L>
+__device__ __forceinline__ void clear_rows(const EmbedArgs& a, const RowArgs& r, W* dtable, int64_t first) {
   const int lane = threadIdx.x % 64;
-  int32_t lo = 0, hi = n;   // the first place of a row not below is in [lo, hi]
-  while (hi - lo > 63) {
-    const int32_t step = (hi - lo + 63) / 64;
-    const int32_t at = lo + lane * step;
-    const int below = __popcll(__ballot(at < hi && r.order[at < hi ? at : lo].row < row));
-    if (below == 0) return r.order[lo].row == row;
-    hi = min(hi, lo + below * step);
-    lo = lo + (below - 1) * step + 1;
+  const int64_t row = first + lane;
+  bool found = lane >= kClear || row >= a.rows;
+  if (!found) {
+    int32_t lo = 0, hi = a.n;  // the first place of a row not below is in [lo, hi]
+    while (lo < hi) {
+      const int32_t mid = lo + (hi - lo) / 2;
+      if (r.order[mid].row < row) lo = mid + 1;
+      else hi = mid;
+    }
+    found = lo < a.n && r.order[lo].row == row;
   }
-  const int32_t at = lo + lane;
-  return __ballot(at < n && r.order[at < n ? at : 0].row == row) != 0;
+  for (uint64_t clear = ~__ballot(found); clear; clear &= clear - 1) {
+    W* d = dtable + (first + __ffsll((unsigned long long)clear) - 1) * a.table_stride;
+    for (int32_t slab = 0; slab < a.slabs; ++slab) Lane8<W, L>::template store<true>(d, Cols<L>(slab, a.hidden), Float8{});
+  }
 }
 
-template <class A, class W, bool VEC, bool ONCE>
+template <class A, class W, int L, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_rows(EmbedArgs a, RowArgs r, const A* __restrict__ grad, W* __restrict__ dtable) {
-  const int64_t waves = (int64_t)gridDim.x * kWaves, all = r.sum_waves + (r.accumulate ? 0 : a.rows);
+  const int64_t waves = (int64_t)gridDim.x * kWaves, all = r.sum_waves + (r.accumulate ? 0 : (a.rows + kClear - 1) / kClear);
   for (int64_t w = wave_index(); w < all; w += waves) {
     if (w < r.sum_waves) {
       const int32_t chunk = (int32_t)(w / a.slabs), slab = (int32_t)(w % a.slabs);
-      RowSum<A, W, VEC, ONCE> s{a, r, grad, dtable, chunk, slab, Cols<VEC>(slab, a.hidden)};
+      RowSum<A, W, L, ONCE> s{a, r, grad, dtable, chunk, slab, Cols<L>(slab, a.hidden)};
       s.run();
     } else {
-      const uint32_t row = (uint32_t)(w - r.sum_waves);
-      if (a.n && has_token(r, a.n, row)) continue;
-      for (int32_t slab = 0; slab < a.slabs; ++slab)
-        Lane8<W, VEC>::template store<true>(dtable + row * a.table_stride, Cols<VEC>(slab, a.hidden), Float8{});
+      clear_rows<W, L>(a, r, dtable, (w - r.sum_waves) * kClear);
     }
   }
 }
 
 // Long runs: a block takes a run and a slab, its waves add up a share of the pieces each, in order, and the
 // shares are added in order.
-template <class W, bool VEC>
+template <class W, int L>
 __global__ __launch_bounds__(kThreads) void k_join(EmbedArgs a, RowArgs r, W* __restrict__ dtable) {
   __shared__ Float8 shares[kWaves][64];
   const int32_t slab = (int32_t)(blockIdx.x % a.slabs), wave = threadIdx.x / 64, lane = threadIdx.x % 64, C = r.chunk;
-  const Cols<VEC> col(slab, a.hidden);
+  const Cols<L> col(slab, a.hidden);
   const int32_t runs = r.longs[0];
   for (int32_t i = (int32_t)(blockIdx.x / a.slabs); i < runs; i += (int32_t)(gridDim.x / a.slabs)) {
     const int32_t c = r.longs[1 + i];
@@ -524,14 +547,103 @@ __global__ __launch_bounds__(kThreads) void k_join(EmbedArgs a, RowArgs r, W* __
       W* d = dtable + row * a.table_stride;
       Float8 y = a.scale * acc;
       if (r.accumulate) {
-        Lane8<W, VEC> old;
+        Lane8<W, L> old;
         old.load(d, col);
         y += old.get();
       }
-      Lane8<W, VEC>::store(d, col, y);
+      Lane8<W, L>::store(d, col, y);
     }
     __syncthreads();
   }
+}
+
+// ---- short inputs ----------------------------------------------------------------------------------
+// Everything in one launch, where launches are what takes the time.  A block takes a token and a slab; it finds
+// the tokens of the same row with a ballot a wave, and goes on if its token is the first of them.  Each
+// wave adds up its 64 tokens' terms in order and the waves' sums are added in order; up to kFew terms
+// are left to the first wave.  Further blocks clear rows without a token, and sum positions.
+constexpr int32_t kShort = 1024;     // tokens, at most
+constexpr int64_t kShortWaves = 16384;
+constexpr int kFew = 8, kShortClear = 64;
+
+template <class A, class W, int L>
+__global__ __launch_bounds__(kShort) void k_short(EmbedArgs a, PosArgs<A, W> pos, const void* __restrict__ ids, const A* __restrict__ grad,
+                                                  W* __restrict__ dtable, int32_t accumulate) {
+  __shared__ Float8 shares[kShort / 64][64];
+  __shared__ uint64_t same[kShort / 64];
+  const int32_t sums = a.n * a.slabs, clears = accumulate ? 0 : (int32_t)((a.rows + kShortClear - 1) / kShortClear);
+  const int32_t i0 = threadIdx.x, wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / 64), lane = threadIdx.x % 64, waves = blockDim.x / 64;
+  int64_t block = blockIdx.x;
+  if (block >= sums + clears) {
+    sum_positions<L>(a, pos, blockIdx.x - sums - clears, gridDim.x - sums - clears);
+    return;
+  }
+  const uint32_t row = i0 < a.n ? token_row(a, ids, i0) : (uint32_t)a.rows;
+  if (block >= sums) {
+    uint8_t* seen = (uint8_t*)same;  // of kShortClear rows
+    const int64_t first = (block - sums) * kShortClear;
+    if (threadIdx.x < kShortClear) seen[threadIdx.x] = 0;
+    __syncthreads();
+    if (row >= first && row < first + kShortClear) seen[row - first] = 1;
+    __syncthreads();
+    for (int k = wave; k < kShortClear && first + k < a.rows; k += waves) {
+      if (seen[k]) continue;
+      for (int32_t slab = 0; slab < a.slabs; ++slab)
+        Lane8<W, L>::template store<true>(dtable + (first + k) * a.table_stride, Cols<L>(slab, a.hidden), Float8{});
+    }
+    return;
+  }
+  const int32_t token = (int32_t)block / a.slabs, slab = (int32_t)block % a.slabs;
+  const uint32_t mine = token_row(a, ids, token);
+  if (mine == (uint32_t)a.rows) return;
+  const uint64_t my = __ballot(row == mine);
+  if (lane == 0) same[wave] = my;
+  __syncthreads();
+  int total = 0;
+  for (int w = 0; w < waves; ++w) {
+    const uint64_t m = same[w];
+    if (m && w * 64 + __ffsll((unsigned long long)m) - 1 < token) return;  // not the first of the row
+    total += __popcll(m);
+  }
+  const Cols<L> col(slab, a.hidden);
+  Float8 acc = {};
+  auto add = [&](uint64_t m, int32_t base) {
+    while (m) {
+      Lane8<A, L> x[kFew];
+      const int count = __popcll(m);
+#pragma unroll
+      for (int k = 0; k < kFew; ++k) {
+        if (k < count) {
+          x[k].load(grad + act_offset(a, base + __ffsll((unsigned long long)m) - 1), col);
+          m &= m - 1;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kFew; ++k)
+        if (k < count) acc += x[k].get();
+    }
+  };
+  if (total <= kFew) {
+    if (wave) return;
+    for (int w = 0; w < waves; ++w) {
+      const uint64_t m = same[w];
+      add((uint64_t)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)m), w * 64);
+    }
+  } else {
+    add(my, wave * 64);
+    shares[wave][lane] = acc;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < waves; ++w) acc += shares[w][lane];
+  }
+  W* d = dtable + mine * a.table_stride;
+  Float8 y = a.scale * acc;
+  if (accumulate) {
+    Lane8<W, L> old;
+    old.load(d, col);
+    y += old.get();
+  }
+  Lane8<W, L>::store(d, col, y);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -569,14 +681,21 @@ EmbedArgs args(const mist_embed_desc* d) {
                    (int32_t)(d->batch * d->seq), (int32_t)((d->hidden + kSlab - 1) / kSlab)};
 }
 
-template <class F>
-void with_bool(bool b, F&& f) {
-  if (b) f(std::true_type{});
-  else f(std::false_type{});
+// f(the layout for the types and hidden).
+template <class A, class W, class F>
+void with_layout(int64_t hidden, F&& f) {
+  if constexpr (sizeof(A) == 2 && sizeof(W) == 2) {
+    if (hidden % 8 == 0) return f(std::integral_constant<int, kWide>{});
+  }
+  if (hidden % 4 == 0) f(std::integral_constant<int, kSplit>{});
+  else f(std::integral_constant<int, kOdd>{});
 }
 
 // Blocks for a number of waves, capped so that a grid stays below 2^32 threads (kernels loop).
 unsigned blocks_of(int64_t waves, int per_block) { return (unsigned)std::min<int64_t>((waves + per_block - 1) / per_block, 1 << 21); }
+
+// Whether one launch does all (k_short): few tokens, and few waves to look through them.
+bool is_short(const EmbedArgs& a) { return a.n <= kShort && (int64_t)a.n * a.slabs * ((a.n + 63) / 64) <= kShortWaves && a.rows <= 1 << 24; }
 
 // Places in the workspace.
 struct Scratch {
@@ -586,6 +705,7 @@ struct Scratch {
 };
 Scratch scratch(const EmbedArgs& a) {
   Scratch s{};
+  if (is_short(a)) return s;
   // Smaller chunks where there are too few waves to hide the gather's latency.
   s.chunk = kMaxChunk;
   while (s.chunk > 8 && ((int64_t)a.n + s.chunk - 1) / s.chunk * a.slabs < 2048) s.chunk /= 2;
@@ -607,14 +727,14 @@ Scratch scratch(const EmbedArgs& a) {
   return s;
 }
 
-template <bool VEC, class A, class W>
+template <int L, class A, class W>
 void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs<A, W> pos, char* ws, hipStream_t st) {
   Entry* order = (Entry*)(ws + s.order);
   const int64_t items = pos.dpos ? a.seq * a.slabs : 0;  // of the positions
   if (a.n <= kCounted) {
     pos.end = items;
     const dim3 grid((unsigned)((a.n + kPlaced - 1) / kPlaced) + blocks_of(items, kPlaced));
-    if (grid.x) hipLaunchKernelGGL((k_place<A, W, VEC>), grid, dim3(kPlaceThreads), 0, st, a, pos, ids, order, (int32_t*)(ws + s.longs));
+    if (grid.x) hipLaunchKernelGGL((k_place<A, W, L>), grid, dim3(kPlaceThreads), 0, st, a, pos, ids, order, (int32_t*)(ws + s.longs));
     return;
   }
   int bits = 1;  // of the largest key, rows
@@ -638,9 +758,9 @@ void order_tokens(const EmbedArgs& a, const void* ids, const Scratch& s, PosArgs
     pos.end = items * (k + 1) / (2 * passes);
     const dim3 grid(p.tiles + blocks_of(pos.end - pos.begin, kSortWaves));
     if (k % 2 == 0) {
-      hipLaunchKernelGGL((k_digits<A, W, VEC>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+      hipLaunchKernelGGL((k_digits<A, W, L>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
     } else {
-      hipLaunchKernelGGL((k_move<A, W, VEC>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
+      hipLaunchKernelGGL((k_move<A, W, L>), grid, dim3(kSortThreads), 0, st, a, p, pos, ids);
       p.in = p.out;
     }
   }
@@ -662,14 +782,14 @@ mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const 
     return lib_fail(MIST_E_INVALID, "embedding: a buffer is not aligned to its elements");
   const EmbedArgs a = args(d);
   // enough tokens a wave to keep several rows in flight, few enough to fill the device
-  const int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 32768, 1, kAhead);
+  const int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 16384, 1, pos ? kAhead<true> : kAhead<false>);
   const int64_t waves = (a.n + per_wave - 1) / per_wave * a.slabs;
   if (waves > (int64_t)kWaves << 23) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
-    with_bool(d->hidden % kVec == 0, [&](auto vec) {
-      const auto kernel = pos ? k_embed<A, W, vec.value, true> : k_embed<A, W, vec.value, false>;
+    with_layout<A, W>(d->hidden, [&](auto layout) {
+      const auto kernel = pos ? k_embed<A, W, layout.value, true> : k_embed<A, W, layout.value, false>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
                          (int32_t)per_wave, ids, (const W*)table, (const W*)pos, (A*)out);
     });
@@ -709,14 +829,24 @@ mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
     const PosArgs<A, W> p{(const A*)grad, (W*)dpos, 0, 0, accumulate};
-    with_bool(d->hidden % kVec == 0, [&](auto vec) {
-      order_tokens<vec.value>(a, ids, s, p, ws, st);
-      const int64_t waves = r.sum_waves + (accumulate ? 0 : a.rows);
+    with_layout<A, W>(d->hidden, [&](auto layout) {
+      constexpr int L = layout.value;
+      if (is_short(a)) {
+        const int threads = std::max(256, (a.n + 63) / 64 * 64);
+        const int64_t blocks = (int64_t)a.n * a.slabs + (accumulate ? 0 : (a.rows + kShortClear - 1) / kShortClear);
+        PosArgs<A, W> all = p;
+        all.end = dpos ? a.seq * a.slabs : 0;
+        const dim3 grid((unsigned)(blocks + blocks_of(all.end, threads / 64)));
+        if (grid.x) hipLaunchKernelGGL((k_short<A, W, L>), grid, dim3(threads), 0, st, a, all, ids, (const A*)grad, (W*)dtable, accumulate);
+        return;
+      }
+      order_tokens<L>(a, ids, s, p, ws, st);
+      const int64_t waves = r.sum_waves + (accumulate ? 0 : (a.rows + kClear - 1) / kClear);
       const bool once = a.n * a.hidden * (int64_t)sizeof(A) > kCache;
-      const auto rows = once ? k_rows<A, W, vec.value, true> : k_rows<A, W, vec.value, false>;
+      const auto rows = once ? k_rows<A, W, L, true> : k_rows<A, W, L, false>;
       if (waves) hipLaunchKernelGGL(rows, dim3(blocks_of(waves, kWaves)), dim3(kThreads), 0, st, a, r, (const A*)grad, (W*)dtable);
       if (s.chunks > 2)
-        hipLaunchKernelGGL((k_join<W, vec.value>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
+        hipLaunchKernelGGL((k_join<W, L>), dim3((unsigned)join_blocks), dim3(kThreads), 0, st, a, r, (W*)dtable);
     });
   });
   const hipError_t e = hipGetLastError();

@@ -17,7 +17,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTotalThreads = 1024;
 constexpr int64_t kChunk = 4096;     // elements a block takes at a time, of one tensor
-constexpr int64_t kMostPieces = (int64_t)1 << 23;  // a grid of a block each stays below 2^32 threads
+constexpr int64_t kMostPieces = (int64_t)1 << 28;
+constexpr uint32_t kGridX = 1 << 22;  // blocks along x, so that a dimension has less than 2^32 threads
 constexpr int kNormBlocks = 2048;    // partial results of the norm, at most
 
 // A block's piece of work: elements [part * kChunk, ...) of a tensor.
@@ -51,6 +52,11 @@ struct Span {
   uint64_t ptr;
   int64_t begin, end;  // elements
 };
+
+// The block's number counted from the last of `blocks`; negative past the first.
+__device__ __forceinline__ int64_t block_from_last(int64_t blocks) {
+  return blocks - 1 - ((int64_t)blockIdx.y * gridDim.x + blockIdx.x);
+}
 
 __device__ __forceinline__ Span span_of(const List& l, const Piece p) {
   const int64_t begin = (int64_t)p.part * kChunk, size = l.size[p.tensor];
@@ -143,12 +149,13 @@ __global__ void k_finish(mist_clip_desc c, mist_step_record* r) { finish(c, r, r
 constexpr int kClipBlocks = 2;
 
 template <class G, class O>
-__global__ __launch_bounds__(kThreads) void k_clip(List g, List out, const mist_step_record* __restrict__ r) {
+__global__ __launch_bounds__(kThreads) void k_clip(List g, List out, int64_t n_pieces, const mist_step_record* __restrict__ r) {
   constexpr int kV = sizeof(G) == 2 && sizeof(O) == 2 ? 8 : 4, kLoads = 2;
   typedef typename Vec<G, kV>::type VG;
   typedef typename Vec<O, kV>::type VO;
   typedef typename Vec<float, kV>::type VF;
-  const uint32_t block = gridDim.x - 1 - blockIdx.x;
+  const int64_t block = block_from_last(n_pieces * kClipBlocks);
+  if (block < 0) return;
   const Piece p = g.piece[block / kClipBlocks];
   Span s = span_of(g, p);
   s.begin += block % kClipBlocks * (kChunk / kClipBlocks);
@@ -201,13 +208,14 @@ __device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamScalars& c
 
 // Pieces from the last to the first, as the clipping takes them.
 template <class G, class W, bool WEIGHTS>
-__global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, const mist_step_record* __restrict__ r) {
+__global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, int64_t n_pieces, const mist_step_record* __restrict__ r) {
   constexpr int kV = 4, kLoads = 4;
   typedef typename Vec<G, kV>::type VG;
   typedef typename Vec<W, kV>::type VW;
   typedef typename Vec<float, kV>::type VF;
-  if (!r->applied) return;
-  const Piece piece = a.g.piece[gridDim.x - 1 - blockIdx.x];
+  const int64_t block = block_from_last(n_pieces);
+  if (block < 0 || !r->applied) return;
+  const Piece piece = a.g.piece[block];
   const Span s = span_of(a.g, piece);
   const AdamScalars c{r->coef, (float)(1.0 / (1.0 - power(a.beta1, r->step))), (float)(1.0 / (1.0 - power(a.beta2, r->step)))};
   const G* g = (const G*)s.ptr + s.begin;
@@ -288,6 +296,11 @@ bool clip_ok(const mist_clip_desc* c) {
 
 bool aligned8(const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; }
 
+dim3 grid_of(int64_t blocks) {
+  const uint32_t x = (uint32_t)std::min<int64_t>(blocks, kGridX);
+  return dim3(x, (uint32_t)((blocks + x - 1) / x));
+}
+
 int32_t norm_blocks(const mist_tensors* g) { return (int32_t)std::min<int64_t>(g->n_pieces, kNormBlocks); }
 
 }  // namespace
@@ -308,7 +321,7 @@ mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, i
     if (sizes[i] && (!ptrs[i] || reinterpret_cast<uintptr_t>(ptrs[i]) % bytes))
       return lib_fail(MIST_E_INVALID, "tensor list: a tensor is null or not aligned to its elements");
     pieces += (sizes[i] + kChunk - 1) / kChunk;
-    if (pieces > kMostPieces) return lib_fail(MIST_E_INVALID, "tensor list: too many elements (over about 2^36)");
+    if (pieces > kMostPieces) return lib_fail(MIST_E_INVALID, "tensor list: too many elements (over about 2^40)");
   }
   mist_tensors* T = nullptr;
   try {
@@ -412,7 +425,8 @@ mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record
   mist::with_types(g->type, out->type, [&](auto x, auto y) {
     using G = typename decltype(x)::type;
     using O = typename decltype(y)::type;
-    hipLaunchKernelGGL((k_clip<G, O>), dim3((unsigned)g->n_pieces * kClipBlocks), dim3(kThreads), 0, (hipStream_t)stream, g->list, out->list, record);
+    hipLaunchKernelGGL((k_clip<G, O>), grid_of(g->n_pieces * kClipBlocks), dim3(kThreads), 0, (hipStream_t)stream, g->list, out->list,
+                       g->n_pieces, record);
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "clipping");
@@ -436,12 +450,12 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
   AdamArgs k{p->list, m->list, v->list, g->list, w ? w->list : List{}, a->beta1, a->beta2,
              (float)a->beta1, (float)a->beta2, (float)(1.0 - a->beta1), (float)(1.0 - a->beta2),
              (float)a->lr, (float)(1.0 - a->lr * a->weight_decay), (float)a->eps};
-  const dim3 grid((unsigned)g->n_pieces), block(kThreads);
+  const dim3 grid = grid_of(g->n_pieces), block(kThreads);
   mist::with_types(g->type, w ? w->type : MIST_F32, [&](auto x, auto y) {
     using G = typename decltype(x)::type;
     using W = typename decltype(y)::type;
-    if (w) hipLaunchKernelGGL((k_adam<G, W, true>), grid, block, 0, (hipStream_t)stream, k, record);
-    else if constexpr (sizeof(W) == 4) hipLaunchKernelGGL((k_adam<G, W, false>), grid, block, 0, (hipStream_t)stream, k, record);
+    if (w) hipLaunchKernelGGL((k_adam<G, W, true>), grid, block, 0, (hipStream_t)stream, k, g->n_pieces, record);
+    else if constexpr (sizeof(W) == 4) hipLaunchKernelGGL((k_adam<G, W, false>), grid, block, 0, (hipStream_t)stream, k, g->n_pieces, record);
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MIST_OK : hip_failed(e, "Adam step");

@@ -99,6 +99,10 @@ GRADS = LOOKUPS + [
     (1, 8192, 9000, 8, "spread"), (1, 8193, 9000, 8, "spread"), (2, 5000, 40, 24, "pad"), (1, 20000, 300, 8, "same"),
     (4, 4096, 30011, 40, "text"), (3, 11000, 1025, 7, "text"), (1, 70000, 2, 8, "text"), (2, 9000, 2048, 8, "none"),
     (2, 33000, 70001, 9, "text"),
+    # one launch up to 1024 tokens, and the sizes around it; rows few and many, and fours that are no eights
+    (1, 1023, 60, 520, "text"), (2, 512, 3000, 12, "pad"), (1, 1025, 60, 20, "text"), (1, 700, 1, 1030, "same"),
+    (16, 64, 100000, 8, "text"), (1, 1024, 2000, 8, "spread"), (3, 300, 40, 4100, "text"), (2, 4500, 700, 516, "text"),
+    (9, 1500, 64, 260, "same"),
 ]
 
 
@@ -293,6 +297,7 @@ def test_refusals(torch):
         mist.embed_grad(ids, grad, table, dpos=torch.zeros(2, 8, device="cuda"))
     L = mist.load()
     import ctypes
+    ids, grad = torch.zeros(2, 3000, dtype=torch.int64, device="cuda"), torch.zeros(2, 3000, 8, device="cuda")
     d = mist._embed_desc(ids, grad, table, 1.0, None, 0)
     assert L.mist_embed_backward(ctypes.byref(d), ids.data_ptr(), grad.data_ptr(), table.data_ptr(), None, 0,
                                  grad.data_ptr(), 1, None) == -5

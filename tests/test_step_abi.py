@@ -44,6 +44,8 @@ def test_embedding_buffers_are_refused():
         assert L.mist_embed_forward(r(_embed(**over)), P, P, None, P, None) == -1 and b"overlap" in L.mist_last_error()
     assert L.mist_embed_forward(r(_embed(pos_stride=4)), P, P, P, P, None) == -1
     need = ctypes.c_size_t()
+    assert L.mist_embed_workspace(r(d), r(need)) == 0  # a short input may need none
+    d = _embed(seq=3000, ids_stride=3000, act_batch_stride=24000)
     assert L.mist_embed_workspace(r(d), r(need)) == 0 and need.value > 0
     assert L.mist_embed_workspace(r(d), None) == -1 and L.mist_embed_workspace(None, r(need)) == -1
     for args in ((None, P, P, None, 0, P), (P, None, P, None, 0, P), (P, P, None, None, 0, P), (P, P, P, None, 0, None),
