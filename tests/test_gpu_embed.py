@@ -94,6 +94,21 @@ def test_lookup(torch, shape, act, weight):
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("hidden", [512, 516, 1024, 1537, 2048, 4096, 4095, 8192, 9000])
+@pytest.mark.parametrize("n", [1, 5, 517, 4001])
+def test_lookup_without_positions(torch, n, hidden):
+    """Every number of column slabs; a power-of-two scale makes the products exact, so that one rounding is left."""
+    from paper_2503_19050_amd import mist
+    table = torch.randn(97, hidden, device="cuda")
+    ids = torch.randint(-3, 100, (1, n), device="cuda", dtype=torch.int32)
+    inside = ((ids >= 0) & (ids < 97))[..., None]
+    for act, weight in ((torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.float32)):
+        w = table.to(weight)
+        want = torch.where(inside, w.double()[ids.clamp(0, 96).long()] * 4.0, 0.0).to(act)
+        out = torch.full((1, n, hidden), float("nan"), device="cuda", dtype=act)
+        assert torch.equal(mist.embed(ids, w, scale=4.0, out=out), want)
+
+
 GRADS = LOOKUPS + [
     (1, 63, 10, 8, "text"), (1, 64, 10, 16, "same"), (1, 65, 10, 8, "text"), (3, 129, 5, 24, "text"), (1, 8191, 500, 16, "text"),
     (1, 8192, 9000, 8, "spread"), (1, 8193, 9000, 8, "spread"), (2, 5000, 40, 24, "pad"), (1, 20000, 300, 8, "same"),
