@@ -602,7 +602,7 @@ mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record
 typedef struct mist_adam_desc {
   double lr;             /* >= 0 */
   double beta1, beta2;   /* in [0, 1) */
-  double eps;            /* >= 0 */
+  double eps;            /* > 0, in the range of fp32 */
   double weight_decay;   /* >= 0, decoupled */
 } mist_adam_desc;
 
@@ -611,7 +611,8 @@ typedef struct mist_adam_desc {
  *     p = p - lr * ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay * p);
  *     w = p rounded to w's type.
  * p, m and v are MIST_F32 (bytes_opt = 12), g is of any type, w may be NULL (no 16-bit weights); all
- * with g's count and sizes.  One step may be made in several calls, e.g. one per layer.  With applied = 0 (gradients
+ * with g's count and sizes.  |g'| past 1.8e19 leaves fp32 when squared (v = inf): such gradients are to be
+ * clipped.  One step may be made in several calls, e.g. one per layer.  With applied = 0 (gradients
  * with inf or NaN) it changes nothing.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const mist_tensors* v, const mist_tensors* g,
                            const mist_tensors* w, const mist_step_record* record, const mist_adam_desc* a,

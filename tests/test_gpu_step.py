@@ -329,7 +329,8 @@ def test_refusals(torch):
            lambda: mist.adam_step(P, M, V, other, rec, lr=0.1), lambda: mist.adam_step(P, M, half, G, rec, lr=0.1),
            lambda: mist.adam_step(P, M, M, G, rec, lr=0.1), lambda: mist.adam_step(P, M, V, G, rec, lr=-1.0),
            lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, betas=(1.0, 0.9)),
-           lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, eps=-1.0), lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, weights=P),
+           lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, eps=-1.0), lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, eps=0.0),
+           lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, eps=1e-60), lambda: mist.adam_step(P, M, V, G, rec, lr=0.1, weights=P),
            lambda: mist.adam_step(P, M, V, G, rec, lr=float("nan")), lambda: mist.grad_finish(rec, max_norm=-1.0)]
     for call in bad:
         with pytest.raises(mist.MistError) as e:
