@@ -7,13 +7,13 @@
 // orders the tokens by row (stable, so that a row's terms are added in token order whatever ran first), sums
 // each row's terms in fp32 registers and writes the row once: no atomics on values.  Measured on one MI355X
 // (16-bit values; a large copy reads and writes 4.9 TB/s, a fill writes 6.8):
-//   lookup    65536 tokens of 2560 columns with positions  94 us, 336 MB written and 205 MB read: 5.7 TB/s
+//   lookup    65536 tokens of 2560 columns with positions  89-94 us, 336 MB written and 205 MB read: 5.7 TB/s
 //             32768 of 8192 in a shard of 4000 rows         81 us, 537 MB written and 80 MB read: 7.6 TB/s
-//   gradient  65536 of 2560, 50257 rows, with positions   191 us: order with the positions' sums 4 x 21 us
-//             (335 MB read), rows 99 us (339 MB read, 262 MB written), long runs 6.5 us.  The gradient is read twice,
-//             once by position and once by row: 4.9 TB/s over the call
-//             131072 of 8192, 32000 rows                  449 us: order 26 us, rows 415 us (1617 MB read, 549 MB
-//             written: 5.2 TB/s), long runs 13 us
+//   gradient  65536 of 2560, 50257 rows, with positions   185-190 us: order with the positions' sums 4 x 21 us
+//             (335 MB read), rows 95 us (339 MB read, 262 MB written), long runs 6.5 us.  The gradient is read twice,
+//             once by position and once by row: 5 TB/s over the call
+//             131072 of 8192, 32000 rows                  427-441 us: order 27 us, rows 401 us (1617 MB read, 549 MB
+//             written: 5.4 TB/s), long runs 13 us
 //             4095 of 4096 added to fp32                   30 us: order 7 us, rows 18 us, long runs 5 us
 //             256 of 512 in fp32, 2048 rows                9.4 us, one launch
 #include <hip/hip_runtime.h>

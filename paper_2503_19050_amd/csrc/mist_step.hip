@@ -1,7 +1,7 @@
 // Lists of tensors, the global gradient norm, clipping and the Adam step.
 //
 // Each is one pass over its values, a few operations a byte: bound by memory.  A list's tensors are cut into
-// pieces of 4096 elements, one block each (blocks that take pieces in turn measured 3650 us where these
+// pieces of 4096 elements, one block each (on one card, blocks that take pieces in turn measured 3650 us where these
 // take 3410, pieces of 2048 or 8192 elements 3515 and 3500: Adam step of 629 million parameters).  Measured on one
 // MI355X, where a large copy reads and writes 4.9 TB/s:
 //   norm   302 million fp32  201 us, 6.0 TB/s;  629 million bf16  212 us, 5.9 TB/s
