@@ -9,6 +9,7 @@ smallest subnormal).  Constants of the call are rounded to fp32 once each.
   m      6 2^-24 (beta1 |m| + (1 - beta1) |g'|) + tiny;   v  8 2^-24 (beta2 v + (1 - beta2) g'^2) + tiny
   p      4 2^-24 |p| + lr 24 2^-24 (beta1 |m| + (1 - beta1) |g'|) / bc1 / (sqrt(v / bc2) + eps) + tiny;   w  u |p| more
 """
+import gc
 import math
 import sys
 
@@ -340,3 +341,34 @@ def test_refusals(torch):
     with pytest.raises(mist.MistError):
         mist.grad_norm(X, rec)
     assert int(rec.step) == 0 and mist.load().mist_grad_norm(G.h, None, 0, 1, rec.data.data_ptr(), None, 0, None) == -1
+
+
+def test_list_without_device_memory(torch):
+    """An allocator that has nothing: MIST_E_NOMEM, no list, nothing freed that was not given."""
+    import ctypes
+    from paper_2503_19050_amd import mist
+    L, freed = mist.load(), []
+    cb = mist.ALLOC_FN(lambda n, s, c: None), mist.FREE_FN(lambda p, c: freed.append(p))
+    t = torch.ones(5, device="cuda")
+    out = ctypes.c_void_p(1)
+    rc = L.mist_tensors_create((ctypes.c_void_p * 1)(t.data_ptr()), (ctypes.c_int64 * 1)(5), 1, 0,
+                               ctypes.byref(mist.Allocator(cb[0], cb[1], None)), ctypes.byref(out))
+    assert rc == -2 and not out.value and not freed and L.mist_last_error()
+
+
+@pytest.mark.parametrize("allocator", ["torch", None])
+def test_lists_come_and_go(torch, allocator):
+    """A list's tables are returned when it is closed; the tensors stay."""
+    from paper_2503_19050_amd import mist
+    t = [torch.full((1000,), float(k), device="cuda") for k in range(50)]
+    gc.collect()  # what earlier tests left
+    before = torch.cuda.memory_allocated()
+    for _ in range(3):
+        with mist.TensorList(t, allocator=allocator) as T:
+            rec = mist.StepRecord()
+            mist.grad_norm(T, rec)
+            assert float(rec.total) == sum(1000.0 * k * k for k in range(50)) and len(T) == 50
+        del rec
+    gc.collect()
+    assert torch.cuda.memory_allocated() == before
+    assert all((x == k).all() for k, x in enumerate(t))
