@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void k_clip(List g, List out, int64_t n_p
 struct AdamArgs {
   List p, m, v, g, w;
   double beta1, beta2;
-  float b1, b2, one_b1, one_b2, lr, keep, eps;  // keep = 1 - lr * weight_decay
+  float b1, b2, one_b1, one_b2, lr, decay, eps;
 };
 
 __device__ double power(double x, int64_t n) {
@@ -211,7 +211,8 @@ __device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamScalars& c
   const float x = c.coef * g;
   m = fmaf(a.b1, m, a.one_b1 * x);
   v = fmaf(a.b2, v, a.one_b2 * x * x);
-  p = fmaf(-a.lr, m * c.ibc1 / (sqrtf(v * c.ibc2) + a.eps), a.keep * p);
+  // the decay joins the update: a factor 1 - lr * weight_decay next to 1 holds a small product in few bits or none
+  p = fmaf(-a.lr, fmaf(a.decay, p, m * c.ibc1 / (sqrtf(v * c.ibc2) + a.eps)), p);
   asm("" : "+v"(p));  // the weights are the stored p rounded, not the sum rounded once to 16 bits
 }
 
@@ -458,7 +459,7 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
   if (!g->n_pieces) return MIST_OK;
   AdamArgs k{p->list, m->list, v->list, g->list, w ? w->list : List{}, a->beta1, a->beta2,
              (float)a->beta1, (float)a->beta2, (float)(1.0 - a->beta1), (float)(1.0 - a->beta2),
-             (float)a->lr, (float)(1.0 - a->lr * a->weight_decay), (float)a->eps};
+             (float)a->lr, (float)a->weight_decay, (float)a->eps};
   const dim3 grid = grid_of(g->n_pieces), block(kThreads);
   mist::with_types(g->type, w ? w->type : MIST_F32, [&](auto x, auto y) {
     using G = typename decltype(x)::type;

@@ -1,0 +1,51 @@
+"""The Adam step's constants and its verdict on the GPU: what the weight decay and the betas are worth in fp32.
+
+A single value cannot show an error far below its last place, the mean over many can: rounding one
+result errs by up to half an ulp either way, evenly where the low bits are spread evenly, so the mean of N
+of them is within 6 ulp / sqrt(12 N) of none (six deviations of N evenly spread errors).  Added to it below: the largest
+error that the other roundings of the formula could share.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+N = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "a GPU is required"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def lists(mist, *tensors):
+    return [mist.TensorList([t]) for t in tensors]
+
+
+def mean_bound(ulp):
+    return 6 * ulp / math.sqrt(12 * N)
+
+
+@pytest.mark.parametrize("lr, decay", [(1e-6, 0.01), (1e-5, 0.01), (3e-7, 0.1), (3e-4, 0.1)])
+def test_small_weight_decay_is_kept(torch, lr, decay):
+    """Weights in [2^-7, 2^-6) (one ulp of 2^-30) under updates of either sign: their mean moves by lr * decay * mean(p)."""
+    from paper_2503_19050_amd import mist
+    gen = torch.Generator("cuda").manual_seed(3)
+    p = torch.empty(N, device="cuda").uniform_(2.0 ** -7, 2.0 ** -6, generator=gen)
+    p.clamp_(2.0 ** -7 + 2 * lr, 2.0 ** -6 - 2 * lr)
+    m = torch.empty(N, device="cuda").uniform_(-1.0, 1.0, generator=gen)
+    v, g = torch.ones(N, device="cuda"), torch.zeros(N, device="cuda")
+    was, t = [x.double() for x in (p, m, v)], 1001
+    rec = mist.StepRecord(step=t - 1)
+    P, M, V, G = lists(mist, p, m, v, g)
+    mist.grad_norm(G, rec)
+    mist.adam_step(P, M, V, G, rec, lr=lr, betas=(0.9, 0.95), eps=1e-8, weight_decay=decay)
+    update = 0.9 * was[1] / (1 - 0.9 ** t) / ((0.95 * was[2] / (1 - 0.95 ** t)).sqrt() + 1e-8)
+    want = was[0] - lr * (update + decay * was[0])
+    error = float((p.double() - want).mean())
+    # the update's roundings: 24 2^-24 of lr * 1, were they all of one sign
+    assert abs(error) <= mean_bound(2.0 ** -30) + 24 * 2.0 ** -24 * lr, (error, lr * decay * float(was[0].mean()))
