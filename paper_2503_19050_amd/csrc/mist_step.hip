@@ -190,10 +190,25 @@ __global__ __launch_bounds__(kThreads) void k_clip(List g, List out, int64_t n_p
   if (const int i = vectors * kV + threadIdx.x; i < n) y[i] = (O)(coef * (float)x[i]);
 }
 
+// A beta in two fp32 terms, hi + lo.  One alone is off by up to 2^-25, which for a slow average (beta near 1) is a part
+// of 1 - beta: 0.1 % at 0.99999, all of it at 1 - 1e-8.  hi is below beta and lo above 0 (unless beta is 0), so
+// that an infinite average stays infinite.
+struct Decay {
+  float hi, lo;
+};
+
+Decay decay_of(double beta) {
+  if (!(beta > 0.0)) return Decay{0.0f, 0.0f};
+  float hi = (float)beta;
+  if ((double)hi >= beta) hi = std::nextafterf(hi, 0.0f);
+  return Decay{hi, (float)(beta - (double)hi)};
+}
+
 struct AdamArgs {
   List p, m, v, g, w;
   double beta1, beta2;
-  float b1, b2, one_b1, one_b2, lr, decay, eps;
+  Decay b1, b2;
+  float one_b1, one_b2, lr, decay, eps;
 };
 
 __device__ double power(double x, int64_t n) {
@@ -209,8 +224,8 @@ struct AdamScalars {
 
 __device__ __forceinline__ void adam_one(const AdamArgs& a, const AdamScalars& c, float g, float& p, float& m, float& v) {
   const float x = c.coef * g;
-  m = fmaf(a.b1, m, a.one_b1 * x);
-  v = fmaf(a.b2, v, a.one_b2 * x * x);
+  m = fmaf(a.b1.hi, m, fmaf(a.b1.lo, m, a.one_b1 * x));
+  v = fmaf(a.b2.hi, v, fmaf(a.b2.lo, v, a.one_b2 * x * x));
   // the decay joins the update: a factor 1 - lr * weight_decay next to 1 holds a small product in few bits or none
   p = fmaf(-a.lr, fmaf(a.decay, p, m * c.ibc1 / (sqrtf(v * c.ibc2) + a.eps)), p);
   asm("" : "+v"(p));  // the weights are the stored p rounded, not the sum rounded once to 16 bits
@@ -458,7 +473,7 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
   if (const mist_status st = on_device(g, "Adam step")) return st;
   if (!g->n_pieces) return MIST_OK;
   AdamArgs k{p->list, m->list, v->list, g->list, w ? w->list : List{}, a->beta1, a->beta2,
-             (float)a->beta1, (float)a->beta2, (float)(1.0 - a->beta1), (float)(1.0 - a->beta2),
+             decay_of(a->beta1), decay_of(a->beta2), (float)(1.0 - a->beta1), (float)(1.0 - a->beta2),
              (float)a->lr, (float)a->weight_decay, (float)a->eps};
   const dim3 grid = grid_of(g->n_pieces), block(kThreads);
   mist::with_types(g->type, w ? w->type : MIST_F32, [&](auto x, auto y) {

@@ -49,3 +49,41 @@ def test_small_weight_decay_is_kept(torch, lr, decay):
     error = float((p.double() - want).mean())
     # the update's roundings: 24 2^-24 of lr * 1, were they all of one sign
     assert abs(error) <= mean_bound(2.0 ** -30) + 24 * 2.0 ** -24 * lr, (error, lr * decay * float(was[0].mean()))
+
+
+@pytest.mark.parametrize("beta", [0.999, 0.99999, 1 - 1e-6])
+@pytest.mark.parametrize("which", ["m", "v"])
+def test_slow_averages_decay_at_their_rate(torch, which, beta):
+    """Averages in [1, 2) (one ulp of 2^-23) decay by 1 - beta, whatever beta rounds to in fp32."""
+    from paper_2503_19050_amd import mist
+    gen = torch.Generator("cuda").manual_seed(4)
+    p = torch.zeros(N, device="cuda")
+    m, v, g = (torch.empty(N, device="cuda").uniform_(1.0, 2.0, generator=gen) for _ in range(3))
+    span = 8 * 2.0 ** -23 / (1 - beta)   # terms that move the average by several ulps at the least, evenly
+    if which == "m":
+        g.uniform_(-max(1.0, span), max(1.0, span), generator=gen)
+    else:
+        g.uniform_(0.0, max(1.0, span), generator=gen).sqrt_()
+    old, x = (m if which == "m" else v).double(), g.double()
+    P, M, V, G = lists(mist, p, m, v, g)
+    rec = mist.StepRecord(step=99)
+    mist.grad_norm(G, rec)
+    mist.adam_step(P, M, V, G, rec, lr=0.0, betas=(beta, 0.9) if which == "m" else (0.9, beta))
+    term = x if which == "m" else x * x
+    want = beta * old + (1 - beta) * term
+    error = float(((m if which == "m" else v).double() - want).mean())
+    shared = 4 * 2.0 ** -24 * (1 - beta) * float(term.abs().max())
+    assert abs(error) <= mean_bound(2.0 ** -23) + shared, (error, beta)
+
+
+def test_infinite_averages_stay(torch):
+    """An average that has left fp32 (a gradient past 1.8e19) stays inf and gives no NaN."""
+    from paper_2503_19050_amd import mist
+    p, m, v, g = (torch.ones(1000, device="cuda") for _ in range(4))
+    v.fill_(float("inf"))
+    P, M, V, G = lists(mist, p, m, v, g)
+    rec = mist.StepRecord()
+    for betas in ((0.9, 0.999), (0.0, 0.5)):
+        mist.grad_norm(G, rec)
+        mist.adam_step(P, M, V, G, rec, lr=0.1, betas=betas)
+        assert v.isinf().all() and (p == 1).all() and m.isfinite().all()
