@@ -600,10 +600,10 @@ mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record
                            void* hip_stream);
 
 typedef struct mist_adam_desc {
-  double lr;             /* >= 0 */
+  double lr;             /* >= 0, finite in fp32 */
   double beta1, beta2;   /* in [0, 1) */
   double eps;            /* > 0, in the range of fp32 */
-  double weight_decay;   /* >= 0, decoupled */
+  double weight_decay;   /* >= 0, finite in fp32, decoupled */
 } mist_adam_desc;
 
 /* The Adam step with decoupled weight decay, tensor by tensor: with t = record->step,

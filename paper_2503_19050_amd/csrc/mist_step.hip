@@ -465,8 +465,8 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
     return lib_fail(MIST_E_INVALID, "Adam step: master weights, m and v must be MIST_F32");
   if (p == m || p == v || m == v || p == g || m == g || v == g || (w && (w == p || w == m || w == v || w == g)))
     return lib_fail(MIST_E_INVALID, "Adam step: the lists must be distinct");
-  if (!(a->lr >= 0.0 && std::isfinite(a->lr)) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0) ||
-      !((float)a->eps > 0.0f && std::isfinite((float)a->eps)) || !(a->weight_decay >= 0.0 && std::isfinite(a->weight_decay)))
+  if (!(a->lr >= 0.0 && std::isfinite((float)a->lr)) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0) ||
+      !((float)a->eps > 0.0f && std::isfinite((float)a->eps)) || !(a->weight_decay >= 0.0 && std::isfinite((float)a->weight_decay)))
     return lib_fail(MIST_E_INVALID, "Adam step: lr, beta, eps or weight_decay out of range");
   for (const mist_tensors* t : {p, m, v, w ? w : g})
     if (const mist_status st = like(g, t)) return st;

@@ -87,3 +87,16 @@ def test_infinite_averages_stay(torch):
         mist.grad_norm(G, rec)
         mist.adam_step(P, M, V, G, rec, lr=0.1, betas=betas)
         assert v.isinf().all() and (p == 1).all() and m.isfinite().all()
+
+
+def test_constants_past_fp32_are_refused(torch):
+    """lr and weight_decay that are finite in 64 bits and infinite in the kernel's 32."""
+    from paper_2503_19050_amd import mist
+    L = lists(mist, *(torch.ones(5, device="cuda") for _ in range(4)))
+    rec = mist.StepRecord()
+    mist.grad_norm(L[3], rec)
+    for bad in (dict(lr=1e39), dict(lr=0.1, weight_decay=1e39)):
+        with pytest.raises(mist.MistError) as e:
+            mist.adam_step(*L, rec, **bad)
+        assert e.value.status == -1
+    assert all((x.tensors[0] == 1).all() for x in L)
