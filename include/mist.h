@@ -567,7 +567,7 @@ typedef struct mist_step_record {
   int64_t step;    /* updates applied so far, this one included */
   float norm;      /* |grad_scale| * sqrt(total) (or |grad_scale| * total) */
   float coef;      /* factor of the stored gradients: grad_scale, times max_norm / norm where norm > max_norm */
-  int32_t applied; /* 1; 0 when the norm is inf or NaN: the step changes nothing */
+  int32_t applied; /* 1; 0 when the norm is inf (past fp32) or NaN: the step changes nothing */
   int32_t skipped; /* steps so far that changed nothing */
 } mist_step_record;
 

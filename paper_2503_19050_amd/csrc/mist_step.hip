@@ -92,8 +92,8 @@ __device__ double block_join(double x) {
 __device__ void finish(const mist_clip_desc& c, mist_step_record* r, double total) {
   const double scale = fabs((double)c.grad_scale);
   const double norm = scale * (c.kind == MIST_NORM_L2 ? sqrt(total) : total);
-  const bool fine = norm < HUGE_VAL;  // false for NaN
   r->norm = (float)norm;
+  const bool fine = r->norm < HUGE_VALF;  // of the norm as it is reported; false for NaN
   r->coef = fine ? (float)(c.grad_scale * (norm > c.max_norm ? c.max_norm / norm : 1.0)) : c.grad_scale;
   r->applied = fine;
   r->step += fine;

@@ -100,3 +100,25 @@ def test_constants_past_fp32_are_refused(torch):
             mist.adam_step(*L, rec, **bad)
         assert e.value.status == -1
     assert all((x.tensors[0] == 1).all() for x in L)
+
+
+def test_norm_past_fp32_changes_nothing(torch):
+    """The record's norm is fp32: where it is inf, so is the verdict, though the sum of squares in 64 bits is finite."""
+    from paper_2503_19050_amd import mist
+    for grads, scale in (([3e38, 3e38], 1.0), ([1e30, 0.0], 1e10)):
+        g = torch.tensor(grads, device="cuda")
+        rec = mist.StepRecord(step=2)
+        G = mist.TensorList([g])
+        mist.grad_norm(G, rec, max_norm=1.0, grad_scale=scale)
+        assert math.isfinite(float(rec.total)) and float(rec.norm) == math.inf
+        assert (int(rec.applied), int(rec.step), int(rec.skipped)) == (0, 2, 1)
+        out = torch.empty_like(g)
+        mist.grad_clip(G, rec, mist.TensorList([out]))
+        assert torch.equal(out, g)
+    g = torch.tensor([3e38, 0.0], device="cuda")   # the largest that has a norm: a subnormal factor
+    rec, out = mist.StepRecord(), torch.empty_like(g)
+    mist.grad_norm(mist.TensorList([g]), rec, max_norm=1.0)
+    mist.grad_clip(mist.TensorList([g]), rec, mist.TensorList([out]))
+    coef = 1.0 / float(g[0].double())
+    assert int(rec.applied) == 1 and abs(float(rec.coef) - coef) <= 2.0 ** -23 * coef + 2.0 ** -150
+    assert abs(float(out[0]) - 1.0) <= 2.0 ** -150 / coef + 2.0 ** -22 and float(out[1]) == 0.0
