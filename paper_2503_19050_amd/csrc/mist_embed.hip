@@ -148,11 +148,11 @@ template <bool POS>
 constexpr int kAhead = POS ? 16 : 4;
 
 template <class A, class W, int L, bool POS>
-__global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wave, bool by_slab, const void* __restrict__ ids,
+__global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wave, bool by_slab, int32_t group0, const void* __restrict__ ids,
                                                     const W* __restrict__ table, const W* __restrict__ pos, A* __restrict__ out) {
   const uint32_t slabs = (uint32_t)a.slabs, wave = (uint32_t)wave_index();
   const int32_t slab = (int32_t)(by_slab ? blockIdx.x % slabs : wave % slabs);
-  const int64_t first = (int64_t)(by_slab ? blockIdx.x / slabs * kWaves + wave % kWaves : wave / slabs) * per_wave;
+  const int64_t first = (int64_t)(group0 + (by_slab ? blockIdx.x / slabs * kWaves + wave % kWaves : wave / slabs)) * per_wave;
   if (first >= a.n) return;
   const int32_t count = (int32_t)(a.n - first < per_wave ? a.n - first : per_wave);
   const int lane = threadIdx.x % 64;
@@ -807,15 +807,20 @@ mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const 
   const int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 16384, 1, pos ? kAhead<true> : kAhead<false>);
   const bool by_slab = !pos && a.slabs > 1 && (a.slabs % 8 == 0 || 8 % a.slabs == 0) &&
                        std::min<int64_t>(a.n, a.rows) * a.hidden * mist::type_bytes(d->table_type) <= kCache;
-  const int64_t groups = (a.n + per_wave - 1) / per_wave, waves = (by_slab ? (groups + kWaves - 1) / kWaves * kWaves : groups) * a.slabs;
-  if (waves > (int64_t)kWaves << 23) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
+  const int64_t groups = (a.n + per_wave - 1) / per_wave;
+  // A launch's grid stays below 2^32 threads; whole blocks of groups, so that no group is in two launches.
+  const int64_t most = ((int64_t)1 << 23) / a.slabs * kWaves;
   mist::with_types(d->act_type, d->table_type, [&](auto x, auto w) {
     using A = typename decltype(x)::type;
     using W = typename decltype(w)::type;
     with_layout<A, W>(d->hidden, [&](auto layout) {
       const auto kernel = pos ? k_embed<A, W, layout.value, true> : k_embed<A, W, layout.value, false>;
-      hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
-                         (int32_t)per_wave, by_slab, ids, (const W*)table, (const W*)pos, (A*)out);
+      for (int64_t group0 = 0; group0 < groups; group0 += most) {
+        const int64_t count = std::min(most, groups - group0);
+        const int64_t waves = (by_slab ? (count + kWaves - 1) / kWaves * kWaves : count) * a.slabs;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, (hipStream_t)stream, a,
+                           (int32_t)per_wave, by_slab, (int32_t)group0, ids, (const W*)table, (const W*)pos, (A*)out);
+      }
     });
   });
   const hipError_t e = hipGetLastError();
