@@ -42,6 +42,27 @@ LOOKUPS = [(2, 20000, 500, 8), (3, 5500, 1000, 1032), (5, 1101, 700, 4104), (1, 
            (3, 100003, 50, 7), (17, 1901, 2000, 4097), (64, 4099, 300, 24), (16384, 17, 99, 40), (300001, 1, 99, 8)]
 
 
+@pytest.mark.parametrize("act, weight", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "f16")])
+@pytest.mark.parametrize("shape", LOOKUPS, ids=str)
+def test_lookup_with_positions_of_many_tokens(torch, shape, act, weight):
+    from paper_2503_19050_amd import mist
+    batch, seq, vocab, hidden = shape
+    say("lookup", shape, act, weight)
+    T, gen = types(torch), torch.Generator("cuda").manual_seed(batch + seq)
+    ids = torch.randint(-3, vocab + 3, (batch, seq), device="cuda", generator=gen, dtype=torch.int32 if seq % 2 else torch.int64)
+    table = torch.empty(vocab, hidden, device="cuda").normal_(generator=gen).to(T[weight])
+    pos = torch.empty(seq, hidden, device="cuda").normal_(generator=gen).to(T[weight])
+    out = torch.full((batch, seq, hidden), float("nan"), device="cuda", dtype=T[act])
+    mist.embed(ids, table, scale=3.7, pos=pos, out=out)
+    inside = (ids >= 0) & (ids < vocab)
+    scale = float(torch.tensor(3.7, dtype=torch.float32))
+    at = max(1, (1 << 25) // (seq * hidden))      # sequences at a time
+    for b in range(0, batch, at):
+        x = torch.where(inside[b:b + at, :, None], table.double()[ids[b:b + at].clamp(0, vocab - 1).long()] * scale, 0.0)
+        p = pos.double()[None]
+        within(out[b:b + at], x + p, UNIT[act] * (x + p).abs() + 2.0 ** -22 * (x.abs() + p.abs()) + TINY[act], "lookup")
+
+
 def test_lookup_of_more_tokens_than_a_launch_takes(torch):
     """2^25 waves of four tokens a launch: past 2^27 tokens there are two."""
     from paper_2503_19050_amd import mist
@@ -68,3 +89,41 @@ def views(torch, sizes, dtype, std, shift, gen):
 
 def untouched(flat, part, shift):
     assert (flat[:shift] == 77.0).all() and (flat[shift + part.numel():] == 77.0).all()
+
+
+@pytest.mark.parametrize("g, w, shift", [("bf16", "bf16", 0), ("f32", "bf16", 1), ("f16", "f32", 3)])
+@pytest.mark.parametrize("sizes", LISTS, ids=str)
+def test_lists_of_more_pieces_than_blocks(torch, sizes, g, w, shift):
+    """Norm, clipping and step; the norm's blocks take two pieces and more."""
+    from paper_2503_19050_amd import mist
+    say("list", sizes, g, w, shift)
+    S, T, gen = LISTS[sizes], types(torch), torch.Generator("cuda").manual_seed(shift)
+    gf, grad, grads = views(torch, S, T[g], 0.01, shift, gen)
+    state = [views(torch, S, torch.float32, 0.01, shift, gen) for _ in range(3)]
+    state[2][1].square_()
+    wf, weight, weights = views(torch, S, T[w], 1.0, shift, gen)
+    G, W = mist.TensorList(grads), mist.TensorList(weights)
+    x = grad.double()
+    total = float((x * x).sum())
+    rec = mist.StepRecord(step=10)
+    mist.grad_norm(G, rec, kind="max")
+    assert float(rec.total) == float(x.abs().max())
+    mist.grad_norm(G, rec, max_norm=1.0)
+    assert abs(float(rec.total) - total) <= len(x) * 2.0 ** -51 * total   # both sums are rounded
+    norm = math.sqrt(total)
+    coef = 1.0 / norm if norm > 1.0 else 1.0
+    mist.grad_clip(G, rec, W)
+    within(weight, coef * x, (UNIT[w] + 2.0 ** -22) * (coef * x).abs() + TINY[w], "clip")
+    was = [s[1].double() for s in state]
+    mist.adam_step(*(mist.TensorList(s[2]) for s in state), G, rec, lr=3e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, weights=W)
+    gx, t = coef * x, 12
+    size = 0.9 * was[1].abs() + 0.1 * gx.abs()
+    m, v = 0.9 * was[1] + (1 - 0.9) * gx, 0.95 * was[2] + (1 - 0.95) * gx * gx
+    down = (v / (1 - 0.95 ** t)).sqrt() + 1e-8
+    p = was[0] - 3e-3 * (m / (1 - 0.9 ** t) / down + 0.1 * was[0])
+    within(state[1][1], m, 6 * E24 * size + TINY["f32"], "m")
+    within(state[2][1], v, 8 * E24 * v + TINY["f32"], "v")
+    within(state[0][1], p, 4 * E24 * was[0].abs() + 3e-3 * 24 * E24 * size / (1 - 0.9 ** t) / down + TINY["f32"], "p")
+    assert torch.equal(weight, state[0][1].to(T[w]))
+    for flat, part in [(gf, grad), (wf, weight)] + [(s[0], s[1]) for s in state]:
+        untouched(flat, part, shift)
