@@ -849,8 +849,7 @@ mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const
       !aligned(dtable, mist::type_bytes(d->table_type)) || !aligned(dpos, mist::type_bytes(d->table_type)) ||
       !aligned(workspace, 256))
     return lib_fail(MIST_E_INVALID, "embedding: a buffer is not aligned to its elements, or the workspace to 256");
-  const int64_t join_blocks = std::min<int64_t>(s.chunks / 2, kJoinRuns) * a.slabs;
-  if (join_blocks > 1 << 23 || (int64_t)a.slabs * kSlab > INT32_MAX) return lib_fail(MIST_E_INVALID, "embedding: too many values for one call");
+  const int64_t join_blocks = std::min<int64_t>(s.chunks / 2, kJoinRuns) * a.slabs;  // at most 2^7 2^15
   const hipStream_t st = (hipStream_t)stream;
   char* ws = (char*)workspace;
   const RowArgs r{(const Entry*)(ws + s.order), (int32_t*)(ws + s.longs), (float*)(ws + s.part), s.chunk, (int32_t)s.chunks, accumulate, s.chunks * a.slabs};
