@@ -195,6 +195,10 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
 template <int L>
 constexpr int kPosAhead = L == kOdd ? 2 : 8;  // one by one, eight take more registers than a block of 1024 threads has
 
+// The batch is summed in parts of 64, the rows' largest piece, so that a term meets 64 + batch / 64 roundings and
+// not batch: one sum over 2^20 sequences lost 0.7 % of terms whose last bits it did not hold.
+constexpr int64_t kPosPart = 64;
+
 template <class A, class W>
 struct PosArgs {
   const A* grad;
@@ -210,7 +214,7 @@ __device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32
   for (; item < p.end; item += (int64_t)blocks * waves) {
     const int64_t s = item / a.slabs;
     const Cols<L> col((int32_t)(item % a.slabs), a.hidden);
-    Float8 acc = {};
+    Float8 acc = {}, done = {};
     for (int64_t b0 = 0; b0 < a.batch; b0 += kPosAhead<L>) {
       Lane8<A, L> x[kPosAhead<L>];
 #pragma unroll
@@ -219,7 +223,12 @@ __device__ void sum_positions(const EmbedArgs& a, const PosArgs<A, W>& p, uint32
 #pragma unroll
       for (int k = 0; k < kPosAhead<L>; ++k)
         if (b0 + k < a.batch) acc += x[k].get();
+      if ((b0 + kPosAhead<L>) % kPosPart == 0) {
+        done += acc;
+        acc = Float8{};
+      }
     }
+    acc += done;
     W* d = p.dpos + s * a.pos_stride;
     if (p.accumulate) {
       Lane8<W, L> old;

@@ -76,6 +76,26 @@ def test_lookup_of_more_tokens_than_a_launch_takes(torch):
         assert torch.equal(out[0, lo:lo + (1 << 26)], want)
 
 
+@pytest.mark.parametrize("act, weight", [("bf16", "f32"), ("f32", "f32"), ("f16", "bf16")])
+@pytest.mark.parametrize("batch, seq, hidden", [(4097, 3, 24), (131072, 1, 8), (1 << 20, 1, 8), (20000, 2, 7), (1000, 1, 8),
+                                                (1000, 1, 520), (9001, 16, 12)])
+def test_positions_of_a_large_batch(torch, batch, seq, hidden, act, weight):
+    """Terms of one sign that a long sum's last place does not hold: sums of at most 64 terms are added up, so that
+    the error is that of 64 + batch / 64 roundings, not of batch."""
+    from paper_2503_19050_amd import mist
+    say("positions", batch, seq, hidden, act, weight)
+    T, gen = types(torch), torch.Generator("cuda").manual_seed(batch)
+    grad = torch.empty(batch, seq, hidden, device="cuda", dtype=T[act])
+    grad[:] = (1.00276 if act == "f32" else 1.0 + 2.0 ** -7) * 2.0 ** (torch.arange(hidden, device="cuda") % 3 - 1)
+    ids = torch.randint(0, 50, (batch, seq), device="cuda", generator=gen)
+    want = grad.double().sum(0)
+    for old in (0.0, 3.0):
+        dtable, dpos = torch.zeros(50, hidden, device="cuda", dtype=T[weight]), torch.full((seq, hidden), old, device="cuda", dtype=T[weight])
+        mist.embed_grad(ids, grad, dtable, dpos=dpos, accumulate=old > 0)
+        x = want + old
+        within(dpos, x, UNIT[weight] * x + (64 + batch / 64 + 3) * E24 * x + TINY[weight], "dpos")
+
+
 LISTS = {"one": [9000001], "two": [12000007, 8000009], "many": [5000 + 7 * k % 9001 for k in range(2600)],
          "mixed": [11000003] + [1 + k % 5000 for k in range(3000)]}
 
