@@ -739,6 +739,7 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
     torch = _torch()
     L = _lib or load()
+    _need(table.is_cuda, "embedding: ids, table, positions and activations must be on one GPU")
     handle, other = _stream_of(torch, stream, table.device)
     if out is None:
         _need(table.dim() == 2, "embedding: the table must be [rows, hidden]")
@@ -832,6 +833,7 @@ class StepRecord:
 
     def __init__(self, step: int = 0, device=None):
         torch = _torch()
+        _need(device is None or torch.device(device).type == "cuda", "step record: must be on a GPU")
         self.data = torch.zeros(8 + NORM_WORKSPACE // 8, dtype=torch.float64, device="cuda" if device is None else device)
         self.device = self.data.device
         self.ptr = self.data.data_ptr()

@@ -1,0 +1,25 @@
+"""The binding's own refusals for the training-step operators, without a GPU: MistError, before the library is called."""
+import types
+
+import pytest
+
+from paper_2503_19050_amd import mist
+
+
+@pytest.fixture(scope="module")
+def torch():
+    return mist._torch()
+
+
+def refused(call):
+    with pytest.raises(mist.MistError) as e:
+        call()
+    assert e.value.status == mist.E_INVALID and str(e.value)
+
+
+def test_host_tensors_are_refused(torch):
+    ids, table, grad = torch.zeros(2, 3, dtype=torch.int64), torch.zeros(5, 8), torch.zeros(2, 3, 8)
+    for call in (lambda: mist.embed(ids, table), lambda: mist.embed(ids, table, out=grad), lambda: mist.embed(ids, table, pos=grad[0]),
+                 lambda: mist.embed_grad(ids, grad, table), lambda: mist.TensorList([table]),
+                 lambda: mist.StepRecord(device="cpu")):
+        refused(call)
