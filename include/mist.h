@@ -564,7 +564,7 @@ mist_status mist_tensors_destroy(mist_tensors* T);
  * at a time. */
 typedef struct mist_step_record {
   double total;    /* sum of squares (or largest magnitude) of the gradients as stored */
-  int64_t step;    /* updates applied so far, this one included */
+  int64_t step;    /* updates applied so far, this one included; set to 0 or more at first */
   float norm;      /* |grad_scale| * sqrt(total) (or |grad_scale| * total) */
   float coef;      /* factor of the stored gradients: grad_scale, times max_norm / norm where norm > max_norm */
   int32_t applied; /* 1; 0 when the norm is inf (past fp32) or NaN: the step changes nothing */

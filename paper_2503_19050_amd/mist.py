@@ -833,6 +833,7 @@ class StepRecord:
 
     def __init__(self, step: int = 0, device=None):
         torch = _torch()
+        _need(step >= 0, "step record: step must be >= 0")
         _need(device is None or torch.device(device).type == "cuda", "step record: must be on a GPU")
         self.data = torch.zeros(8 + NORM_WORKSPACE // 8, dtype=torch.float64, device="cuda" if device is None else device)
         self.device = self.data.device

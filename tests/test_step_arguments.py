@@ -23,3 +23,8 @@ def test_host_tensors_are_refused(torch):
                  lambda: mist.embed_grad(ids, grad, table), lambda: mist.TensorList([table]),
                  lambda: mist.StepRecord(device="cpu")):
         refused(call)
+
+
+def test_a_step_count_below_zero_is_refused(torch):
+    """Its bias correction would divide by 1 - beta^0 or less."""
+    refused(lambda: mist.StepRecord(step=-1))
