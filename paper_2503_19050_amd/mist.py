@@ -681,6 +681,7 @@ def _stream_of(torch, stream, device):
         return torch._C._cuda_getCurrentRawStream(device.index), None
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    _need(stream.device == device, "the stream is of another device than the tensors")
     return stream.cuda_stream, stream
 
 

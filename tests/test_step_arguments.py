@@ -28,3 +28,10 @@ def test_host_tensors_are_refused(torch):
 def test_a_step_count_below_zero_is_refused(torch):
     """Its bias correction would divide by 1 - beta^0 or less."""
     refused(lambda: mist.StepRecord(step=-1))
+
+
+def test_a_stream_of_another_device_is_refused(torch):
+    here, there = torch.device("cuda", 0), torch.device("cuda", 1)
+    stream = types.SimpleNamespace(device=there, cuda_stream=64)
+    refused(lambda: mist._stream_of(torch, stream, here))
+    assert mist._stream_of(torch, stream, there) == (64, stream)
