@@ -651,6 +651,8 @@ class Corun:
 
 
 # -- operators of a training step's two ends ---------------------------------------------------
+# They are outside autograd: a gradient is a call of its own, and tensors written in place do not count as
+# modified (their version counters stay).
 E_INVALID = -1
 _NORMS = {"l2": 0, "max": 1}
 NORM_WORKSPACE = 16384
@@ -740,6 +742,8 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
     torch = _torch()
     L = _lib or load()
+    _need(not (torch.is_grad_enabled() and (table.requires_grad or pos is not None and pos.requires_grad)),
+          "embedding: records no gradient; call it under torch.no_grad() and embed_grad for the gradients")
     _need(table.is_cuda, "embedding: ids, table, positions and activations must be on one GPU")
     handle, other = _stream_of(torch, stream, table.device)
     if out is None:

@@ -35,3 +35,13 @@ def test_a_stream_of_another_device_is_refused(torch):
     stream = types.SimpleNamespace(device=there, cuda_stream=64)
     refused(lambda: mist._stream_of(torch, stream, here))
     assert mist._stream_of(torch, stream, there) == (64, stream)
+
+
+def test_a_lookup_that_autograd_would_lose_is_refused(torch):
+    """The result has no graph: a table or positions that require a gradient are taken where none is recorded."""
+    ids, table, pos = torch.zeros(2, 3, dtype=torch.int64), torch.zeros(5, 8, requires_grad=True), torch.zeros(3, 8, requires_grad=True)
+    for call in (lambda: mist.embed(ids, table), lambda: mist.embed(ids, table.detach(), pos=pos)):
+        with pytest.raises(mist.MistError, match="no_grad"):
+            call()
+        with torch.no_grad(), pytest.raises(mist.MistError, match="on one GPU"):  # the next check
+            call()
