@@ -553,7 +553,9 @@ typedef struct mist_tensors mist_tensors;
 mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, int64_t n, int32_t type,
                                 const mist_allocator* alloc, mist_tensors** out);
 
-/* Waits for the device's work and frees the tables.  NULL is accepted. */
+/* Waits for the device's work and frees the tables.  NULL is accepted.  Neither this call nor the last belongs in a
+ * graph's capture, and a graph needs the lists that it was captured with.  Errors: MIST_E_DEVICE (the work cannot
+ * be waited for, e.g. during a capture: nothing is freed, and the call can be made again). */
 mist_status mist_tensors_destroy(mist_tensors* T);
 
 #define MIST_NORM_L2 0

@@ -285,18 +285,30 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, int64_t n_pieces,
   }
 }
 
+// Frees the tables and the list, on its device.  Nothing uses them any more.
 void release(mist_tensors* T) {
   if (!T) return;
   int cur = 0;
   const bool known = hipGetDevice(&cur) == hipSuccess;
   if (known && cur != T->device) (void)hipSetDevice(T->device);
   if (T->block) {
-    (void)hipDeviceSynchronize();
     if (T->own_alloc) (void)hipFree(T->block);
     else T->alloc.free(T->block, T->alloc.ctx);
   }
   if (known && cur != T->device) (void)hipSetDevice(cur);
   delete T;
+}
+
+// Waits for the work of the list's device.
+hipError_t wait_for(const mist_tensors* T) {
+  int cur = 0;
+  hipError_t e = hipGetDevice(&cur);
+  if (e == hipSuccess && cur != T->device) e = hipSetDevice(T->device);
+  if (e != hipSuccess) return e;
+  e = hipDeviceSynchronize();
+  if (e != hipSuccess) (void)hipGetLastError();
+  if (cur != T->device) (void)hipSetDevice(cur);
+  return e;
 }
 
 mist_status on_device(const mist_tensors* T, const char* what) {
@@ -397,6 +409,10 @@ mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, i
 }
 
 mist_status mist_tensors_destroy(mist_tensors* T) {
+  if (T && T->block) {
+    const hipError_t e = wait_for(T);
+    if (e != hipSuccess) return hip_failed(e, "tensor list: its work cannot be waited for");
+  }
   release(T);
   return MIST_OK;
 }

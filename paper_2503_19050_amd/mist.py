@@ -742,9 +742,10 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
     torch = _torch()
     L = _lib or load()
-    _need(not (torch.is_grad_enabled() and (table.requires_grad or pos is not None and pos.requires_grad)),
-          "embedding: records no gradient; call it under torch.no_grad() and embed_grad for the gradients")
-    _need(table.is_cuda, "embedding: ids, table, positions and activations must be on one GPU")
+    if (table.requires_grad or pos is not None and pos.requires_grad) and torch.is_grad_enabled():
+        _need(False, "embedding: records no gradient; call it under torch.no_grad() and embed_grad for the gradients")
+    if not table.is_cuda:
+        _need(False, "embedding: ids, table, positions and activations must be on one GPU")
     handle, other = _stream_of(torch, stream, table.device)
     if out is None:
         _need(table.dim() == 2, "embedding: the table must be [rows, hidden]")
@@ -781,9 +782,24 @@ def embed_grad(ids, grad, dtable, *, scale: float = 1.0, dpos=None, vocab_begin:
     return dtable
 
 
+_closed = []  # lists that wait to be freed: (library, handle, callbacks)
+
+
+def _free_closed(torch) -> None:
+    """Frees closed lists, which waits for the device: not while a graph is captured, whose capture that would end."""
+    if torch.cuda.is_current_stream_capturing():
+        return
+    for _ in range(len(_closed)):
+        entry = _closed.pop()
+        if entry[0].mist_tensors_destroy(entry[1]) != 0:
+            _closed.insert(0, entry)
+
+
 class TensorList:
     """Tensors of one type on the current GPU as one list (mist_tensors_create), e.g. a stage's gradients.  They
-    must be contiguous and stay where they are; the list keeps them alive."""
+    must be contiguous and stay where they are; the list keeps them alive.  Making a list copies its tables to the
+    device and waits, closing it waits for the device: lists are for tensors that stay over many steps.  No list is
+    made while a graph is captured, one that is closed then is freed later; a graph needs its lists as long as it is replayed."""
 
     def __init__(self, tensors, allocator: str | None = "torch"):
         self.h = None
@@ -804,6 +820,8 @@ class TensorList:
         sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
+            _need(not torch.cuda.is_current_stream_capturing(), "tensor list: cannot be made while a graph is captured")
+            _free_closed(torch)
             self._alloc = None
             if allocator == "torch":
                 self._alloc, self._cb = _torch_allocator([])
@@ -816,8 +834,9 @@ class TensorList:
 
     def close(self) -> None:
         if getattr(self, "h", None):
-            self.L.mist_tensors_destroy(self.h)
-            self.h = None
+            h, self.h = self.h, None
+            _closed.append((self.L, h, getattr(self, "_cb", None)))
+            _free_closed(_torch())
 
     def __del__(self):
         try:
