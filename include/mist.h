@@ -547,7 +547,8 @@ mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const
 typedef struct mist_tensors mist_tensors;
 
 /* Host ptrs[0..n-1] are device addresses (each aligned to its element) of sizes[0..n-1]
- * contiguous elements of the given type; a tensor may be empty, then its address is not used.  alloc as in
+ * contiguous elements of the given type; a tensor may be empty, then its address is not used.  A list whose tensors
+ * overlap (one parameter listed twice) can be read, each time it occurs, but not written.  alloc as in
  * mist_space_create (NULL: hipMalloc/hipFree).  Errors: MIST_E_INVALID, MIST_E_NOMEM,
  * MIST_E_DEVICE. */
 mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, int64_t n, int32_t type,
@@ -595,8 +596,8 @@ mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32
  * part of the gradients add up (or take the largest of) their totals first.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_grad_finish(const mist_clip_desc* c, mist_step_record* record, void* hip_stream);
 
-/* out = coef * g, tensor by tensor (the same count and sizes; of any type; out may be g).  With
- * applied = 0 the values are carried over as they are, rounded to out's type.  Errors:
+/* out = coef * g, tensor by tensor (the same count and sizes; of any type; out may be g, otherwise they share no
+ * memory).  With applied = 0 the values are carried over as they are, rounded to out's type.  Errors:
  * MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record, const mist_tensors* out,
                            void* hip_stream);
@@ -613,8 +614,8 @@ typedef struct mist_adam_desc {
  *     p = p - lr * ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay * p);
  *     w = p rounded to w's type.
  * p, m and v are MIST_F32 (bytes_opt = 12), g is of any type, w may be NULL (no 16-bit weights); all
- * with g's count and sizes.  |g'| past 1.8e19 leaves fp32 when squared (v = inf): such gradients are to be
- * clipped.  One step may be made in several calls, e.g. one per layer.  With applied = 0 (gradients
+ * with g's count and sizes, and none shares memory with another.  |g'| past 1.8e19 leaves fp32 when squared
+ * (v = inf): such gradients are to be clipped.  One step may be made in several calls, e.g. one per layer.  With applied = 0 (gradients
  * with inf or NaN) it changes nothing.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const mist_tensors* v, const mist_tensors* g,
                            const mist_tensors* w, const mist_step_record* record, const mist_adam_desc* a,

@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "mist_ops.h"
@@ -49,6 +50,7 @@ struct mist_tensors {
   int32_t type = 0;
   std::vector<int64_t> size;
   int64_t n_pieces = 0;
+  bool overlaps = false;  // a value is in two of the tensors
   List list{};
   void* block = nullptr;  // the device tables
   mist_allocator alloc{};
@@ -285,6 +287,17 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a, int64_t n_pieces,
   }
 }
 
+bool tensors_overlap(const void* const* ptrs, const int64_t* sizes, int64_t n, int64_t bytes) {
+  std::vector<std::pair<uintptr_t, int64_t>> at;
+  at.reserve((size_t)n);
+  for (int64_t i = 0; i < n; ++i)
+    if (sizes[i]) at.emplace_back(reinterpret_cast<uintptr_t>(ptrs[i]), sizes[i] * bytes);
+  std::sort(at.begin(), at.end());
+  for (size_t i = 1; i < at.size(); ++i)
+    if (at[i].first - at[i - 1].first < (uint64_t)at[i - 1].second) return true;
+  return false;
+}
+
 // Frees the tables and the list, on its device.  Nothing uses them any more.
 void release(mist_tensors* T) {
   if (!T) return;
@@ -324,6 +337,11 @@ mist_status like(const mist_tensors* a, const mist_tensors* b) {
   if (a->device != b->device) return lib_fail(MIST_E_INVALID, "tensor lists are on different devices");
   if (a->size != b->size) return lib_fail(MIST_E_INVALID, "tensor lists differ in count or sizes");
   return MIST_OK;
+}
+
+// A list that is written: two blocks would take a value that occurs twice, in any order.
+mist_status written(const mist_tensors* T) {
+  return T && T->overlaps ? lib_fail(MIST_E_INVALID, "tensor list: tensors that are written overlap") : MIST_OK;
 }
 
 bool clip_ok(const mist_clip_desc* c) {
@@ -366,6 +384,7 @@ mist_status mist_tensors_create(const void* const* ptrs, const int64_t* sizes, i
     T->type = type;
     T->size.assign(sizes, sizes + n);
     T->n_pieces = pieces;
+    T->overlaps = tensors_overlap(ptrs, sizes, n, bytes);
     hipError_t e = hipGetDevice(&T->device);
     if (e == hipSuccess && pieces) {
       // one block: addresses, sizes, pieces (8 bytes each)
@@ -461,6 +480,7 @@ mist_status mist_grad_clip(const mist_tensors* g, const mist_step_record* record
   if (!g || !record || !out) return lib_fail(MIST_E_INVALID, "clipping: null argument");
   if (!aligned8(record)) return lib_fail(MIST_E_INVALID, "clipping: record not aligned to 8");
   if (const mist_status st = like(g, out)) return st;
+  if (const mist_status st = written(out)) return st;
   if (const mist_status st = on_device(g, "clipping")) return st;
   if (!g->n_pieces) return MIST_OK;
   mist::with_types(g->type, out->type, [&](auto x, auto y) {
@@ -486,6 +506,8 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
     return lib_fail(MIST_E_INVALID, "Adam step: lr, beta, eps or weight_decay out of range");
   for (const mist_tensors* t : {p, m, v, w ? w : g})
     if (const mist_status st = like(g, t)) return st;
+  for (const mist_tensors* t : {p, m, v, w})
+    if (const mist_status st = written(t)) return st;
   if (const mist_status st = on_device(g, "Adam step")) return st;
   if (!g->n_pieces) return MIST_OK;
   AdamArgs k{p->list, m->list, v->list, g->list, w ? w->list : List{}, a->beta1, a->beta2,

@@ -797,7 +797,8 @@ def _free_closed(torch) -> None:
 
 class TensorList:
     """Tensors of one type on the current GPU as one list (mist_tensors_create), e.g. a stage's gradients.  They
-    must be contiguous and stay where they are; the list keeps them alive.  Making a list copies its tables to the
+    must be contiguous and stay where they are; the list keeps them alive.  One that holds a value twice (tied weights listed
+    under both names) can be read but not written.  Making a list copies its tables to the
     device and waits, closing it waits for the device: lists are for tensors that stay over many steps.  No list is
     made while a graph is captured, one that is closed then is freed later; a graph needs its lists as long as it is replayed."""
 

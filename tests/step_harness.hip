@@ -149,12 +149,14 @@ float g_values[1 << 12];
 mist_step_record g_record;
 double g_workspace[MIST_NORM_WORKSPACE / 8];
 const mist_clip_desc kClip{MIST_NORM_L2, 1.0f, 1.0};
+const mist_adam_desc kAdam{0.1, 0.9, 0.99, 1e-8, 0.0};
 
 mist_tensors* list(std::vector<const void*> at, std::vector<int64_t> sizes, int32_t type = MIST_F32, const mist_allocator* alloc = &kAlloc) {
   mist_tensors* T = nullptr;
   check(mist_tensors_create(at.data(), sizes.data(), (int64_t)at.size(), type, alloc, &T) == MIST_OK && T, "a list is refused");
   return T;
 }
+mist_tensors* part(int64_t first, int64_t n) { return list({g_values + first}, {n}); }
 
 // Tables hold what was given, are freed on the list's device after its work, and the current device stays.
 void lists() {
@@ -213,6 +215,33 @@ void failing_wait() {
   }
 }
 
+// Lists that are written hold no value twice; lists that are read may.
+void overlaps() {
+  mist_tensors *a = part(0, 100), *b = part(100, 100), *c = part(200, 100), *d = part(300, 100), *e = part(400, 100);
+  auto clip = [&](mist_tensors* g, mist_tensors* out) { return mist_grad_clip(g, &g_record, out, nullptr); };
+  auto adam = [&](mist_tensors* p, mist_tensors* m, mist_tensors* v, mist_tensors* g, mist_tensors* w) {
+    return mist_adam_step(p, m, v, g, w, &g_record, &kAdam, nullptr);
+  };
+  check(clip(a, a) == MIST_OK && clip(a, b) == MIST_OK && adam(a, b, c, d, e) == MIST_OK, "lists apart");
+  for (auto* T : {a, b, c, d, e}) mist_tensors_destroy(T);
+  const std::vector<int64_t> sizes{100, 7, 0, 100};
+  auto four = [&](int64_t first, int64_t second, int64_t fourth) {
+    return list({g_values + first, g_values + second, nullptr, g_values + fourth}, sizes);
+  };
+  mist_tensors *p = four(700, 800, 807), *m = four(1000, 1200, 1100), *v = four(1607, 1500, 1507), *g = four(2000, 2300, 2400), *w = four(2707, 2700, 2807);
+  check(clip(g, g) == MIST_OK && clip(g, p) == MIST_OK && adam(p, m, v, g, w) == MIST_OK && adam(p, m, v, g, nullptr) == MIST_OK, "tensors that touch");
+  for (mist_tensors* bad : {four(3000, 3200, 3000), four(3000, 3099, 3200), four(3000, 3093, 3200), four(3106, 3100, 3300), four(3050, 3010, 3000)}) {
+    const size_t launches = g_launches.size();
+    check(clip(bad, bad) == MIST_E_INVALID && clip(g, bad) == MIST_E_INVALID, "clipping into values that occur twice");
+    check(adam(bad, m, v, g, w) == MIST_E_INVALID && adam(p, bad, v, g, w) == MIST_E_INVALID && adam(p, m, bad, g, nullptr) == MIST_E_INVALID &&
+              adam(p, m, v, g, bad) == MIST_E_INVALID, "a step of values that occur twice");
+    check(g_launches.size() == launches, "a refused call's launches");
+    check(clip(bad, g) == MIST_OK && adam(p, m, v, bad, w) == MIST_OK, "values that are read twice");
+    mist_tensors_destroy(bad);
+  }
+  for (auto* T : {p, m, v, g, w}) mist_tensors_destroy(T);
+}
+
 // Long lists: every piece has a block.
 void grids() {
   for (const int64_t n : {(int64_t)1, kChunk, kChunk + 1, kChunk * 2047, kChunk * (kGridX / 2) + 5, kChunk * kGridX - 1, kChunk * kGridX + 1}) {
@@ -263,7 +292,7 @@ int main(int argc, char** argv) {
   const struct {
     const char* name;
     void (*run)();
-  } all[] = {{"lists", lists}, {"failures", failures}, {"failing_wait", failing_wait}, {"grids", grids}, {"lookups", lookups}};
+  } all[] = {{"lists", lists}, {"failures", failures}, {"failing_wait", failing_wait}, {"overlaps", overlaps}, {"grids", grids}, {"lookups", lookups}};
   for (const auto& s : all)
     if (argc == 2 && !std::strcmp(argv[1], s.name)) {
       s.run();
