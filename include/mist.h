@@ -523,7 +523,8 @@ typedef struct mist_embed_desc {
 } mist_embed_desc;
 
 /* out[b, s, :] = scale * table[id - vocab_begin, :] + pos[s, :] (the first term 0 for an id
- * outside the shard; pos may be NULL: no positions).  The positions of out must not overlap.
+ * outside the shard; pos may be NULL: no positions).  Ranks that hold shards of the table add up their outputs: one of
+ * them alone passes pos.  The positions of out must not overlap, nor out an input.
  * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const void* table, const void* pos, void* out,
                                void* hip_stream);
@@ -535,9 +536,9 @@ mist_status mist_embed_workspace(const mist_embed_desc* d, size_t* bytes);
  * memory, stride 0): dtable[v, :] = scale * sum of grad[b, s, :] over the tokens of row v, and
  * dpos[s, :] = sum over b of grad[b, s, :] (dpos may be NULL).  Sums are in fp32 in an order that
  * depends on the ids and sizes alone.  accumulate = 0 writes every row, zeros where no token is; accumulate
- * = 1 adds to what dtable and dpos hold and touches only the rows of the tokens.  workspace: at
- * least mist_embed_workspace bytes, aligned to 256.  Errors: MIST_E_INVALID, MIST_E_RANGE
- * (workspace too small), MIST_E_DEVICE. */
+ * = 1 adds to what dtable and dpos hold and touches only the rows of the tokens.  dtable, dpos and grad
+ * share no memory.  workspace: at least mist_embed_workspace bytes, aligned to 256.  Errors: MIST_E_INVALID,
+ * MIST_E_RANGE (workspace too small), MIST_E_DEVICE. */
 mist_status mist_embed_backward(const mist_embed_desc* d, const void* ids, const void* grad, void* dtable, void* dpos,
                                 int32_t accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
 
@@ -593,7 +594,10 @@ mist_status mist_grad_norm(const mist_tensors* g, const mist_clip_desc* c, int32
                            mist_step_record* record, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Forms norm, coef and applied from record->total and counts the step.  Ranks that each hold a
- * part of the gradients add up (or take the largest of) their totals first.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+ * part of the gradients add up (or take the largest of) their totals first, each tensor counted once: those that every
+ * rank of a group holds (norm weights and positions under tensor parallelism) are left out on all ranks but one.  A total that
+ * the caller sets to 0 gives coef = grad_scale: a step without a pass over the gradients, clipping and the check for
+ * inf and NaN.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_grad_finish(const mist_clip_desc* c, mist_step_record* record, void* hip_stream);
 
 /* out = coef * g, tensor by tensor (the same count and sizes; of any type; out may be g, otherwise they share no

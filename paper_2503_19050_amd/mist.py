@@ -739,7 +739,8 @@ def embed(ids, table, *, scale: float = 1.0, pos=None, vocab_begin: int = 0, out
     """mist_embed_forward: scale * table[ids - vocab_begin] + pos[position], zero in the first term for ids
     outside the shard (padding, other ranks' rows).  ids: [seq] or [batch, seq], int32 or int64 (batch strides
     allowed); table: [rows, hidden]; pos: [at least seq, hidden] or None; out: ids' shape + [hidden], of
-    any of float32, bfloat16, float16 (default: a new tensor of the table's type)."""
+    any of float32, bfloat16, float16 (default: a new tensor of the table's type).  Ranks that hold shards of the
+    table add up what they get: one of them passes pos, the others None."""
     torch = _torch()
     L = _lib or load()
     if (table.requires_grad or pos is not None and pos.requires_grad) and torch.is_grad_enabled():
@@ -886,7 +887,8 @@ def _lists_on(record, *lists) -> None:
 def grad_norm(grads: TensorList, record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
               accumulate: bool = False, finish: bool = True, stream=None) -> StepRecord:
     """mist_grad_norm over a list: record.total, and with finish the norm, the clip factor and the count of
-    the step.  Nothing is waited for.  accumulate joins record.total (a step with several lists)."""
+    the step.  Nothing is waited for.  accumulate joins record.total (a step with several lists).  Where ranks add
+    up their totals, a tensor that several of them hold is in one rank's list alone."""
     torch = _torch()
     c = _clip_desc(kind, grad_scale, max_norm)
     _lists_on(record, grads)
@@ -900,7 +902,8 @@ def grad_norm(grads: TensorList, record: StepRecord, *, max_norm: float = float(
 
 def grad_finish(record: StepRecord, *, max_norm: float = float("inf"), grad_scale: float = 1.0, kind: str = "l2",
                 stream=None) -> StepRecord:
-    """mist_grad_finish: forms the norm and the clip factor from record.total, e.g. after an all-reduce of it."""
+    """mist_grad_finish: forms the norm and the clip factor from record.total, e.g. after an all-reduce of it.  With
+    record.total.zero_() before it, a step without a pass over the gradients: the factor is grad_scale."""
     torch = _torch()
     L = _lib or load()
     c = _clip_desc(kind, grad_scale, max_norm)

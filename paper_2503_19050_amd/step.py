@@ -2,11 +2,13 @@
 
 The tuner's plan gives every stage its layers, its microbatch and its parallelism; the layers' GEMMs are
 in the operator database (calibrate.py), the step's ends are not.  For the first stage of a workload's
-plan this program allocates one rank's tensors as the cost model counts them (the vocabulary shard and
-the positions, the layers' shards, fp32 master weights with Adam's m and v of the rank's ZeRO share) and
-makes training steps with synthetic data: per microbatch the embedding lookup and its gradient, then
-the gradient norm, the clip factor and the Adam step of the rank's share.  The embedding learns
-random targets, so its loss falls; the layers' gradients are random.  It prints each
+plan this program allocates the tensors of one rank, the first of its tensor-parallel group: the parameters that
+the cost model counts, which has no biases of the projections (the vocabulary shard and the positions, the
+layers' shards), and fp32 master weights with Adam's m and v of the rank's ZeRO share.  It makes training steps
+with synthetic data: per microbatch the embedding lookup and its gradient, then the gradient norm, the
+clip factor and the Adam step of the rank's share.  Weights and gradients are whole and the norm is of all the
+rank's gradients, for ZeRO-2 and ZeRO-3 too, which split them; nothing is exchanged with other ranks.
+The embedding learns random targets, so its loss falls; the layers' gradients are random.  It prints each
 operator's time and its bytes per second.
 
     python -m paper_2503_19050_amd.step --workload gpt2.7b-d16 --out step.json

@@ -122,3 +122,20 @@ def test_norm_past_fp32_changes_nothing(torch):
     coef = 1.0 / float(g[0].double())
     assert int(rec.applied) == 1 and abs(float(rec.coef) - coef) <= 2.0 ** -23 * coef + 2.0 ** -150
     assert abs(float(out[0]) - 1.0) <= 2.0 ** -150 / coef + 2.0 ** -22 and float(out[1]) == 0.0
+
+
+def test_step_without_a_norm(torch):
+    """grad_finish on a total of zero forms a factor of grad_scale and counts the step: no pass over the gradients."""
+    from paper_2503_19050_amd import mist
+    g = torch.full((777,), 2.0, device="cuda")
+    p, m, v = (torch.zeros(777, device="cuda") for _ in range(3))
+    rec = mist.StepRecord()
+    L = lists(mist, p, m, v, g)
+    for k in range(2):
+        rec.total.zero_()
+        mist.grad_finish(rec, grad_scale=0.5)
+        mist.adam_step(*L, rec, lr=0.25, betas=(0.5, 0.5))
+        assert (int(rec.applied), int(rec.step), float(rec.coef)) == (1, k + 1, 0.5)
+        # g' = 1 in every step: both averages are 1 after bias correction, the update is lr
+        assert torch.equal(m, torch.full_like(m, 1 - 0.5 ** (k + 1)))
+        assert ((p + 0.25 * (k + 1)).abs() <= 1e-6).all()
