@@ -35,6 +35,7 @@ constexpr int kVec = 8;             // values of a lane
 constexpr int kSlab = 64 * kVec;    // columns of a wave
 constexpr int kJoinRuns = 128;      // long runs joined at a time
 constexpr int64_t kCache = (int64_t)256 << 20;  // the memory-side cache
+constexpr int64_t kHeld = 86000000;             // of rows that a lookup reaches, see k_embed
 constexpr int64_t kMostTokens = (int64_t)1 << 30;  // places past the last token stay below 2^31
 constexpr int kMaxChunk = 64;       // ordered tokens of a wave, one a lane, at most
 
@@ -140,10 +141,13 @@ __device__ __forceinline__ int64_t act_offset(const EmbedArgs& a, uint32_t token
 // of 8192 columns: 88 us; 8 tokens 98, 16 102), or 16 with positions (65536 of 2560: 94 us; 8 tokens 99,
 // 4 106).  With positions the tokens are taken position by position, so that a wave reads a position's row once for
 // its part of the batch.
-// by_slab: the blocks take the slabs in turn, so that with 2, 4 or a multiple of 8 slabs an XCD (blocks are dealt
-// to the 8 in turn) sees few columns, and its L2 holds more of the table's rows.  Where the rows that can occur fit
-// the memory-side cache this takes 81 instead of 88 us (4000 rows of 8192) and 54 instead of 61 (65536 tokens,
-// 2048 columns); otherwise the longer strides between writes cost more (65536 tokens of 4096: 143 instead of 134 us).
+// by_slab: the blocks take the slabs in turn, so that with 2, 4, 8 or 16 slabs an XCD (blocks are dealt to the 8 in
+// turn) sees few columns, and its L2 holds more of the table's rows.  That gains 4 to 17 % while the rows that the
+// tokens reach take at most kHeld bytes, and loses up to 30 % past it, where the longer strides between accesses
+// cost more.  Both ways, text's tokens, 16 bits (us by slab / in order, by megabytes of rows reached): 65536 tokens of 4096
+// columns 76: 93 / 110, 81: 101 / 110, 86: 119 / 109, 94: 135 / 117; 65536 of 8192 75: 179 / 195, 87: 192 / 193, 97: 245 / 208;
+// 65536 of 2048 69: 57 / 62; 32768 of 8192 in a shard of 4000 rows 82 / 89.  In fp32 the sides change at 90 to 100.  With 32 slabs
+// there is nothing to gain (16384 of 16384: 95 / 94).
 template <bool POS>
 constexpr int kAhead = POS ? 16 : 4;
 
@@ -704,6 +708,16 @@ mist_status check(const mist_embed_desc* d, bool out) {
   return MIST_OK;
 }
 
+// Rows of a table that n tokens reach, as text has them (the k-th most frequent 1 / k as often as the first): the sum over k of
+// 1 - (1 - p_k)^n with p_k = 1 / (k ln(rows + 1)), as an integral: rows (1 - e^-x) + rows x E1(x), x = n / (rows ln(rows + 1)).
+// E1 from its series below 1 and the approximation 5.1.54 of Abramowitz and Stegun from there on.
+double rows_reached(int64_t n, int64_t rows) {
+  const double x = (double)n / ((double)rows * std::log((double)rows + 1.0));
+  if (x >= 1.0) return (double)rows * (1.0 - std::exp(-x) * (1.0 - (x * (x + 2.334733) + 0.250621) / (x * (x + 3.330657) + 1.681534)));
+  const double e1 = -0.57721566 - std::log(x) + x * (1.0 - x * (1.0 / 4 - x * (1.0 / 18 - x * (1.0 / 96 - x / 600))));
+  return (double)rows * (x * e1 - std::expm1(-x));
+}
+
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 EmbedArgs args(const mist_embed_desc* d) {
@@ -814,8 +828,8 @@ mist_status mist_embed_forward(const mist_embed_desc* d, const void* ids, const 
   const EmbedArgs a = args(d);
   // enough tokens a wave to keep several rows in flight, few enough to fill the device
   const int64_t per_wave = std::clamp<int64_t>((int64_t)a.n * a.slabs / 16384, 1, pos ? kAhead<true> : kAhead<false>);
-  const bool by_slab = !pos && a.slabs > 1 && (a.slabs % 8 == 0 || 8 % a.slabs == 0) &&
-                       std::min<int64_t>(a.n, a.rows) * a.hidden * mist::type_bytes(d->table_type) <= kCache;
+  const int64_t row_bytes = a.hidden * mist::type_bytes(d->table_type);
+  const bool by_slab = !pos && a.slabs > 1 && 16 % a.slabs == 0 && (a.rows * row_bytes <= kHeld || rows_reached(a.n, a.rows) * row_bytes <= kHeld);
   const int64_t groups = (a.n + per_wave - 1) / per_wave;
   // A launch's grid stays below 2^32 threads; whole blocks of groups, so that no group is in two launches.
   const int64_t most = ((int64_t)1 << 23) / a.slabs * kWaves;

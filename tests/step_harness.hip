@@ -286,13 +286,41 @@ void lookups() {
   }
 }
 
+// Which lookups take the slabs in turn: by the rows that their tokens reach, from both sides of where it was measured.
+void slab_order() {
+  g_is_embed = true;
+  for (const int64_t rows : {(int64_t)1, (int64_t)300, (int64_t)20000}) {
+    for (const int64_t n : {(int64_t)1, (int64_t)5000, (int64_t)400000}) {
+      double sum = 0.0;
+      for (int64_t k = 1; k <= rows; ++k) sum += 1.0 - std::pow(1.0 - 1.0 / (double)k / std::log((double)rows + 1.0), (double)n);
+      if (rows > 1) check(std::fabs(lookup::rows_reached(n, rows) - sum) < 0.03 * sum + 1.0, "the rows reached");
+      check(lookup::rows_reached(n, rows) >= 0.0 && lookup::rows_reached(n, rows) <= (double)rows, "more rows than there are");
+    }
+  }
+  const struct {
+    int64_t n, hidden, rows;
+    int32_t type;
+    bool pos, want;
+  } all[] = {{65536, 4096, 13671, MIST_BF16, false, true},  {65536, 4096, 24000, MIST_BF16, false, false}, {65536, 4096, 32000, MIST_F16, false, false},
+             {16384, 4096, 32000, MIST_BF16, false, true},  {65536, 2048, 50257, MIST_BF16, false, true},  {32768, 8192, 4000, MIST_BF16, false, true},
+             {65536, 8192, 4882, MIST_BF16, false, true},   {65536, 8192, 12000, MIST_BF16, false, false}, {65536, 2048, 15625, MIST_F32, false, true},
+             {65536, 2048, 23437, MIST_F32, false, false},  {16384, 16384, 4000, MIST_BF16, false, false}, {65536, 512, 100, MIST_BF16, false, false},
+             {65536, 2048, 50257, MIST_BF16, true, false},  {65536, 2560, 100, MIST_BF16, false, false},   {1, 1024, 1, MIST_BF16, false, true}};
+  for (const auto& c : all) {
+    const mist_embed_desc d{1, c.n, c.hidden, c.rows, 0, c.n, 0, c.hidden, c.hidden, c.hidden, 8, c.type, c.type, 1.0f};
+    g_launches.clear();
+    check(mist_embed_forward(&d, (void*)4096, (void*)4096, c.pos ? (void*)4096 : nullptr, (void*)4096, nullptr) == MIST_OK &&
+              g_launches.size() == 1 && g_launches[0].by_slab == c.want, "which lookups take the slabs in turn");
+  }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const struct {
     const char* name;
     void (*run)();
-  } all[] = {{"lists", lists}, {"failures", failures}, {"failing_wait", failing_wait}, {"overlaps", overlaps}, {"grids", grids}, {"lookups", lookups}};
+  } all[] = {{"lists", lists}, {"failures", failures}, {"failing_wait", failing_wait}, {"overlaps", overlaps}, {"grids", grids}, {"lookups", lookups}, {"slab_order", slab_order}};
   for (const auto& s : all)
     if (argc == 2 && !std::strcmp(argv[1], s.name)) {
       s.run();

@@ -29,7 +29,7 @@ def harness(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["lists", "failures", "failing_wait", "overlaps", "grids", "lookups"])
+@pytest.mark.parametrize("scenario", ["lists", "failures", "failing_wait", "overlaps", "grids", "lookups", "slab_order"])
 def test_scenario(harness, scenario):
     """What each one checks stands at its function in step_harness.hip."""
     r = subprocess.run([harness, scenario], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1"))
