@@ -7,15 +7,15 @@
 // orders the tokens by row (stable, so that a row's terms are added in token order whatever ran first), sums
 // each row's terms in fp32 registers and writes the row once: no atomics on values.  Measured on one MI355X
 // (16-bit values; a large copy reads and writes 4.9 TB/s, a fill writes 6.8):
-//   lookup    65536 tokens of 2560 columns with positions  89-94 us, 336 MB written and 205 MB read: 5.7 TB/s
+//   lookup    65536 tokens of 2560 columns with positions  93 us, 336 MB written and 205 MB read: 5.7 TB/s
 //             32768 of 8192 in a shard of 4000 rows         81 us, 537 MB written and 80 MB read: 7.6 TB/s
-//   gradient  65536 of 2560, 50257 rows, with positions   185-190 us: order with the positions' sums 4 x 21 us
-//             (335 MB read), rows 95 us (339 MB read, 262 MB written), long runs 6.5 us.  The gradient is read twice,
+//   gradient  65536 of 2560, 50257 rows, with positions   188 us: order with the positions' sums 4 x 23 us
+//             (335 MB read), rows 98 us (339 MB read, 262 MB written), long runs 6.5 us.  The gradient is read twice,
 //             once by position and once by row: 5 TB/s over the call
-//             131072 of 8192, 32000 rows                  427-441 us: order 27 us, rows 401 us (1617 MB read, 549 MB
-//             written: 5.4 TB/s), long runs 13 us
-//             4095 of 4096 added to fp32                   30 us: order 7 us, rows 18 us, long runs 5 us
-//             256 of 512 in fp32, 2048 rows                9.4 us, one launch
+//             131072 of 8192, 32000 rows                  443 us: order 27 us, rows 405 us (1617 MB read, 549 MB
+//             written: 5.3 TB/s), long runs 13 us
+//             4095 of 4096 added to fp32                   30 us: order 7 us, rows 19 us, long runs 5 us
+//             256 of 512 in fp32, 2048 rows                9.1 us, one launch
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -139,7 +139,8 @@ __device__ __forceinline__ int64_t act_offset(const EmbedArgs& a, uint32_t token
 // ---- lookup ----------------------------------------------------------------------------------------
 // A wave takes `per_wave` (at most kAhead) tokens and one slab of columns, all rows in flight: 4 (32768 tokens
 // of 8192 columns: 88 us; 8 tokens 98, 16 102), or 16 with positions (65536 of 2560: 94 us; 8 tokens 99,
-// 4 106).  With positions the tokens are taken position by position, so that a wave reads a position's row once for
+// 4 106).  These are in 16 bits; fp32 tables and odd widths hold 256 registers with 16 (fp32 189 us for the 172 of a copy).
+// With positions the tokens are taken position by position, so that a wave reads a position's row once for
 // its part of the batch.
 // by_slab: the blocks take the slabs in turn, so that with 2, 4, 8 or 16 slabs an XCD (blocks are dealt to the 8 in
 // turn) sees few columns, and its L2 holds more of the table's rows.  That gains 4 to 17 % while the rows that the
@@ -194,8 +195,9 @@ __global__ __launch_bounds__(kThreads) void k_embed(EmbedArgs a, int32_t per_wav
 // ---- sums of the positions -------------------------------------------------------------------------
 // A wave takes a position and a slab, and adds up the batch.  The work is spread over the launches that order
 // the tokens, which leave most of the device idle: `block` of `blocks` more blocks takes the items [begin, end).
-// The reads reach 4.2 TB/s (32 x 2048 tokens of 2560 columns, 16 bits); more loads at once, several
-// positions a wave, or several waves a position measured the same or worse.
+// The reads reach 3.6 to 3.9 TB/s (32 x 2048 tokens of 2560 columns, 16 bits): a launch's share is 160 blocks beside the 64
+// that order, fewer than the CUs.  More loads at once, several positions a wave, or several waves a position measured the same or
+// worse there; a batch far larger than the sequence leaves few waves.
 template <int L>
 constexpr int kPosAhead = L == kOdd ? 2 : 8;  // one by one, eight take more registers than a block of 1024 threads has
 

@@ -34,7 +34,8 @@ struct Elem<MIST_F16> {
 };
 
 // N consecutive values, read and written by instructions of up to 16 bytes.  They need only their element's
-// alignment (the device's global memory instructions take any), so that shards and odd rows take the same path.
+// alignment (the device's global memory instructions take any), so that shards take the same path.  Rows of the
+// embedding have to be whole vectors too.
 template <class T, int N>
 struct Vec {
   typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));

@@ -4,10 +4,10 @@
 // pieces of 4096 elements, one block each (on one card, blocks that take pieces in turn measured 3650 us where these
 // take 3410, pieces of 2048 or 8192 elements 3515 and 3500: Adam step of 629 million parameters).  Measured on one
 // MI355X, where a large copy reads and writes 4.9 TB/s:
-//   norm   302 million fp32  201 us, 6.0 TB/s;  629 million bf16  212 us, 5.9 TB/s
-//   clip   302 million fp32 to bf16  293 us, 6.2 TB/s (its reads partly from the cache)
-//   Adam   629 million, bf16 gradients and weights  3190 us, 5.5 TB/s;  39.7 million in f16, one element
-//          off alignment  224 us, 5.0 TB/s
+//   norm   302 million fp32  200 us, 6.1 TB/s;  629 million bf16  212 us, 6.0 TB/s
+//   clip   302 million fp32 to bf16  294 us, 6.2 TB/s (its reads partly from the cache)
+//   Adam   629 million, bf16 gradients and weights  3156 us, 5.6 TB/s;  39.7 million in f16, one element
+//          off alignment  222 us, 5.3 TB/s
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
