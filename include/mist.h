@@ -625,6 +625,168 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
                            const mist_tensors* w, const mist_step_record* record, const mist_adam_desc* a,
                            void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of the last stage and of a layer beside its matrix products, on the current device: token log
+ * probabilities and the loss, over the whole vocabulary or a shard of it (the cost model's last-stage head of
+ * ceil(V/TP) rows), the norms around a block, and activations kept in 8 bits for the backward pass (a smaller
+ * form of what a plan recomputes or offloads).  As above: each call enqueues and returns, can be captured, keeps nothing,
+ * and gives the same bits on every run.  An output shares memory with nothing else unless it says so (refused where the
+ * addresses' ranges show it).
+ * --------------------------------------------------------------------------------------- */
+
+#define MIST_TOKEN_MAX_TOP 64
+
+/* Logits of batch sequences of seq tokens: columns [vocab_begin, vocab_begin + rows) of the vocabulary, this rank's
+ * shard.  With z = scale * logits, m = max z, s = sum exp(z - m) and u = sum exp(z - m) (z - m):
+ * lse = m + log s, the target's log probability is z[target] - lse, the entropy log s - u / s.
+ * A logit of -inf is masked out.  A target below 0 is padding: its log probability is 0 and has no gradient.  One
+ * of 0 or more that no rank holds, or that is masked out, has -inf.  A token whose logits are all -inf has lse = -inf,
+ * entropy 0 and no gradient; one with NaN or +inf among them has NaN.  Strides are in elements; columns are contiguous. */
+typedef struct mist_token_desc {
+  int64_t batch, seq;      /* >= 0; batch * seq < 2^30 */
+  int64_t rows;            /* columns of the logits, 1..2^31 - 2 */
+  int64_t vocab_begin;     /* id of the first, in [0, 2^31) */
+  int64_t ids_stride;      /* between sequences' targets (those of one sequence are contiguous) */
+  int64_t logits_batch_stride, logits_stride; /* of the logits, between sequences and between tokens */
+  int64_t grad_batch_stride, grad_stride;     /* of their gradient */
+  int32_t ids_bytes;       /* 4 or 8: signed ids */
+  int32_t type;            /* of the logits and their gradient */
+  int32_t top;             /* alternatives a token, 0..MIST_TOKEN_MAX_TOP */
+  float scale;             /* > 0, finite (1 / temperature) */
+} mist_token_desc;
+
+/* Over the whole vocabulary (vocab_begin = 0): per token fp32 logp, lse and entropy (logp and entropy may be NULL; without
+ * logp, targets may be), and int32 top_ids[tokens * top] with fp32 top_logp[tokens * top], the most probable tokens by logit, the
+ * lower id first among equals (a NaN above everything); where fewer than top are not masked out the rest has
+ * id -1 and -inf.  Per-token arrays are contiguous, sequence by sequence.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_token_logprob(const mist_token_desc* d, const void* logits, const void* targets, float* logp, float* lse,
+                               float* entropy, int32_t* top_ids, float* top_logp, void* hip_stream);
+
+/* One rank's part: stats[tokens * 4] = (m, s, u, the target's z or -inf where another rank holds it) and its
+ * alternatives as ids of the whole vocabulary with z.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_token_part(const mist_token_desc* d, const void* logits, const void* targets, float* stats, int32_t* top_ids,
+                            float* top_z, void* hip_stream);
+
+/* The ranks' parts joined: stats[ranks][tokens * 4], top_ids and top_z [ranks][tokens * top] as gathered; outputs as
+ * of mist_token_logprob.  Of *d it uses batch, seq, ids_stride, ids_bytes and top.  ranks in 1..65536.  Errors:
+ * MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_token_join(const mist_token_desc* d, int32_t ranks, const float* stats, const int32_t* top_ids, const float* top_z,
+                            const void* targets, float* logp, float* lse, float* entropy, int32_t* out_ids, float* out_logp,
+                            void* hip_stream);
+
+/* The logits' gradient from the log probabilities' (dlogp, NULL: zero) and the entropies' (dentropy, NULL: zero; then
+ * entropy may be NULL too), with lse and entropy of the whole vocabulary: dlogits[j] = scale * (dlogp ([j = target] -
+ * p[j]) - dentropy p[j] (log p[j] + entropy)).  dlogits may be the logits (with their strides).
+ * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_token_grad(const mist_token_desc* d, const void* logits, const void* targets, const float* lse, const float* dlogp,
+                            const float* entropy, const float* dentropy, void* dlogits, void* hip_stream);
+
+/* A training microbatch in one pass over the whole vocabulary (vocab_begin = 0): fp32 logp per token, and the gradient of
+ * the loss -sum weights[t] logp[t]: dlogits[j] = scale * weights[t] (p[j] - [j = target]), zeros for padding.  weights: fp32 per token (NULL: weight
+ * for every token; otherwise weight is a factor of them).  dlogits may be the logits (with their strides).
+ * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_token_loss(const mist_token_desc* d, const void* logits, const void* targets, const float* weights, float weight,
+                            float* logp, void* dlogits, void* hip_stream);
+
+#define MIST_BLOCK_RMS 0
+#define MIST_BLOCK_LAYER 1
+#define MIST_BLOCK_MAX_HIDDEN 16384
+
+/* The residual around a block and the norms before and after it, for batch sequences of seq tokens.  N is
+ * n = x / sqrt(mean x^2 + eps) (RMS) or n = (x - mean x) / sqrt(var x + eps) (LAYER).
+ *     v = N(block) post_weight + post_bias   (block itself without post_weight)
+ *     y = res_scale x + block_scale gate v   (gate: one value a column, or a row of them for each sequence; none: 1)
+ *     h = N(y) weight + bias                 (of y as stored; biases may be NULL)
+ * Row strides are in elements, tokens of all sequences at one stride; columns are contiguous.  Those of gradients are
+ * with the backward call. */
+typedef struct mist_block_desc {
+  int64_t batch, seq;      /* >= 0; batch * seq < 2^30 */
+  int64_t hidden;          /* 1..MIST_BLOCK_MAX_HIDDEN */
+  int64_t x_stride, block_stride, y_stride, h_stride;
+  int64_t gate_stride;     /* between sequences' gates; 0: one gate for all */
+  int32_t kind;            /* MIST_BLOCK_RMS or MIST_BLOCK_LAYER */
+  int32_t type;            /* of block and h, and their gradients */
+  int32_t res_type;        /* of x and y, and their gradients: type, or MIST_F32 */
+  int32_t weight_type;     /* of weights, biases and gates, and their gradients */
+  float eps;               /* >= 0, finite */
+  float res_scale, block_scale; /* finite */
+} mist_block_desc;
+
+/* y and h, and fp32 stats[tokens * 4] for the backward pass: mean and 1 / sqrt(var + eps) of block and of y (0 and 1 where there is
+ * no such norm).  block may be NULL: then y = x, which is not written (y NULL, no post_weight, no gate, scales 1), and h is its norm.
+ * weight may be NULL: no h.  y may be x (with its stride), or block (if the types are the same, with its stride).
+ * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_block_forward(const mist_block_desc* d, const void* x, const void* block, const void* weight, const void* bias,
+                               const void* post_weight, const void* post_bias, const void* gate, void* y, void* h, float* stats,
+                               void* hip_stream);
+
+/* Gradients: dh of h (NULL iff weight is) and dy of y by its other uses (NULL: none) give dx and dblock (each may be
+ * NULL: not wanted), and, where their addresses are given, those of the weights, biases and gates, overwritten or
+ * (accumulate = 1) added to.  Sums over tokens are in fp32 in an order that depends on the sizes alone. */
+typedef struct mist_block_grads {
+  const void *dh, *dy;
+  void *dx, *dblock;
+  void *dweight, *dbias, *dpost_weight, *dpost_bias, *dgate;
+  int64_t dh_stride, dy_stride, dx_stride, dblock_stride;
+  int64_t dgate_stride;    /* between sequences' gates */
+  int32_t accumulate;
+} mist_block_grads;
+
+/* Scratch bytes that mist_block_backward needs.  Errors: MIST_E_INVALID. */
+mist_status mist_block_workspace(const mist_block_desc* d, const mist_block_grads* g, size_t* bytes);
+
+/* From y (as stored), block and stats of the forward call.  dx may be dy, and dblock dh or block (each with the other's
+ * stride).  workspace: at least mist_block_workspace bytes, aligned to 256.  Errors: MIST_E_INVALID, MIST_E_RANGE
+ * (workspace too small), MIST_E_DEVICE. */
+mist_status mist_block_backward(const mist_block_desc* d, const void* y, const void* block, const float* stats, const void* weight,
+                                const void* post_weight, const void* post_bias, const void* gate, const mist_block_grads* g,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+#define MIST_KEPT_GROUP 128
+
+/* A tensor of rows x width kept in 8 bits.  Each group of 128 values along a row (the last may be shorter) has a byte
+ * e + 127 with the least e >= -126 for which max |x| <= 127 * 2^e; values are int8 round(x / 2^e), ties to even.  Loaded values are
+ * values * 2^e, exact in fp32 and bf16, off by at most 2^e / 2 (magnitudes past 127 * 2^121 saturate there, those
+ * past f16's largest at it).  A group with inf or NaN has the byte 255 and comes back as NaN.
+ * int8 values[rows][groups * 128] and bytes exponents[rows][groups], groups = ceil(width / 128); values past
+ * width are zeros.  values are aligned to 16. */
+typedef struct mist_kept_desc {
+  int64_t rows;            /* 0..2^31 - 1 */
+  int64_t width;           /* 1..2^31 - 1; rows * groups < 2^40 */
+  int64_t stride;          /* between rows of the tensor */
+  int32_t type;            /* of the tensor */
+} mist_kept_desc;
+
+mist_status mist_kept_store(const mist_kept_desc* d, const void* x, int8_t* values, uint8_t* exponents, void* hip_stream);
+mist_status mist_kept_load(const mist_kept_desc* d, const int8_t* values, const uint8_t* exponents, void* x, void* hip_stream);
+
+#define MIST_ACT_SILU 0 /* x / (1 + exp(-x)) */
+#define MIST_ACT_GELU 1 /* x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) */
+
+typedef struct mist_act_desc {
+  int64_t rows, width;     /* as of mist_kept_desc */
+  int64_t up_stride, gate_stride, out_stride; /* of up and gate (or their gradients) and of the activation (or its gradient) */
+  int64_t again_stride;    /* of the activation formed again */
+  int32_t type, kind;
+} mist_act_desc;
+
+/* A tensor in 8 bits, as of mist_kept_store. */
+typedef struct mist_kept {
+  int8_t* values;
+  uint8_t* exponents;
+} mist_kept;
+
+/* out = act(gate) * up, or act(up) where gate is NULL.  up8 and gate8 receive up and gate in 8 bits (NULL: not
+ * kept).  out may be up or gate (with its stride).  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_act_forward(const mist_act_desc* d, const void* up, const void* gate, void* out, const mist_kept* up8,
+                             const mist_kept* gate8, void* hip_stream);
+
+/* Gradients at the kept values: dgate = dout * up * act'(gate) and dup = dout * act(gate), or dup = dout * act'(up)
+ * where gate8 is NULL (then dgate is too).  again (NULL: not wanted) receives the activation at the kept values.
+ * dup or dgate may be dout (with its stride).  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+mist_status mist_act_backward(const mist_act_desc* d, const mist_kept* up8, const mist_kept* gate8, const void* dout, void* dup,
+                              void* dgate, void* again, void* hip_stream);
+
 /* Frees every buffer of the space (through its allocator).  NULL is accepted. */
 mist_status mist_space_destroy(mist_space* S);
 

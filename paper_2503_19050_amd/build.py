@@ -18,7 +18,8 @@ SOURCES = [os.path.join(CSRC, "mist_host.cpp"), os.path.join(CSRC, "mist_plan.cp
            os.path.join(CSRC, "mist_search.hip"), os.path.join(CSRC, "mist_extract.hip"),
            os.path.join(CSRC, "mist_exact.hip"), os.path.join(CSRC, "mist_corun.hip"),
            os.path.join(CSRC, "mist_probe.hip"), os.path.join(CSRC, "mist_noalloc.hip"),
-           os.path.join(CSRC, "mist_embed.hip"), os.path.join(CSRC, "mist_step.hip")]
+           os.path.join(CSRC, "mist_embed.hip"), os.path.join(CSRC, "mist_step.hip"),
+           os.path.join(CSRC, "mist_token.hip"), os.path.join(CSRC, "mist_block.hip"), os.path.join(CSRC, "mist_kept.hip")]
 LIBS = ["-lrocblas"]  # the calibration's GEMMs
 HEADERS = [os.path.join(CSRC, "mist_internal.h"), os.path.join(CSRC, "mist_device.h"),
            os.path.join(CSRC, "mist_bounds.h"), os.path.join(CSRC, "mist_ops.h"), os.path.join(INCLUDE, "mist.h")]

@@ -41,6 +41,76 @@ struct Vec {
   typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
+typedef float Float8 __attribute__((ext_vector_type(8)));
+
+// Eight consecutive values as fp32, of which `left` are there (the others are `fill`).
+template <class T>
+__device__ __forceinline__ Float8 load8(const T* p, int64_t left, float fill = 0.0f) {
+  if (left >= 8) return __builtin_convertvector(*(const typename Vec<T, 8>::type*)p, Float8);
+  Float8 x = fill;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < left) x[k] = (float)p[k];
+  return x;
+}
+template <class T>
+__device__ __forceinline__ void store8(T* p, int64_t left, Float8 x) {
+  if (left >= 8) {
+    *(typename Vec<T, 8>::type*)p = __builtin_convertvector(x, typename Vec<T, 8>::type);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < left) p[k] = (T)x[k];
+}
+
+// Sum, or largest, over a wave; every lane has the result.
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// exp(x) by the base-2 instruction: off by 2^-24 |x| from the product and 1 ulp from the instruction.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// The addresses of rows of width elements, for checks of what shares memory.
+struct Range {
+  uintptr_t lo, hi;
+};
+inline Range range_of(const void* p, int64_t rows, int64_t stride, int64_t width, int64_t bytes) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  if (!p || rows <= 0 || width <= 0) return Range{lo, lo};
+  const unsigned __int128 n = ((unsigned __int128)(rows - 1) * (uint64_t)stride + (uint64_t)width) * (uint64_t)bytes;
+  return Range{lo, n > UINTPTR_MAX - lo ? UINTPTR_MAX : lo + (uintptr_t)n};
+}
+inline bool overlap(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
+
+// Whether two sets of rows share memory: their ranges do, unless both lie beside each other in rows of one stride (the
+// halves of a product's output).
+struct Rows {
+  const void* p;
+  int64_t rows, stride, width, bytes;  // bytes: of an element
+};
+inline bool overlap(const Rows& a, const Rows& b) {
+  if (!overlap(range_of(a.p, a.rows, a.stride, a.width, a.bytes), range_of(b.p, b.rows, b.stride, b.width, b.bytes))) return false;
+  const int64_t step = a.stride * a.bytes, wa = a.width * a.bytes, wb = b.width * b.bytes;
+  if (a.rows <= 1 || b.rows <= 1 || step != b.stride * b.bytes || wa > step || wb > step) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p), m = (uintptr_t)step;
+  const int64_t off = (int64_t)(y >= x ? (y - x) % m : (m - (x - y) % m) % m);
+  return off < wa || off + wb > step;
+}
+
+inline bool is_aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+constexpr int64_t kMostStride = (int64_t)1 << 40;
+inline bool stride_ok(int64_t x) { return x >= 0 && x <= kMostStride; }
+
 inline int64_t type_bytes(int32_t type) { return type == MIST_F32 ? 4 : 2; }
 inline bool type_ok(int32_t type) { return type == MIST_F32 || type == MIST_BF16 || type == MIST_F16; }
 

@@ -8,7 +8,9 @@ raises; there is no fallback.
 
 from __future__ import annotations
 
+import collections
 import ctypes
+import math
 import os
 import threading
 
@@ -31,6 +33,9 @@ EXPORTS = [
     "mist_search_info", "mist_tile_info", "mist_debug_eval_tiles", "mist_eval_ids_noalloc", "mist_exact_group_sizes",
     "mist_embed_forward", "mist_embed_workspace", "mist_embed_backward", "mist_tensors_create", "mist_tensors_destroy",
     "mist_norm_workspace", "mist_grad_norm", "mist_grad_finish", "mist_grad_clip", "mist_adam_step",
+    "mist_token_logprob", "mist_token_part", "mist_token_join", "mist_token_grad", "mist_token_loss",
+    "mist_block_forward", "mist_block_workspace", "mist_block_backward", "mist_kept_store", "mist_kept_load",
+    "mist_act_forward", "mist_act_backward",
 ]
 
 PROBE_KINDS = {"add": 0, "mul": 1, "fma": 2, "min": 3, "max": 4, "cmp": 5}
@@ -144,6 +149,40 @@ class AdamDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ["lr", "beta1", "beta2", "eps", "weight_decay"]]
 
 
+class TokenDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in
+                ["batch", "seq", "rows", "vocab_begin", "ids_stride", "logits_batch_stride", "logits_stride",
+                 "grad_batch_stride", "grad_stride"]] + \
+               [("ids_bytes", ctypes.c_int32), ("type", ctypes.c_int32), ("top", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class BlockDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in
+                ["batch", "seq", "hidden", "x_stride", "block_stride", "y_stride", "h_stride", "gate_stride"]] + \
+               [(n, ctypes.c_int32) for n in ["kind", "type", "res_type", "weight_type"]] + \
+               [(n, ctypes.c_float) for n in ["eps", "res_scale", "block_scale"]]
+
+
+class BlockGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ["dh", "dy", "dx", "dblock", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate"]] + \
+               [(n, ctypes.c_int64) for n in ["dh_stride", "dy_stride", "dx_stride", "dblock_stride", "dgate_stride"]] + \
+               [("accumulate", ctypes.c_int32)]
+
+
+class KeptDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ["rows", "width", "stride"]] + [("type", ctypes.c_int32)]
+
+
+class ActDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ["rows", "width", "up_stride", "gate_stride", "out_stride", "again_stride"]] + \
+               [("type", ctypes.c_int32), ("kind", ctypes.c_int32)]
+
+
+class Kept(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -210,6 +249,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         L.mist_grad_finish.argtypes = [P(ClipDesc), vp, vp]
         L.mist_grad_clip.argtypes = [vp, vp, vp, vp]
         L.mist_adam_step.argtypes = [vp, vp, vp, vp, vp, vp, P(AdamDesc), vp]
+        f32 = ctypes.c_float
+        L.mist_token_logprob.argtypes = [P(TokenDesc)] + [vp] * 8
+        L.mist_token_part.argtypes = [P(TokenDesc)] + [vp] * 6
+        L.mist_token_join.argtypes = [P(TokenDesc), i32] + [vp] * 10
+        L.mist_token_grad.argtypes = [P(TokenDesc)] + [vp] * 8
+        L.mist_token_loss.argtypes = [P(TokenDesc), vp, vp, vp, f32, vp, vp, vp]
+        L.mist_block_forward.argtypes = [P(BlockDesc)] + [vp] * 11
+        L.mist_block_workspace.argtypes = [P(BlockDesc), P(BlockGrads), P(sz)]
+        L.mist_block_backward.argtypes = [P(BlockDesc)] + [vp] * 7 + [P(BlockGrads), vp, sz, vp]
+        L.mist_kept_store.argtypes = [P(KeptDesc)] + [vp] * 4
+        L.mist_kept_load.argtypes = [P(KeptDesc)] + [vp] * 4
+        L.mist_act_forward.argtypes = [P(ActDesc), vp, vp, vp, P(Kept), P(Kept), vp]
+        L.mist_act_backward.argtypes = [P(ActDesc), P(Kept), P(Kept)] + [vp] * 5
         L.mist_last_error.restype = ctypes.c_char_p
         for name in EXPORTS:
             if name != "mist_last_error":
@@ -938,3 +990,468 @@ def adam_step(master: TensorList, m: TensorList, v: TensorList, grads: TensorLis
                record.ptr, ctypes.byref(a), handle)
     if other is not None:
         _used_on(other, record.data, *(t for x in lists for t in x.tensors))
+
+
+# ---- the last stage and a layer beside its matrix products: loss, norms, kept activations ---------------
+TOKEN_MAX_TOP = 64
+KEPT_GROUP = 128
+_BLOCK_KINDS = {"rms": 0, "layer": 1}
+_ACTS = {"silu": 0, "gelu": 1}
+
+TokenLogprob = collections.namedtuple("TokenLogprob", "logp lse entropy top_ids top_logp")
+TokenPart = collections.namedtuple("TokenPart", "stats top_ids top_z")
+BlockNorm = collections.namedtuple("BlockNorm", "y h stats")
+MlpAct = collections.namedtuple("MlpAct", "out up gate")
+
+
+def _no_graph(torch, what, *tensors) -> None:
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        _need(False, "%s: records no gradient; call it under torch.no_grad() and the gradient's call for the gradients" % what)
+
+
+def _here(what, first, *tensors) -> None:
+    _need(first.is_cuda and all(t is None or t.device == first.device for t in tensors), "%s: the tensors must be on one GPU" % what)
+
+
+def _shaped(what, t, shape, dtype, name) -> None:
+    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), "%s: %s must be %s of %s" % (what, name, dtype, tuple(shape)))
+
+
+def _flat(what, t) -> tuple[int, int]:
+    """(rows, their stride) of a tensor whose last dimension is contiguous and whose others are rows at one stride."""
+    shape, strides = t.shape, t.stride()
+    _need(len(shape) >= 1, "%s: a tensor without dimensions" % what)
+    if t.is_contiguous():
+        width = shape[-1]
+        return (t.numel() // width if width else 0), width
+    rows, stride = 1, shape[-1]
+    if t.numel() == 0:
+        return 0, stride
+    _need(shape[-1] == 1 or strides[-1] == 1, "%s: the last dimension must be contiguous" % what)
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n == 1:
+            continue
+        if rows == 1:
+            stride = s
+        _need(s == stride * rows, "%s: the leading dimensions must be rows at one stride" % what)
+        rows *= n
+    return rows, stride
+
+
+def _packed(what, t, shape, dtype, name):
+    _shaped(what, t, shape, dtype, name)
+    _need(t.is_contiguous(), "%s: %s must be contiguous" % (what, name))
+    return t
+
+
+def _token_desc(torch, logits, targets, grad, vocab_begin, scale, top) -> TokenDesc:
+    what = "token log probabilities"
+    _here(what, logits, targets, grad)
+    lshape = logits.shape
+    shape = lshape[:-1]
+    _need(len(lshape) in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    two = len(lshape) == 3
+    ist, id_bytes = 0, 8
+    if targets is not None:
+        id_bytes = targets.element_size()
+        _need(id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed,
+              "%s: targets must be int32 or int64" % what)
+        _need(targets.shape == shape, "%s: targets must have the logits' shape but for the last dimension" % what)
+        _need(shape[-1] <= 1 or targets.stride(-1) == 1, "%s: the targets of a sequence must be contiguous" % what)
+        ist = targets.stride(0) if two else 0
+    lst = logits.stride()
+    _need(lshape[-1] <= 1 or lst[-1] == 1 or logits.numel() == 0, "%s: the last dimension must be contiguous" % what)
+    gst = lst
+    if grad is not None:
+        _need(grad.shape == lshape and grad.dtype == logits.dtype, "%s: the gradient must have the logits' shape and type" % what)
+        gst = grad.stride()
+        _need(lshape[-1] <= 1 or gst[-1] == 1 or logits.numel() == 0, "%s: the last dimension must be contiguous" % what)
+    return TokenDesc(lshape[0] if two else 1, lshape[-2], lshape[-1], int(vocab_begin), ist, lst[0] if two else 0, lst[-2], gst[0] if two else 0,
+                     gst[-2], id_bytes, _type(logits, what), int(top), float(scale))
+
+
+def _top_space(torch, shape, top, device):
+    if not top:
+        return None, None
+    _need(0 < top <= TOKEN_MAX_TOP, "token log probabilities: top must be in 0..%d" % TOKEN_MAX_TOP)
+    return (torch.empty(shape + (top,), dtype=torch.int32, device=device), torch.empty(shape + (top,), dtype=torch.float32, device=device))
+
+
+def token_logprob(logits, targets=None, *, scale: float = 1.0, entropy: bool = False, top: int = 0, stream=None) -> TokenLogprob:
+    """mist_token_logprob over the whole vocabulary: fp32 logp of the targets (None without them; 0 for padding, targets below 0),
+    lse, entropy (None if not asked for), and the `top` most probable ids with their log probabilities.  logits: [seq, vocab] or
+    [batch, seq, vocab] (strides allowed, e.g. without the last position), scale 1 / temperature; targets: int32 or int64."""
+    torch = _torch()
+    L = _lib or load()
+    _no_graph(torch, "token log probabilities", logits)
+    d = _token_desc(torch, logits, targets, None, 0, scale, top)
+    device, shape = logits.device, tuple(logits.shape[:-1])
+    handle, other = _stream_of(torch, stream, device)
+    with torch.cuda.stream(other):
+        lse = torch.empty(shape, dtype=torch.float32, device=device)
+        logp = None if targets is None else torch.empty_like(lse)
+        ent = torch.empty_like(lse) if entropy else None
+        ids, values = _top_space(torch, shape, top, device)
+    _on_device(torch, device, L.mist_token_logprob, ctypes.byref(d), logits.data_ptr(), _ptr(targets), _ptr(logp), lse.data_ptr(), _ptr(ent),
+               _ptr(ids), _ptr(values), handle)
+    if other is not None:
+        _used_on(other, logits, targets)
+    return TokenLogprob(logp, lse, ent, ids, values)
+
+
+def token_part(logits, targets, *, vocab_begin: int, scale: float = 1.0, top: int = 0, stats=None, stream=None) -> TokenPart:
+    """mist_token_part: what a rank with the logits of ids [vocab_begin, vocab_begin + rows) knows of each token, for
+    token_join over all ranks' (all-gathered) parts: stats [..., 4] (given, e.g. this rank's place in what is gathered, or
+    new) and its `top` alternatives.  targets are ids of the whole vocabulary."""
+    torch = _torch()
+    L = _lib or load()
+    _no_graph(torch, "token log probabilities", logits)
+    d = _token_desc(torch, logits, targets, None, vocab_begin, scale, top)
+    device, shape = logits.device, tuple(logits.shape[:-1])
+    handle, other = _stream_of(torch, stream, device)
+    with torch.cuda.stream(other):
+        if stats is None:
+            stats = torch.empty(shape + (4,), dtype=torch.float32, device=device)
+        ids, z = _top_space(torch, shape, top, device)
+    _here("token log probabilities", logits, stats)
+    _packed("token log probabilities", stats, shape + (4,), torch.float32, "stats")
+    _on_device(torch, device, L.mist_token_part, ctypes.byref(d), logits.data_ptr(), targets.data_ptr(), stats.data_ptr(), _ptr(ids), _ptr(z), handle)
+    if other is not None:
+        _used_on(other, logits, targets, stats)
+    return TokenPart(stats, ids, z)
+
+
+def token_join(stats, targets=None, *, entropy: bool = False, top_ids=None, top_z=None, stream=None) -> TokenLogprob:
+    """mist_token_join: token_logprob's results from the parts of all ranks, stats [ranks, ..., 4], and top_ids and top_z
+    [ranks, ..., top] where alternatives are wanted."""
+    torch = _torch()
+    L = _lib or load()
+    what = "token log probabilities"
+    _need(stats.dim() in (3, 4) and stats.shape[-1] == 4, "%s: stats must be [ranks, seq, 4] or [ranks, batch, seq, 4]" % what)
+    _here(what, stats, targets, top_ids, top_z)
+    ranks, shape, device = stats.shape[0], tuple(stats.shape[1:-1]), stats.device
+    _packed(what, stats, stats.shape, torch.float32, "stats")
+    top = 0
+    _need((top_ids is None) == (top_z is None), "%s: top_ids and top_z come together" % what)
+    if top_ids is not None:
+        top = top_ids.shape[-1]
+        _packed(what, top_ids, (ranks,) + shape + (top,), torch.int32, "top_ids")
+        _packed(what, top_z, (ranks,) + shape + (top,), torch.float32, "top_z")
+    ist, id_bytes = 0, 8
+    if targets is not None:
+        id_bytes = targets.element_size()
+        _need(id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed,
+              "%s: targets must be int32 or int64" % what)
+        _need(tuple(targets.shape) == shape, "%s: targets must have the tokens' shape" % what)
+        _need(shape[-1] <= 1 or targets.stride(-1) == 1, "%s: the targets of a sequence must be contiguous" % what)
+        ist = targets.stride(0) if len(shape) == 2 else 0
+    d = TokenDesc(shape[0] if len(shape) == 2 else 1, shape[-1], 1, 0, ist, 0, 0, 0, 0, id_bytes, 0, top, 1.0)
+    handle, other = _stream_of(torch, stream, device)
+    with torch.cuda.stream(other):
+        lse = torch.empty(shape, dtype=torch.float32, device=device)
+        logp = None if targets is None else torch.empty_like(lse)
+        ent = torch.empty_like(lse) if entropy else None
+        ids, values = _top_space(torch, shape, top, device)
+    _on_device(torch, device, L.mist_token_join, ctypes.byref(d), ranks, stats.data_ptr(), _ptr(top_ids), _ptr(top_z), _ptr(targets), _ptr(logp),
+               lse.data_ptr(), _ptr(ent), _ptr(ids), _ptr(values), handle)
+    if other is not None:
+        _used_on(other, stats, targets, top_ids, top_z)
+    return TokenLogprob(logp, lse, ent, ids, values)
+
+
+def token_grad(logits, targets, lse, *, dlogp=None, entropy=None, dentropy=None, vocab_begin: int = 0, scale: float = 1.0, dlogits=None,
+               stream=None):
+    """mist_token_grad: the logits' gradient from those of logp and entropy (fp32 per token; None: zero), with lse and entropy of the
+    whole vocabulary.  dlogits: of the logits' shape and type (it may be the logits; default: a new tensor)."""
+    torch = _torch()
+    L = _lib or load()
+    what = "token log probabilities' gradient"
+    _here(what, logits, lse, dlogp, entropy, dentropy, targets, dlogits)
+    _need(logits.dim() in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    handle, other = _stream_of(torch, stream, logits.device)
+    if dlogits is None:
+        with torch.cuda.stream(other):
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _need(dlogp is None or targets is not None, "%s: dlogp without targets" % what)
+    _need(dentropy is None or entropy is not None, "%s: dentropy without entropy" % what)
+    d = _token_desc(torch, logits, targets, dlogits, vocab_begin, scale, 0)
+    for t, name in ((lse, "lse"), (dlogp, "dlogp"), (entropy, "entropy"), (dentropy, "dentropy")):
+        if t is not None:
+            _packed(what, t, logits.shape[:-1], torch.float32, name)
+    _on_device(torch, logits.device, L.mist_token_grad, ctypes.byref(d), logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(dlogp), _ptr(entropy),
+               _ptr(dentropy), dlogits.data_ptr(), handle)
+    if other is not None:
+        _used_on(other, logits, targets, lse, dlogp, entropy, dentropy, dlogits)
+    return dlogits
+
+
+def token_loss(logits, targets, weights=1.0, *, scale: float = 1.0, dlogits=None, stream=None):
+    """mist_token_loss, a training microbatch in one pass: (logp, dlogits) with dlogits the gradient of the loss
+    -sum(weights * logp).  weights: fp32 per token, or one number (1 / tokens for a mean).  dlogits as in token_grad."""
+    torch = _torch()
+    L = _lib or load()
+    what = "token loss"
+    _no_graph(torch, what, logits)
+    _here(what, logits, targets, dlogits)
+    _need(logits.dim() in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    device, shape = logits.device, logits.shape[:-1]
+    w, factor = (weights, 1.0) if isinstance(weights, torch.Tensor) else (None, float(weights))
+    if w is not None:
+        _here(what, logits, w)
+        _packed(what, w, shape, torch.float32, "weights")
+    handle, other = _stream_of(torch, stream, device)
+    with torch.cuda.stream(other):
+        if dlogits is None:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=device)
+        logp = torch.empty(shape, dtype=torch.float32, device=device)
+    d = _token_desc(torch, logits, targets, dlogits, 0, scale, 0)
+    _on_device(torch, device, L.mist_token_loss, ctypes.byref(d), logits.data_ptr(), targets.data_ptr(), _ptr(w), factor, logp.data_ptr(),
+               dlogits.data_ptr(), handle)
+    if other is not None:
+        _used_on(other, logits, targets, w, dlogits)
+    return logp, dlogits
+
+
+def _block_weights(what, hidden, dtype, weight, bias, post_weight, post_bias) -> None:
+    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"), (post_bias, "post_bias")):
+        if t is not None:
+            _packed(what, t, (hidden,), dtype, name)
+
+
+def _block_gate(what, x, gate, dtype) -> int:
+    """The stride between sequences' gates."""
+    if gate is None:
+        return 0
+    hidden = x.shape[-1]
+    _need(gate.dtype == dtype and (tuple(gate.shape) == (hidden,) or (x.dim() == 3 and tuple(gate.shape) == (x.shape[0], hidden))),
+          "%s: the gate must be [hidden], or [batch, hidden] for [batch, seq, hidden], of the weights' type" % what)
+    _need(hidden <= 1 or gate.stride(-1) == 1, "%s: the last dimension must be contiguous" % what)
+    return gate.stride(0) if gate.dim() == 2 else 0
+
+
+def _block_desc(what, x, block, y, h, weights, gate, kind, eps, res_scale, block_scale):
+    _need(x.dim() in (2, 3), "%s: must be [tokens, hidden] or [batch, seq, hidden]" % what)
+    _need(kind in _BLOCK_KINDS, "%s: kind must be 'rms' or 'layer'" % what)
+    like = block if block is not None else h
+    some = [t for t in (*weights, gate) if t is not None]
+    wtype = some[0].dtype if some else x.dtype
+    _block_weights(what, x.shape[-1], wtype, *weights)
+    strides = []
+    for t in (x, block, y, h):
+        if t is not None:
+            _need(t.shape == x.shape, "%s: the tensors must have one shape" % what)
+        strides.append(0 if t is None else _flat(what, t)[1])
+    _need(y is None or y.dtype == x.dtype, "%s: y must have x's type" % what)
+    _need(block is None or h is None or h.dtype == block.dtype, "%s: h must have the block's type" % what)
+    batch, seq = (x.shape[0], x.shape[1]) if x.dim() == 3 else (1, x.shape[0])
+    return BlockDesc(batch, seq, x.shape[-1], *strides, _block_gate(what, x, gate, wtype), _BLOCK_KINDS[kind],
+                     _type(x if like is None else like, what), _type(x, what), _TYPES.get(wtype, -1), float(eps), float(res_scale), float(block_scale))
+
+
+def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, kind: str = "rms", eps: float = 1e-6,
+               res_scale: float = 1.0, block_scale: float = 1.0, y=None, h=None, dtype=None, stream=None) -> BlockNorm:
+    """mist_block_forward: y = res_scale * x + block_scale * gate * N(block), h = N(y) * weight + bias, and the stats that
+    block_norm_grad takes.  x: [tokens, hidden] or [batch, seq, hidden], the residual, of the block's type or float32; gate: [hidden]
+    or [batch, hidden].  Without post_weight the block's output is not normed; without weight there is no h (None); without
+    block, y is x and h its norm (of dtype, default x's).  y may be x or block."""
+    torch = _torch()
+    L = _lib or load()
+    what = "block norm"
+    _no_graph(torch, what, x, block, weight, bias, post_weight, post_bias, gate)
+    _here(what, x, block, weight, bias, post_weight, post_bias, gate, y, h)
+    handle, other = _stream_of(torch, stream, x.device)
+    _need(block is None or dtype is None or dtype == block.dtype, "block norm: dtype is the block's")
+    _need(block is not None or y is None, "block norm: without a block y is x")
+    _need(weight is not None or h is None, "block norm: h without its weight")
+    with torch.cuda.stream(other):
+        if block is not None and y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if weight is not None and h is None:
+            h = torch.empty(x.shape, dtype=block.dtype if block is not None else dtype or x.dtype, device=x.device)
+        stats = torch.empty(tuple(x.shape[:-1]) + (4,), dtype=torch.float32, device=x.device)
+    d = _block_desc(what, x, block, y, h, (weight, bias, post_weight, post_bias), gate, kind, eps, res_scale, block_scale)
+    _on_device(torch, x.device, L.mist_block_forward, ctypes.byref(d), x.data_ptr(), _ptr(block), _ptr(weight), _ptr(bias), _ptr(post_weight),
+               _ptr(post_bias), _ptr(gate), _ptr(y), _ptr(h), stats.data_ptr(), handle)
+    if other is not None:
+        _used_on(other, x, block, weight, bias, post_weight, post_bias, gate, y, h)
+    return BlockNorm(x if y is None else y, h, stats)
+
+
+def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post_weight=None, post_bias=None, gate=None, kind: str = "rms",
+                    res_scale: float = 1.0, block_scale: float = 1.0, dweight=None, dbias=None, dpost_weight=None, dpost_bias=None, dgate=None,
+                    accumulate: bool = False, dx=None, dblock=None, stream=None):
+    """mist_block_backward: (dx, dblock) from dh and dy (the gradient of y by its other uses; None: none), with y and stats of
+    block_norm and its arguments.  Gradients of weights, biases and gates go to the given tensors of the weights' type
+    (accumulate: added to them).  dx may be dy, dblock may be dh or block; by default they are new."""
+    torch = _torch()
+    L = _lib or load()
+    what = "block norm's gradient"
+    grads = (dweight, dbias, dpost_weight, dpost_bias)
+    _here(what, y, stats, dh, block, dy, weight, post_weight, post_bias, gate, *grads, dgate, dx, dblock)
+    handle, other = _stream_of(torch, stream, y.device)
+    _need(dh is not None or dy is not None, "%s: neither dh nor dy" % what)
+    _need((dh is None) == (weight is None), "%s: dh comes with weight" % what)
+    _need(block is not None or dblock is None, "%s: of a block that is not there" % what)
+    with torch.cuda.stream(other):
+        if dx is None:
+            dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        if block is not None and dblock is None:
+            dblock = torch.empty(block.shape, dtype=block.dtype, device=y.device)
+    d = _block_desc(what, y, block, y, dh, (weight, None, post_weight, post_bias), gate, kind, 0.0, res_scale, block_scale)
+    wtype = next((t.dtype for t in (weight, post_weight, post_bias, gate) if t is not None), y.dtype)
+    _block_weights(what, y.shape[-1], wtype, *grads)
+    dgate_stride = 0
+    if dgate is not None:
+        _need(gate is not None and dgate.shape == gate.shape, "%s: dgate must have the gate's shape" % what)
+        dgate_stride = _block_gate(what, y, dgate, wtype)
+    _packed(what, stats, tuple(y.shape[:-1]) + (4,), torch.float32, "stats")
+    strides = []
+    for t, dtype in ((dh, None if block is None else block.dtype), (dy, y.dtype), (dx, y.dtype), (dblock, None if block is None else block.dtype)):
+        _need(t is None or (t.shape == y.shape and (dtype is None or t.dtype == dtype)), "%s: a gradient must have its tensor's shape and type" % what)
+        strides.append(0 if t is None else _flat(what, t)[1])
+    g = BlockGrads(_ptr(dh), _ptr(dy), _ptr(dx), _ptr(dblock), *(_ptr(t) for t in grads), _ptr(dgate), *strides, dgate_stride, 1 if accumulate else 0)
+    need = ctypes.c_size_t()
+    _check(L, L.mist_block_workspace(ctypes.byref(d), ctypes.byref(g), ctypes.byref(need)))
+    ws = None
+    if need.value:
+        with torch.cuda.stream(other):  # of that stream's pool
+            ws = torch.empty(need.value, dtype=torch.uint8, device=y.device)
+    _on_device(torch, y.device, L.mist_block_backward, ctypes.byref(d), y.data_ptr(), _ptr(block), stats.data_ptr(), _ptr(weight), _ptr(post_weight),
+               _ptr(post_bias), _ptr(gate), ctypes.byref(g), _ptr(ws), need.value, handle)
+    if other is not None:
+        _used_on(other, y, stats, dh, block, dy, weight, post_weight, post_bias, gate, *grads, dgate, dx, dblock)
+    return dx, dblock
+
+
+class Checkpoint:
+    """A tensor kept in 8 bits (mist_kept_store): int8 values and uint8 exponents, a byte for each 128 values of a row, both plain tensors
+    that a program can offload or send.  shape and dtype are the tensor's."""
+
+    def __init__(self, shape, dtype, device="cuda", stream=None):
+        torch = _torch()
+        device = torch.device(device)
+        _need(device.type == "cuda", "checkpoint: must be on a GPU")
+        _need(dtype in _TYPES, "checkpoint: %s is not float32, bfloat16 or float16" % dtype)
+        self.shape, self.dtype = tuple(int(n) for n in shape), dtype
+        _need(len(self.shape) >= 1 and self.shape[-1] >= 1 and min(self.shape) >= 0, "checkpoint: the last dimension must be at least 1")
+        self.rows, self.width = math.prod(self.shape[:-1]), self.shape[-1]
+        groups = -(-self.width // KEPT_GROUP)
+        with torch.cuda.stream(stream):
+            self.values = torch.empty(self.rows, groups * KEPT_GROUP, dtype=torch.int8, device=device)
+            self.exponents = torch.empty(self.rows, groups, dtype=torch.uint8, device=device)
+
+    def kept(self, what, device) -> Kept:
+        torch = _torch()
+        groups = -(-self.width // KEPT_GROUP)
+        _need(self.values.device == device and self.exponents.device == device, "%s: the tensors must be on one GPU" % what)
+        _packed(what, self.values, (self.rows, groups * KEPT_GROUP), torch.int8, "a checkpoint's values")
+        _packed(what, self.exponents, (self.rows, groups), torch.uint8, "a checkpoint's exponents")
+        return Kept(self.values.data_ptr(), self.exponents.data_ptr())
+
+
+def _checkpoint_for(what, t, given, other) -> Checkpoint:
+    if given is None:
+        return Checkpoint(t.shape, t.dtype, t.device, other)
+    _need(isinstance(given, Checkpoint) and given.shape == tuple(t.shape) and given.dtype == t.dtype, "%s: a checkpoint of another shape or type" % what)
+    return given
+
+
+def checkpoint_store(x, checkpoint: Checkpoint | None = None, *, stream=None) -> Checkpoint:
+    """mist_kept_store: x (its last dimension contiguous, the others rows at one stride) in 8 bits, into a checkpoint of its shape and
+    type or a new one."""
+    torch = _torch()
+    L = _lib or load()
+    what = "checkpoint"
+    _no_graph(torch, what, x)
+    _here(what, x)
+    handle, other = _stream_of(torch, stream, x.device)
+    rows, stride = _flat(what, x)
+    c = _checkpoint_for(what, x, checkpoint, other)
+    k = c.kept(what, x.device)
+    d = KeptDesc(rows, c.width, stride, _type(x, what))
+    _on_device(torch, x.device, L.mist_kept_store, ctypes.byref(d), x.data_ptr(), k.values, k.exponents, handle)
+    if other is not None:
+        _used_on(other, x, c.values, c.exponents)
+    return c
+
+
+def checkpoint_load(checkpoint: Checkpoint, *, out=None, dtype=None, stream=None):
+    """mist_kept_load: the kept values, in out or a new tensor (of dtype, default the stored tensor's)."""
+    torch = _torch()
+    L = _lib or load()
+    what = "checkpoint"
+    device = checkpoint.values.device
+    _need(device.type == "cuda", "checkpoint: the tensors must be on one GPU")
+    handle, other = _stream_of(torch, stream, device)
+    if out is None:
+        with torch.cuda.stream(other):
+            out = torch.empty(checkpoint.shape, dtype=dtype or checkpoint.dtype, device=device)
+    _need(tuple(out.shape) == checkpoint.shape and (dtype is None or out.dtype == dtype), "%s: out must have the checkpoint's shape" % what)
+    _need(out.device == device, "%s: the tensors must be on one GPU" % what)
+    k = checkpoint.kept(what, device)
+    rows, stride = _flat(what, out)
+    d = KeptDesc(rows, checkpoint.width, stride, _type(out, what))
+    _on_device(torch, device, L.mist_kept_load, ctypes.byref(d), k.values, k.exponents, out.data_ptr(), handle)
+    if other is not None:
+        _used_on(other, checkpoint.values, checkpoint.exponents, out)
+    return out
+
+
+def mlp_act(up, gate=None, *, kind: str = "silu", save=False, out=None, stream=None) -> MlpAct:
+    """mist_act_forward: act(gate) * up, or act(up) without a gate (kind 'silu' or 'gelu').  save: True keeps up and gate in 8 bits in new checkpoints,
+    a pair (up's, gate's) in these; the result's up and gate are the checkpoints, for mlp_act_grad.  out may be up or gate."""
+    torch = _torch()
+    L = _lib or load()
+    what = "activation"
+    _no_graph(torch, what, up, gate)
+    _here(what, up, gate, out)
+    _need(kind in _ACTS, "activation: kind must be 'silu' or 'gelu'")
+    handle, other = _stream_of(torch, stream, up.device)
+    _need(up.dim() >= 1 and up.shape[-1] >= 1, "activation: the last dimension must be at least 1")
+    _need(gate is None or (gate.shape == up.shape and gate.dtype == up.dtype), "activation: gate must have up's shape and type")
+    if out is None:
+        with torch.cuda.stream(other):
+            out = torch.empty(up.shape, dtype=up.dtype, device=up.device)
+    _need(out.shape == up.shape and out.dtype == up.dtype, "activation: out must have up's shape and type")
+    keep = (None, None)
+    if save:
+        pair = (None, None) if save is True else save
+        _need(len(pair) == 2, "activation: save must be a bool or (up's checkpoint, gate's or None)")
+        keep = (_checkpoint_for(what, up, pair[0], other), None if gate is None else _checkpoint_for(what, gate, pair[1], other))
+    rows, stride = _flat(what, up)
+    d = ActDesc(rows, up.shape[-1], stride, 0 if gate is None else _flat(what, gate)[1], _flat(what, out)[1], 0, _type(up, what), _ACTS[kind])
+    k = [None if c is None else ctypes.byref(c.kept(what, up.device)) for c in keep]
+    _on_device(torch, up.device, L.mist_act_forward, ctypes.byref(d), up.data_ptr(), _ptr(gate), out.data_ptr(), k[0], k[1], handle)
+    if other is not None:
+        _used_on(other, up, gate, out, *(t for c in keep if c is not None for t in (c.values, c.exponents)))
+    return MlpAct(out, *keep)
+
+
+def mlp_act_grad(dout, up: Checkpoint, gate: Checkpoint | None = None, *, kind: str = "silu", dup=None, dgate=None, out=None, stream=None):
+    """mist_act_backward: (dup, dgate) from the activation's gradient and the kept up and gate.  out, where given, receives the activation
+    formed again from them (for the gradient of the projection after it).  dup or dgate may be dout."""
+    torch = _torch()
+    L = _lib or load()
+    what = "activation's gradient"
+    _here(what, dout, dup, dgate, out)
+    _need(kind in _ACTS, "activation: kind must be 'silu' or 'gelu'")
+    _need(isinstance(up, Checkpoint) and (gate is None or isinstance(gate, Checkpoint)), "%s: up and gate must be checkpoints" % what)
+    _need(up.shape == tuple(dout.shape) and (gate is None or gate.shape == up.shape), "%s: a checkpoint of another shape" % what)
+    _need(gate is not None or dgate is None, "%s: of a gate that is not there" % what)
+    handle, other = _stream_of(torch, stream, dout.device)
+    with torch.cuda.stream(other):
+        if dup is None:
+            dup = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+        if gate is not None and dgate is None:
+            dgate = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+    for t in (dup, dgate, out):
+        _need(t is None or (t.shape == dout.shape and t.dtype == dout.dtype), "%s: an output must have dout's shape and type" % what)
+    rows, stride = _flat(what, dout)
+    d = ActDesc(rows, up.width, _flat(what, dup)[1], 0 if gate is None else _flat(what, dgate)[1], stride, 0 if out is None else _flat(what, out)[1],
+                _type(dout, what), _ACTS[kind])
+    k = up.kept(what, dout.device), None if gate is None else gate.kept(what, dout.device)
+    _on_device(torch, dout.device, L.mist_act_backward, ctypes.byref(d), ctypes.byref(k[0]), None if k[1] is None else ctypes.byref(k[1]),
+               dout.data_ptr(), dup.data_ptr(), _ptr(dgate), _ptr(out), handle)
+    if other is not None:
+        _used_on(other, dout, dup, dgate, out, *(t for c in (up, gate) if c is not None for t in (c.values, c.exponents)))
+    return dup, dgate

@@ -1,0 +1,397 @@
+"""Token log probabilities, entropies, alternatives, their gradient and the loss on the GPU against the definition in 64 bits.
+
+Tolerances, fixed before the first run.  u = 2^-24, U the output type's unit roundoff, p the probabilities, d = z - max z.  A
+sum over a row is of at least 64 shares: chains of at most rows / 64 + 30 additions.  An exponential is off by
+3 |d| u from its argument (two products, one sum) and 2^-22 of itself.
+  s:        relative E = (rows / 64 + 30) u + 3 u sum p |d| + 2^-22
+  lse:      E + 2^-23 (|m| + |lse|) + 2^-23
+  logp:     that + 2^-23 (|z| + |logp|)
+  entropy:  E (1 + 2 sum p |d|) + (rows / 64 + 34) u sum p |d| + 3 u sum p d^2 + 2^-22 (1 + sum p |d|)
+  gradient: with l = log p: p (|c0| + |c1 l|) (e + 2^-22 (2 + |l|)) + p |c1| (e + 2^-22 |l|) + 2^-22 |up| + 2^-126 (|c0| + |c1 l|) (a p below 2^-126
+            is 0 in the instruction's result: all of p (c0 + c1 l), l down to -104, is lost) + U |x| + tiny, where e is the
+            lse's error and c0, c1, up the row's factors (c0's own error 2^-22 (|dlogp| + |dentropy entropy|) + that of the entropy)
+"""
+import math
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+TINY = {"bf16": 2.0 ** -134, "f16": 2.0 ** -25, "f32": 2.0 ** -150}
+U24 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "a GPU is required"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+def types(torch):
+    return {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+class Truth:
+    """The definition on [tokens, rows] logits in 64 bits, and what the kernels may be off by."""
+
+    def __init__(self, torch, logits, targets, scale):
+        x = logits.double().reshape(-1, logits.shape[-1])
+        t = targets.reshape(-1).long()
+        self.n, rows = x.shape
+        z = x * scale
+        self.z = z
+        m = z.amax(-1)
+        self.nothing = m == -math.inf
+        d = z - torch.where(self.nothing, 0.0, m)[:, None]
+        s = d.exp().sum(-1)
+        self.lse = torch.where(self.nothing, -math.inf, m + s.log())
+        self.l = z - torch.where(self.nothing, 0.0, self.lse)[:, None]
+        self.p = torch.where(self.nothing[:, None], 0.0, self.l.exp())
+        at0 = self.p == 0
+        pd = torch.where(at0, 0.0, self.p * d.abs())
+        R, R2 = pd.sum(-1), torch.where(at0, 0.0, self.p * d * d).sum(-1)
+        self.entropy = -torch.where(at0, 0.0, self.p * self.l).sum(-1)
+        here = (t >= 0) & (t < rows)
+        self.t, self.here = t, here
+        self.zt = torch.where(here, z.gather(1, t.clamp(0, rows - 1)[:, None])[:, 0], -math.inf)
+        self.logp = torch.where(t < 0, 0.0, torch.where(self.zt == -math.inf, -math.inf, self.zt - self.lse))
+        E = (rows / 64 + 30) * U24 + 3 * U24 * R + 2.0 ** -22
+        f = lambda v: torch.nan_to_num(v.abs(), posinf=0.0)  # noqa: E731
+        self.e_lse = E + 2.0 ** -23 * (f(m) + f(self.lse) + 1)
+        self.e_logp = self.e_lse + 2.0 ** -23 * (f(self.zt) + f(self.logp))
+        self.e_entropy = E * (1 + 2 * R) + (rows / 64 + 34) * U24 * R + 3 * U24 * R2 + 2.0 ** -22 * (1 + R)
+
+    def grad(self, torch, dlogp, dentropy, scale, kind):
+        """The gradient and its tolerance; kind: the output's type."""
+        dl = torch.where((self.t >= 0) & ~self.nothing, dlogp.double().reshape(-1), 0.0)
+        de = torch.where(self.nothing, 0.0, dentropy.double().reshape(-1))
+        c0, c1 = scale * (-dl - de * self.entropy), scale * -de
+        l = torch.where(self.p == 0, 0.0, self.l)
+        x = self.p * (c0[:, None] + c1[:, None] * l)
+        at = self.t.clamp(0, x.shape[1] - 1)[:, None]
+        up = torch.where(self.here, scale * dl, 0.0)[:, None]
+        x.scatter_add_(1, at, up)
+        a0 = (scale * (dl.abs() + (de * self.entropy).abs()))[:, None]
+        a1, e = c1.abs()[:, None], self.e_lse[:, None]
+        slack = self.p * (a0 + a1 * l.abs()) * (e + 2.0 ** -22 * (2 + l.abs())) + self.p * a1 * (e + 2.0 ** -22 * l.abs())
+        slack += self.p * (2.0 ** -22 * a0 + a1 * self.e_entropy[:, None]) + 2.0 ** -126 * (a0 + a1 * l.abs())
+        slack.scatter_add_(1, at, 2.0 ** -22 * up.abs())
+        return x, slack + UNIT[kind] * x.abs() + TINY[kind]
+
+
+def within(got, want, slack, what):
+    got = got.double().reshape(want.shape)
+    same = (got == want) | (got.isnan() & want.isnan())
+    bad = ~(same | ((got - want).abs() <= slack))
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:3].tolist(), got[bad][:3].tolist(), want[bad][:3].tolist())
+
+
+def alternatives(torch, logits, top):
+    """Ids by logit, lower first among equals, without those of -inf."""
+    x = logits.float().reshape(-1, logits.shape[-1])
+    order = torch.sort(x, dim=-1, descending=True, stable=True)
+    ids = torch.full((x.shape[0], top), -1, device=x.device, dtype=torch.int32)
+    k = min(top, x.shape[1])
+    ids[:, :k] = torch.where(order.values[:, :k] == -math.inf, -1, order.indices[:, :k]).int()
+    return ids
+
+
+def inputs(torch, batch, seq, rows, kind, look, seed=0):
+    g = torch.Generator("cuda").manual_seed(seed + rows)
+    x = torch.empty(batch, seq, rows, device="cuda").normal_(0.0, 3.0, generator=g)
+    t = torch.randint(0, rows, (batch, seq), device="cuda", generator=g)
+    if look == "masked":
+        x[torch.rand(x.shape, device="cuda", generator=g) < 0.7] = -math.inf
+    elif look == "half":
+        x[..., rows // 3:] = -math.inf
+    elif look == "nothing":
+        x[:, ::2] = -math.inf
+    elif look == "lowest":
+        x[..., ::2] = torch.finfo(types(torch)[kind]).min
+    elif look == "equal":
+        x.fill_(0.5)
+    elif look == "ascending":
+        x = torch.linspace(-20, 20, rows, device="cuda").expand(batch, seq, rows).contiguous()
+    elif look == "peaked":
+        x.scatter_(2, t[..., None], 60.0)
+    elif look == "signed zeros":
+        x = torch.where(x > 0, 0.0, -0.0)
+    if look != "text":
+        t[torch.rand(t.shape, device="cuda", generator=g) < 0.2] = -1
+        t[torch.rand(t.shape, device="cuda", generator=g) < 0.1] = -100
+    return x.to(types(torch)[kind]), t
+
+
+SHAPES = [(1, 1, 1), (2, 3, 2), (1, 5, 63), (3, 2, 64), (1, 7, 100), (2, 9, 511), (1, 4, 513), (2, 3, 1000), (1, 3, 4095), (1, 3, 4097),
+          (2, 2, 8193), (1, 3, 16384), (1, 2, 16391), (2, 5, 32000), (1, 3, 50257), (1, 2, 65537), (1, 1, 131073), (1, 2, 262147)]
+LOOKS = ["text", "masked", "half", "nothing", "lowest", "equal", "ascending", "peaked", "signed zeros"]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("look", LOOKS)
+def test_logprob(torch, shape, kind, look):
+    from paper_2503_19050_amd import mist
+    say("logprob", shape, kind, look)
+    logits, t = inputs(torch, *shape, kind, look)
+    scale = 1.0 if look in ("text", "lowest") else 0.75
+    top = {0: 1, 1: 5, 2: 20, 3: 64}[shape[2] % 4]
+    r = mist.token_logprob(logits, t, scale=scale, entropy=True, top=top)
+    w = Truth(torch, logits, t, scale)
+    within(r.lse, w.lse, w.e_lse, "lse")
+    within(r.logp, w.logp, w.e_logp, "logp")
+    within(r.entropy, w.entropy, w.e_entropy, "entropy")
+    ids = alternatives(torch, logits, top)
+    assert torch.equal(r.top_ids.reshape(ids.shape), ids)
+    z = torch.where(ids >= 0, w.z.gather(1, ids.clamp(min=0).long()), -math.inf)
+    want = torch.where(ids >= 0, z - w.lse[:, None], -math.inf)
+    within(r.top_logp, want, (w.e_lse[:, None] + 2.0 ** -22 * (z.abs() + want.abs())).nan_to_num(posinf=0.0), "top_logp")
+    few = mist.token_logprob(logits, scale=scale)
+    assert few.logp is None and few.entropy is None and few.top_ids is None and torch.equal(few.lse, r.lse)
+    again = mist.token_logprob(logits, t, scale=scale, entropy=True, top=top)
+    assert all(torch.equal(a, b) for a, b in zip(r, again))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("look", LOOKS)
+def test_loss_and_gradient(torch, shape, kind, look):
+    from paper_2503_19050_amd import mist
+    say("loss", shape, kind, look)
+    logits, t = inputs(torch, *shape, kind, look, seed=1)
+    g = torch.Generator("cuda").manual_seed(3)
+    weights = torch.rand(t.shape, device="cuda", generator=g)
+    scale = 1.0 if look in ("text", "lowest") else 1.25
+    w = Truth(torch, logits, t, scale)
+    logp, d = mist.token_loss(logits, t, weights, scale=scale)
+    within(logp, w.logp, w.e_logp, "logp")
+    want, slack = w.grad(torch, -weights, torch.zeros_like(weights), scale, kind)
+    within(d, want, slack, "dlogits")
+    # in place, and one weight for all
+    x = logits.clone()
+    logp2, same = mist.token_loss(x, t, 0.25, scale=scale, dlogits=x)
+    assert same is x and torch.equal(logp2, logp)
+    want, slack = w.grad(torch, torch.full_like(weights, -0.25), torch.zeros_like(weights), scale, kind)
+    within(x, want, slack, "in place")
+    r = mist.token_logprob(logits, t, scale=scale, entropy=True)
+    dlogp, dentropy = torch.empty_like(weights).normal_(generator=g), torch.empty_like(weights).normal_(generator=g)
+    d = mist.token_grad(logits, t, r.lse, dlogp=dlogp, entropy=r.entropy, dentropy=dentropy, scale=scale)
+    want, slack = w.grad(torch, dlogp, dentropy, scale, kind)
+    within(d, want, slack, "gradient")
+    x = logits.clone()
+    assert torch.equal(mist.token_grad(x, t, r.lse, dlogp=dlogp, entropy=r.entropy, dentropy=dentropy, scale=scale, dlogits=x), d)
+    only = mist.token_grad(logits, None, r.lse, entropy=r.entropy, dentropy=dentropy, scale=scale)
+    want, slack = w.grad(torch, torch.zeros_like(dlogp), dentropy, scale, kind)
+    within(only, want, slack, "entropies alone")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, ranks", [(1000, 2), (32000, 8), (1001, 3), (5, 5), (50257, 4)])
+def test_shards_give_what_the_whole_gives(torch, rows, ranks, kind):
+    from paper_2503_19050_amd import mist
+    say("shards", rows, ranks, kind)
+    logits, t = inputs(torch, 2, 5, rows, kind, "masked", seed=5)
+    logits[0, 1, : -(-rows // ranks)] = -math.inf   # a rank without a visible logit
+    logits[0, 2] = -math.inf
+    w = Truth(torch, logits, t, 0.9)
+    per, top = -(-rows // ranks), 7
+    stats = torch.empty(ranks, 2, 5, 4, device="cuda")
+    parts = [mist.token_part(logits[..., k * per:(k + 1) * per], t, vocab_begin=k * per, scale=0.9, top=top, stats=stats[k]) for k in range(ranks)]
+    r = mist.token_join(stats, t, entropy=True, top_ids=torch.stack([p.top_ids for p in parts]), top_z=torch.stack([p.top_z for p in parts]))
+    within(r.lse, w.lse, 2 * w.e_lse, "lse")       # joined: one more rounding of each rank's share
+    within(r.logp, w.logp, 2 * w.e_logp, "logp")
+    within(r.entropy, w.entropy, 2 * w.e_entropy, "entropy")
+    assert torch.equal(r.top_ids.reshape(-1, top), alternatives(torch, logits, top))
+    one = mist.token_logprob(logits, t, scale=0.9, top=top)
+    assert torch.allclose(r.top_logp.nan_to_num(neginf=-1e4), one.top_logp.nan_to_num(neginf=-1e4), rtol=1e-5, atol=1e-5)
+    g = torch.Generator("cuda").manual_seed(3)
+    dlogp, dentropy = torch.empty(2, 5, device="cuda").normal_(generator=g), torch.empty(2, 5, device="cuda").normal_(generator=g)
+    want, slack = w.grad(torch, dlogp, dentropy, 0.9, kind)
+    for k in range(ranks):
+        at = slice(k * per, (k + 1) * per)
+        d = mist.token_grad(logits[..., at], t, r.lse, dlogp=dlogp, entropy=r.entropy, dentropy=dentropy, vocab_begin=k * per, scale=0.9)
+        within(d, want[:, at].reshape(d.shape), 2 * slack[:, at].reshape(d.shape), "rank %d" % k)
+    plain = mist.token_join(stats, entropy=False)
+    assert plain.logp is None and plain.entropy is None and plain.top_ids is None and torch.equal(plain.lse, r.lse)
+
+
+def test_gradient_against_differences(torch):
+    """Of sum(a logp + b entropy), by central differences of the definition in 64 bits."""
+    from paper_2503_19050_amd import mist
+    logits, t = inputs(torch, 1, 4, 9, "f32", "text")
+    a, b = torch.tensor([[1.0, -2.0, 0.5, 3.0]], device="cuda"), torch.tensor([[0.3, 0.0, -1.0, 2.0]], device="cuda")
+    r = mist.token_logprob(logits, t, entropy=True, scale=0.7)
+    d = mist.token_grad(logits, t, r.lse, dlogp=a, entropy=r.entropy, dentropy=b, scale=0.7)
+
+    def value(x):
+        l = torch.log_softmax(x * 0.7, -1)
+        return (a.double() * l.gather(-1, t[..., None])[..., 0] - b.double() * (l.exp() * l).sum(-1)).sum()
+
+    x = logits.double()
+    for i in range(4):
+        for j in range(9):
+            e = torch.zeros_like(x)
+            e[0, i, j] = 1e-5
+            assert abs(float((value(x + e) - value(x - e)) / 2e-5) - float(d[0, i, j])) < 1e-5
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_logits_that_are_no_numbers(torch, bad):
+    """A row with NaN or +inf gives NaN, and only it; padding and tokens without weight get no gradient from it."""
+    from paper_2503_19050_amd import mist
+    for rows in (7, 5000, 70000):
+        logits, t = inputs(torch, 1, 5, rows, "f32", "text")
+        logits[0, 1, rows // 2] = bad
+        logits[0, 3] = bad
+        t[0, 3] = -1
+        r = mist.token_logprob(logits, t, entropy=True, top=2)
+        assert r.lse.isnan().tolist() == [[False, True, False, True, False]] and r.entropy.isnan().tolist() == r.lse.isnan().tolist()
+        assert r.logp.isnan().tolist() == [[False, True, False, False, False]] and float(r.logp[0, 3]) == 0.0
+        assert int(r.top_ids[0, 1, 0]) == rows // 2 and r.top_ids[0, 3].tolist() == [0, 1]
+        _, d = mist.token_loss(logits, t, 1.0)
+        assert d[0, 1].isnan().all() and (d[0, 3] == 0).all() and d[0, [0, 2, 4]].isfinite().all()
+        d = mist.token_grad(logits, t, r.lse, dlogp=torch.ones(1, 5, device="cuda"))
+        assert d[0, 1].isnan().all() and (d[0, 3] == 0).all() and d[0, [0, 2, 4]].isfinite().all()
+
+
+def test_all_nan(torch):
+    from paper_2503_19050_amd import mist
+    x = torch.full((1, 2, 300), float("nan"), device="cuda")
+    r = mist.token_logprob(x, torch.zeros(1, 2, dtype=torch.int64, device="cuda"), entropy=True)
+    assert r.lse.isnan().all() and r.logp.isnan().all() and r.entropy.isnan().all()
+
+
+def test_targets_of_no_one(torch):
+    """An id past the vocabulary has no probability: -inf, and a gradient of the others alone."""
+    from paper_2503_19050_amd import mist
+    logits, t = inputs(torch, 1, 3, 50, "f32", "text")
+    t[0, 1] = 50
+    t[0, 2] = 2 ** 40
+    logp, d = mist.token_loss(logits, t, 1.0)
+    assert logp[0, 0].isfinite() and (logp[0, 1:] == -math.inf).all()
+    assert abs(float(d[0, 0].sum())) < 1e-5 and abs(float(d[0, 1].sum()) - 1) < 1e-5
+    assert torch.equal(mist.token_logprob(logits, t).logp, logp)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_strides(torch, kind):
+    """Views: without a last position, sequences inside positions, rows off alignment, shared rows; what lies between is left as it was."""
+    from paper_2503_19050_amd import mist
+    T = types(torch)[kind]
+    whole, t = inputs(torch, 3, 6, 1003, kind, "text")
+    for x in (whole[:, :-1], whole.transpose(0, 1).contiguous().transpose(0, 1)[:, :-1], whole[:, 1:, 1:-1],
+              whole[:1, :5].expand(3, 5, 1003), whole[:, :1].expand(3, 5, 1003)):
+        wide = torch.cat([t, t], 1).int()
+        targets = wide[:, 2:7] % x.shape[-1]
+        solid = x.contiguous()
+        r, want = mist.token_logprob(x, targets, entropy=True, top=3), mist.token_logprob(solid, targets.contiguous(), entropy=True, top=3)
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+        room = torch.full((3, 7, x.shape[-1] + 5), 7.0, device="cuda", dtype=T)
+        out = room[:, 1:6, 2:-3]
+        logp, _ = mist.token_loss(x, targets, 0.5, dlogits=out)
+        logp2, d = mist.token_loss(solid, targets.contiguous(), 0.5)
+        assert torch.equal(logp, logp2) and torch.equal(out, d)
+        out.fill_(7.0)
+        assert bool((room == 7.0).all())
+        mist.token_grad(x, targets, r.lse, dlogp=logp, dlogits=out)
+        assert torch.equal(out, mist.token_grad(solid, targets.contiguous(), r.lse, dlogp=logp))
+        out.fill_(7.0)
+        assert bool((room == 7.0).all())
+
+
+def test_nothing_to_do(torch):
+    from paper_2503_19050_amd import mist
+    for shape in ((0, 3, 10), (2, 0, 10)):
+        x, t = torch.zeros(shape, device="cuda"), torch.zeros(shape[:2], device="cuda", dtype=torch.int64)
+        r = mist.token_logprob(x, t, entropy=True, top=2)
+        assert r.logp.shape == shape[:2] and r.top_ids.shape == shape[:2] + (2,)
+        assert mist.token_loss(x, t)[1].shape == shape
+        assert mist.token_join(torch.zeros((2,) + shape[:2] + (4,), device="cuda"), t).lse.shape == shape[:2]
+
+
+def test_sequences_without_a_batch(torch):
+    from paper_2503_19050_amd import mist
+    x, t = inputs(torch, 1, 6, 300, "bf16", "text")
+    a, b = mist.token_logprob(x, t, entropy=True, top=2), mist.token_logprob(x[0], t[0], entropy=True, top=2)
+    assert all(torch.equal(p[0], q) for p, q in zip(a, b))
+
+
+def test_large_offsets(torch):
+    """Logits past 2^31 elements: the last rows and the first are those of small calls."""
+    from paper_2503_19050_amd import mist
+    n, rows = 34000, 65537   # 2.2e9
+    x = torch.zeros(1, n, rows, device="cuda", dtype=torch.bfloat16)
+    at = [0, n // 2, n - 1]
+    g = torch.Generator("cuda").manual_seed(1)
+    x[0, at] = torch.empty(3, rows, device="cuda").normal_(0, 2, generator=g).bfloat16()
+    t = torch.full((1, n), rows - 1, device="cuda", dtype=torch.int64)
+    small, ts = x[:, at].clone(), t[:, at].clone()
+    r, want = mist.token_logprob(x, t, top=1), mist.token_logprob(small, ts, top=1)
+    assert torch.equal(r.logp[:, at], want.logp) and torch.equal(r.top_ids[:, at], want.top_ids)
+    assert abs(float(r.lse[0, 1]) - math.log(rows)) < 1e-5
+    logp, d = mist.token_loss(x, t, 1.0, dlogits=x)
+    logp2, d2 = mist.token_loss(small, ts, 1.0)
+    assert torch.equal(logp[:, at], logp2) and torch.equal(d[:, at], d2)
+
+
+def test_streams_and_graphs(torch):
+    """A run of the operators on another stream, and captured: replays with new inputs and eager work between give the eager results."""
+    from paper_2503_19050_amd import mist
+    x, t = inputs(torch, 2, 40, 5003, "bf16", "text")
+    w = torch.rand(2, 40, device="cuda")
+
+    def work(stream=None):
+        r = mist.token_logprob(x, t, entropy=True, top=4, stream=stream)
+        stats = mist.token_part(x, t, vocab_begin=0, stream=stream).stats
+        j = mist.token_join(stats[None], t, entropy=True, stream=stream)
+        logp, d = mist.token_loss(x, t, w, stream=stream)
+        return [*r, j.lse, j.logp, j.entropy, logp, d, mist.token_grad(x, t, r.lse, dlogp=w, entropy=r.entropy, dentropy=w, stream=stream)]
+
+    want = work()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for s in (side, side.cuda_stream):
+        got = work(s)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work()
+    for k in range(4):
+        x.copy_(inputs(torch, 2, 40, 5003, "bf16", "masked" if k == 1 else "text", seed=k)[0])
+        graph.replay()
+        torch.randn(1 << 20, device="cuda").sum().item()
+        want = work()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+def test_refusals(torch):
+    from paper_2503_19050_amd import mist
+    x, t = inputs(torch, 2, 4, 30, "f32", "text")
+    f = torch.zeros(2, 4, device="cuda")
+    big = torch.zeros(2, 4, 31, device="cuda")
+    bad = [lambda: mist.token_logprob(x, t.float()), lambda: mist.token_logprob(x, t[:, :3]), lambda: mist.token_logprob(x.double(), t),
+           lambda: mist.token_logprob(x, t, scale=0.0), lambda: mist.token_logprob(x, t, scale=float("inf")), lambda: mist.token_logprob(x, t, top=65),
+           lambda: mist.token_logprob(x, t, top=-1), lambda: mist.token_logprob(x.transpose(1, 2), t), lambda: mist.token_logprob(x, t.cpu()),
+           lambda: mist.token_logprob(x[0, 0], t[0, 0]), lambda: mist.token_logprob(x, t.t().contiguous().t()),
+           lambda: mist.token_logprob(torch.zeros(2, 4, 0, device="cuda"), t),
+           lambda: mist.token_loss(x, t, f.double()), lambda: mist.token_loss(x, t, f[:, :3]), lambda: mist.token_loss(x, t, float("nan")),
+           lambda: mist.token_loss(x, t, dlogits=x.half()), lambda: mist.token_loss(big[..., :-1], t, dlogits=big[..., 1:]),
+           lambda: mist.token_loss(x, t, dlogits=x[:1].expand(2, 4, 30)),
+           lambda: mist.token_part(x, t, vocab_begin=-1), lambda: mist.token_part(x, t, vocab_begin=2 ** 31 - 5),
+           lambda: mist.token_part(x, t, vocab_begin=0, stats=f), lambda: mist.token_join(f, t), lambda: mist.token_join(torch.zeros(0, 2, 4, 4, device="cuda"), t),
+           lambda: mist.token_join(torch.zeros(1, 2, 4, 4, device="cuda"), t, top_ids=t.int()),
+           lambda: mist.token_grad(x, None, f, dlogp=f), lambda: mist.token_grad(x, t, f, dentropy=f), lambda: mist.token_grad(x, t, f.double()),
+           lambda: mist.token_logprob(x.clone().requires_grad_(), t)]
+    for k, call in enumerate(bad):
+        with pytest.raises(mist.MistError) as e:
+            call()
+        assert e.value.status == -1 and str(e.value), k
