@@ -64,16 +64,28 @@ __device__ __forceinline__ void store8(T* p, int64_t left, Float8 x) {
     if (k < left) p[k] = (T)x[k];
 }
 
-// Sum, or largest, over a wave; every lane has the result.
+// Sum, or largest, over a wave; every lane has the result.  Exchanges within 16 lanes are operands of the additions
+// themselves, those of halves and quarters of the wave two instructions: no trip through shared memory.
+template <int CTRL>
+__device__ __forceinline__ float lanes(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+template <class J>
+__device__ __forceinline__ float wave_join(float x, J join) {
+  x = join(x, lanes<0xB1>(x));   // pairs
+  x = join(x, lanes<0x4E>(x));   // fours
+  x = join(x, lanes<0x141>(x));  // eights: mirrored
+  x = join(x, lanes<0x140>(x));  // sixteens: mirrored
+  const auto q = __builtin_amdgcn_permlane16_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
+  x = join(__int_as_float((int)q[0]), __int_as_float((int)q[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
+  return join(__int_as_float((int)h[0]), __int_as_float((int)h[1]));
+}
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+  return wave_join(x, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
+  return wave_join(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // exp(x) by the base-2 instruction: off by 2^-24 |x| from the product and 1 ulp from the instruction.

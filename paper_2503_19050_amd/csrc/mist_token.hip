@@ -74,74 +74,290 @@ __device__ __forceinline__ float logp_of(float z, float lse, int64_t target) {
   return target < 0 ? 0.0f : z == -HUGE_VALF && !(lse != lse) ? z : z - lse;
 }
 
-template <class F, class J>
-__device__ __forceinline__ float block_join(float x, F wave, J join) {
-  __shared__ float part[kThreads / 64];
-  x = wave(x);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
-  __syncthreads();
-  x = part[0];
-  for (int k = 1; k < kThreads / 64; ++k) x = join(x, part[k]);
-  return x;
-}
-__device__ __forceinline__ float block_sum(float x) { return block_join(x, [](float v) { return wave_sum(v); }, [](float p, float q) { return p + q; }); }
-__device__ __forceinline__ float block_max(float x) { return block_join(x, [](float v) { return wave_max(v); }, [](float p, float q) { return fmaxf(p, q); }); }
-
-// m, s and u of a row; every thread has them.
-template <class T>
-__device__ Stats row_stats(const TokenArgs& a, const T* x) {
-  float m = -HUGE_VALF;
-  for (int64_t j = threadIdx.x; j < a.rows; j += kThreads) m = fmaxf(m, (float)x[j]);
-  m = block_max(m) * a.scale;
-  const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
-  float s = 0.0f, u = 0.0f;
-  for (int64_t j = threadIdx.x; j < a.rows; j += kThreads) {
-    const float d = fmaf((float)x[j], a.scale, -from), e = fast_exp(d);
-    s += e;
-    u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
+// A block's sums and largest values: joined over its waves through two places in turn, so that a wave writes one only after
+// every wave has read its last values.
+template <int WAVES>
+struct Join {
+  float2 (*part)[WAVES];
+  int turn;
+  __device__ __forceinline__ float2 get(float a, float b) {
+    float2* p = part[turn];
+    turn ^= 1;
+    if (threadIdx.x % 64 == 0) p[threadIdx.x / 64] = float2{a, b};
+    __syncthreads();
+    return float2{0.0f, 0.0f};
   }
-  return Stats{m, block_sum(s), block_sum(u), 0.0f};
+  __device__ __forceinline__ float2 sum(float a, float b) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if (WAVES == 1) return float2{a, b};
+    const float2* p = part[turn];
+    get(a, b);
+    float2 s = p[0];
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) s.x += p[k].x, s.y += p[k].y;
+    return s;
+  }
+  template <class J>
+  __device__ __forceinline__ float of_waves(float x, J join) {
+    if (WAVES == 1) return x;
+    const float2* p = part[turn];
+    get(x, 0.0f);
+    x = p[0].x;
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) x = join(x, p[k].x);
+    return x;
+  }
+};
+
+// A chunk of a row in the registers of its block: N vectors of 16 bytes a thread, in turn over the threads, and what is
+// left over a whole vector, one value a thread.  What is not there is -inf.  The values stay in their type between the passes over
+// them (the empty assembly keeps the compiler from holding them converted, which takes twice the registers of 16-bit values).
+typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+
+template <class T, int THREADS, int N>
+struct Chunk {
+  static constexpr int kV = 16 / sizeof(T), kAll = THREADS * N * kV;
+  typedef T V __attribute__((ext_vector_type(kV)));
+  typedef typename mist::Vec<T, kV>::type Anywhere;
+  Raw v[N];
+  float last;
+  __device__ __forceinline__ static int place(int j) {
+    int at = threadIdx.x;
+    asm("" : "+v"(at));  // formed anew where it is used, rather than N of them held
+    return (j * THREADS + at) * kV;
+  }
+  __device__ __forceinline__ static int last_place(int n) { return n / kV * kV + (int)threadIdx.x; }
+  __device__ __forceinline__ void load(const T* x, int n) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      V r = (T)-HUGE_VALF;
+      const int at = place(j);
+      if (at + kV <= n) r = *(const Anywhere*)(x + (uint32_t)at);
+      v[j] = __builtin_bit_cast(Raw, r);
+    }
+    last = last_place(n) < n ? (float)x[last_place(n)] : -HUGE_VALF;
+  }
+  // f(value, its place in the chunk); whole vectors that no thread has are passed over
+  template <class F>
+  __device__ __forceinline__ void each(int n, F&& f) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (j * THREADS * kV >= n) continue;
+      asm("" : "+v"(v[j]));
+      const V r = __builtin_bit_cast(V, v[j]);
+      const int at = place(j);
+#pragma unroll
+      for (int k = 0; k < kV; ++k) f((float)r[k], at + k);
+    }
+    f(last, last_place(n));
+  }
+  // y = f(value)
+  template <class F>
+  __device__ __forceinline__ void store(T* y, int n, F&& f) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int at = place(j);
+      if (at + kV > n) continue;
+      asm("" : "+v"(v[j]));
+      const V r = __builtin_bit_cast(V, v[j]);
+      V q;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) q[k] = (T)f((float)r[k]);
+      *(Anywhere*)(y + (uint32_t)at) = q;
+    }
+    if (last_place(n) < n) y[last_place(n)] = (T)f(last);
+  }
+  // whether this thread holds a place
+  __device__ __forceinline__ static bool mine(int at, int n) {
+    return at >= n / kV * kV ? at - n / kV * kV == (int)threadIdx.x : at / kV % THREADS == (int)threadIdx.x;
+  }
+};
+
+constexpr int kCandidates = 512;
+
+// The `top` largest keys of a row, by chunks.
+struct Top {
+  uint64_t list[kCandidates + MIST_TOKEN_MAX_TOP];
+  uint64_t best[MIST_TOKEN_MAX_TOP];  // the largest so far, in order; 0: none
+  uint64_t part[16];
+  int count;
+};
+
+// Joins a chunk into t.best.  At least ceil(top / waves) lanes of each wave have a value of at least the wave's
+// ceil(top / waves)-th largest lane maximum, so the least of these over the waves bounds the row's top-th largest value from below:
+// the few values from there on are the candidates, and each one's place is the number of larger ones.  Where there are
+// too many (equal values, or a row with NaN, whose lanes' maxima say nothing) the largest are taken one by one.
+// low: of the row, the thread's largest value.
+template <class T, int THREADS, int N>
+__device__ void join_top(Chunk<T, THREADS, N>& c, int n, uint32_t base, int top, float low, bool plain, Top& t, Join<THREADS / 64>& join) {
+  constexpr int kWaves = THREADS / 64;
+  const int tid = threadIdx.x, lane = tid % 64;
+  const uint64_t least = t.best[top - 1];  // of what is there
+  float bound = -HUGE_VALF, x = low;
+  for (int k = 0; k < (top + kWaves - 1) / kWaves; ++k) {
+    bound = wave_max(x);
+    if (bound == -HUGE_VALF) break;
+    if (lane == __ffsll((unsigned long long)__ballot(x == bound)) - 1) x = -HUGE_VALF;
+  }
+  bound = join.of_waves(bound, [](float p, float q) { return fminf(p, q); });  // a barrier: t.best has been read
+  if (tid == 0) t.count = 0;
+  __syncthreads();
+  if (plain && low >= bound) {
+    c.each(n, [&](float v, int at) {
+      if (v >= bound && v != -HUGE_VALF && at < n) {
+        const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
+        if (key > least) {
+          const int i = atomicAdd(&t.count, 1);
+          if (i < kCandidates) t.list[i] = key;
+        }
+      }
+    });
+  }
+  __syncthreads();
+  int count = t.count;
+  if (!plain || count > kCandidates) {
+    __syncthreads();
+    uint64_t last = ~0ull;
+    count = 0;
+    for (int k = 0; k < top; ++k) {
+      uint64_t best = 0;
+      c.each(n, [&](float v, int at) {
+        const uint32_t rank = rank_of(v);
+        const uint64_t key = rank && at < n ? key_of(rank, base + (uint32_t)at) : 0;
+        if (key > best && key < last) best = key;
+      });
+      best = wave_max_key(best);
+      if (kWaves > 1) {
+        if (lane == 0) t.part[tid / 64] = best;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) best = std::max(best, t.part[w]);
+      }
+      if (tid == 0 && best) t.list[k] = best;
+      __syncthreads();
+      if (!best) break;
+      last = best;
+      ++count;
+    }
+  }
+  // the former best join the candidates
+  if (base) {
+    if (tid < top) t.list[count + tid] = t.best[tid];
+    count += top;
+  }
+  __syncthreads();
+  if (tid < top) t.best[tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < count; i += THREADS) {
+    const uint64_t key = t.list[i];
+    int larger = 0;
+    for (int k = 0; k < count; ++k) larger += t.list[k] > key;
+    if (key && larger < top) t.best[larger] = key;
+  }
+  __syncthreads();
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_logprob(TokenArgs a, const T* logits, const void* targets, float* stats, float* logp, float* lse,
-                                                      float* entropy, int32_t* top_ids, float* top_logp) {
-  __shared__ uint64_t part[kThreads / 64];
+// A row's gradient, p (c0 + c1 log p) + [j = target] up with scale in the factors.  One without factors is zeros, whatever the
+// logits are: they are not looked at.
+struct Slope {
+  float lse, c0, c1, up;
+};
+__device__ __forceinline__ bool flat(const Slope& g) { return g.c0 == 0.0f && g.c1 == 0.0f && g.up == 0.0f; }
+__device__ __forceinline__ Slope slope_of(float lse, float scale, float dlogp, float dentropy, float entropy) {
+  if (lse == -HUGE_VALF) return Slope{0.0f, 0.0f, 0.0f, 0.0f};
+  return Slope{lse, scale * (dentropy != 0.0f ? -dlogp - dentropy * entropy : -dlogp), scale * -dentropy, scale * dlogp};
+}
+__device__ __forceinline__ float slope_at(const Slope& g, float x, float scale) {
+  const float l = fmaf(x, scale, -g.lse), p = fast_exp(l);
+  return p * fmaf(g.c1, fmaxf(l, kLow), g.c0);
+}
+
+struct RowOut {
+  float *stats, *logp, *lse, *entropy;
+  int32_t* top_ids;
+  float* top_logp;
+  const float* weights;
+  float weight;
+};
+
+// A row a block.  LOSS: logp and the gradient, otherwise the row's results.
+template <class T, int THREADS, int N, bool LOSS>
+__global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits, const void* targets, RowOut o, T* dlogits) {
+  using C = Chunk<T, THREADS, N>;
+  __shared__ float2 part[2][THREADS / 64];
+  __shared__ Top top;
+  Join<THREADS / 64> join{part, 0};
   for (int32_t t = blockIdx.x; t < a.n; t += gridDim.x) {
     const T* x = logits + logits_offset(a, t);
-    Stats r = row_stats(a, x);
     const int64_t target = targets ? target_of(a, targets, t) : -1, at = target - a.vocab_begin;
-    r.z = target >= 0 && at >= 0 && at < a.rows ? (float)x[at] * a.scale : -HUGE_VALF;
-    const float l = lse_of(r);
-    if (threadIdx.x == 0) {
-      if (stats) {
-        *(float4*)(stats + (int64_t)t * 4) = float4{r.m, r.s, r.u, r.z};
-      } else {
-        lse[t] = l;
-        if (logp) logp[t] = logp_of(r.z, l, target);
-        if (entropy) entropy[t] = entropy_of(r);
+    const bool here = target >= 0 && at >= 0 && at < a.rows;
+    const float xt = here ? (float)x[at] : -HUGE_VALF;
+    Stats r{-HUGE_VALF, 0.0f, 0.0f, here ? xt * a.scale : -HUGE_VALF};
+    if (!LOSS && a.top) {
+      if (threadIdx.x < (unsigned)a.top) top.best[threadIdx.x] = 0;
+      __syncthreads();
+    }
+    C c;
+    float s = 0.0f, u = 0.0f;
+    for (int64_t base = 0; base < a.rows; base += C::kAll) {
+      const int n = (int)min((int64_t)C::kAll, a.rows - base);
+      c.load(x + base, n);
+      float low = -HUGE_VALF;
+      c.each(n, [&](float v, int) { low = fmaxf(low, v); });
+      const float m = fmaxf(r.m, join.of_waves(wave_max(low), [](float p, float q) { return fmaxf(p, q); }) * a.scale);
+      const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
+      if (base) {
+        const float d = r.m == -HUGE_VALF ? 0.0f : r.m - from, f = fast_exp(d);  // where nothing was visible s and u are 0
+        u = f * fmaf(d, s, u);
+        s *= f;
+      }
+      r.m = m;
+      c.each(n, [&](float v, int) {
+        const float d = fmaf(v, a.scale, -from), e = fast_exp(d);
+        s += e;
+        if (!LOSS) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
+      });
+      if (!LOSS && a.top) {
+        const float odd = s != s ? 1.0f : 0.0f;
+        const bool plain = !(join.sum(odd, 0.0f).x > 0.0f);
+        join_top(c, n, (uint32_t)base, a.top, low, plain, top, join);
       }
     }
-    uint64_t last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-      uint64_t best = 0;
-      for (int64_t j = threadIdx.x; j < a.rows; j += kThreads) {
-        const uint32_t rank = rank_of((float)x[j]);
-        const uint64_t key = rank ? key_of(rank, (uint32_t)j) : 0;
-        if (key > best && key < last) best = key;
+    const float2 su = join.sum(s, u);
+    r.s = su.x, r.u = su.y;
+    const float l = lse_of(r);
+    if (threadIdx.x == 0) {
+      if (LOSS) {
+        o.logp[t] = logp_of(r.z, l, target);
+      } else if (o.stats) {
+        *(float4*)(o.stats + (int64_t)t * 4) = float4{r.m, r.s, r.u, r.z};
+      } else {
+        o.lse[t] = l;
+        if (o.logp) o.logp[t] = logp_of(r.z, l, target);
+        if (o.entropy) o.entropy[t] = entropy_of(r);
       }
-      best = wave_max_key(best);
-      __syncthreads();
-      if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = best;
-      __syncthreads();
-      for (int w = 0; w < kThreads / 64; ++w) best = std::max(best, part[w]);
-      last = best;
-      if (threadIdx.x == 0) {
+    }
+    if constexpr (LOSS) {
+      const Slope g = slope_of(l, a.scale, target < 0 ? 0.0f : -(o.weights ? o.weight * o.weights[t] : o.weight), 0.0f, 0.0f);
+      const bool zero = flat(g);
+      T* y = dlogits + grad_offset(a, t);
+      // the last chunk is still here; the others are read again
+      const int64_t final = (a.rows - 1) / C::kAll * C::kAll;
+      for (int64_t base = final; base >= 0; base -= C::kAll) {
+        const int n = (int)min((int64_t)C::kAll, a.rows - base);
+        if (base != final) c.load(x + base, n);
+        c.store(y + base, n, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
+        const int64_t k = at - base;
+        if (here && k >= 0 && k < n && C::mine((int)k, n)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
+      }
+    } else if (a.top) {
+      if (threadIdx.x < (unsigned)a.top) {
+        const uint64_t best = top.best[threadIdx.x];
         const float z = of_rank((uint32_t)(best >> 32)) * a.scale;
-        top_ids[(int64_t)t * a.top + k] = best ? (int32_t)(~(uint32_t)best + (uint32_t)a.vocab_begin) : -1;
-        top_logp[(int64_t)t * a.top + k] = !best ? -HUGE_VALF : stats ? z : z - l;
+        o.top_ids[(int64_t)t * a.top + threadIdx.x] = best ? (int32_t)(~(uint32_t)best + (uint32_t)a.vocab_begin) : -1;
+        o.top_logp[(int64_t)t * a.top + threadIdx.x] = !best ? -HUGE_VALF : o.stats ? z : z - l;
       }
+      __syncthreads();
     }
   }
 }
@@ -195,55 +411,38 @@ __global__ __launch_bounds__(kThreads) void k_join(TokenArgs a, int32_t ranks, c
   }
 }
 
-// A row's gradient, p (c0 + c1 log p) + [j = target] up with scale in the factors.  One without factors is zeros, whatever the
-// logits are: they are not looked at.
-struct Slope {
-  float lse, c0, c1, up;
-};
-__device__ __forceinline__ bool flat(const Slope& g) { return g.c0 == 0.0f && g.c1 == 0.0f && g.up == 0.0f; }
-__device__ __forceinline__ Slope slope_of(float lse, float scale, float dlogp, float dentropy, float entropy) {
-  if (lse == -HUGE_VALF) return Slope{0.0f, 0.0f, 0.0f, 0.0f};
-  return Slope{lse, scale * (dentropy != 0.0f ? -dlogp - dentropy * entropy : -dlogp), scale * -dentropy, scale * dlogp};
-}
-__device__ __forceinline__ float slope_at(const Slope& g, float x, float scale) {
-  const float l = fmaf(x, scale, -g.lse), p = fast_exp(l);
-  return p * fmaf(g.c1, fmaxf(l, kLow), g.c0);
-}
+// One pass: a block takes a slab of a row.
+constexpr int kGradVectors = 2;
 
 template <class T>
-__device__ void write_slope(const TokenArgs& a, const Slope& g, const T* x, T* y, int64_t at) {
-  const bool zero = flat(g);
-  for (int64_t j = threadIdx.x; j < a.rows; j += kThreads) {
-    float d = zero ? 0.0f : slope_at(g, (float)x[j], a.scale);
-    if (j == at) d += g.up;
-    y[j] = (T)d;
-  }
-}
-
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_grad(TokenArgs a, const T* logits, const void* targets, const float* lse, const float* dlogp,
+__global__ __launch_bounds__(kThreads) void k_grad(TokenArgs a, int32_t slabs, const T* logits, const void* targets, const float* lse, const float* dlogp,
                                                    const float* entropy, const float* dentropy, T* dlogits) {
-  for (int32_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-    const int64_t target = dlogp ? target_of(a, targets, t) : -1;
+  using C = Chunk<T, kThreads, kGradVectors>;
+  for (int64_t i = blockIdx.x; i < (int64_t)a.n * slabs; i += gridDim.x) {
+    const int32_t t = (int32_t)(i / slabs);
+    const int64_t base = i % slabs * C::kAll;
+    const int n = (int)min((int64_t)C::kAll, a.rows - base);
+    const int64_t target = dlogp ? target_of(a, targets, t) : -1, at = target - a.vocab_begin - base;
     const Slope g = slope_of(lse[t], a.scale, target >= 0 ? dlogp[t] : 0.0f, dentropy ? dentropy[t] : 0.0f, dentropy ? entropy[t] : 0.0f);
-    write_slope(a, g, logits + logits_offset(a, t), dlogits + grad_offset(a, t), target < 0 ? -1 : target - a.vocab_begin);
+    const bool zero = flat(g), here = target >= 0 && at >= 0 && at < n;
+    const T* x = logits + logits_offset(a, t) + base;
+    T* y = dlogits + grad_offset(a, t) + base;
+    C c;
+    if (!zero) c.load(x, n);
+    const bool owner = here && C::mine((int)at, n);
+    const float xt = owner && !zero ? (float)x[at] : 0.0f;
+    c.store(y, n, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
+    if (owner && !zero) y[at] = (T)(slope_at(g, xt, a.scale) + g.up);
   }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_loss(TokenArgs a, const T* logits, const void* targets, const float* weights, float weight, float* logp,
-                                                   T* dlogits) {
-  for (int32_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-    const T* x = logits + logits_offset(a, t);
-    const int64_t target = target_of(a, targets, t);
-    Stats r = row_stats(a, x);
-    r.z = target >= 0 && target < a.rows ? (float)x[target] * a.scale : -HUGE_VALF;
-    __syncthreads();  // the gradient may overwrite the target's logit
-    const float l = lse_of(r);
-    if (threadIdx.x == 0) logp[t] = logp_of(r.z, l, target);
-    const Slope g = slope_of(l, a.scale, target < 0 ? 0.0f : -(weights ? weight * weights[t] : weight), 0.0f, 0.0f);
-    write_slope(a, g, x, dlogits + grad_offset(a, t), target);
-  }
+// f(threads, vectors a thread): the smallest block that holds a row in its registers; the largest takes longer ones by chunks.
+template <class T, class F>
+void with_block(int64_t rows, F&& f) {
+  constexpr int kN = 8, kWave = 64 * kN * 16 / (int)sizeof(T);
+  if (rows <= kWave) f(std::integral_constant<int, 64>{}, std::integral_constant<int, kN>{});
+  else if (rows <= 4 * kWave) f(std::integral_constant<int, 256>{}, std::integral_constant<int, kN>{});
+  else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, kN>{});
 }
 
 mist_status check(const mist_token_desc* d) {
@@ -316,8 +515,10 @@ mist_status forward(const mist_token_desc* d, const void* logits, const void* ta
   const unsigned blocks = (unsigned)std::min<int64_t>(a.n, kMostBlocks);
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
-    hipLaunchKernelGGL((k_logprob<T>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a, (const T*)logits, targets, stats, logp, lse,
-                       entropy, top_ids, top_logp);
+    with_block<T>(d->rows, [&](auto threads, auto vectors) {
+      hipLaunchKernelGGL((k_row<T, threads.value, vectors.value, false>), dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
+                         RowOut{stats, logp, lse, entropy, top_ids, top_logp, nullptr, 0.0f}, (T*)nullptr);
+    });
   });
   return launched("token log probabilities");
 }
@@ -370,10 +571,12 @@ mist_status mist_token_grad(const mist_token_desc* d, const void* logits, const 
       !floats_ok({lse, dlogp, entropy, dentropy}))
     return lib_fail(MIST_E_INVALID, "token log probabilities: a buffer is not aligned to its elements");
   if (const mist_status st = check_grad(d, logits, dlogits)) return st;
-  const unsigned blocks = (unsigned)std::min<int64_t>(a.n, kMostBlocks);
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
-    hipLaunchKernelGGL((k_grad<T>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a, (const T*)logits, targets, lse, dlogp, entropy, dentropy,
+    constexpr int kSlab = Chunk<T, kThreads, kGradVectors>::kAll;
+    const int32_t slabs = (int32_t)((d->rows + kSlab - 1) / kSlab);
+    const unsigned blocks = (unsigned)std::min<int64_t>((int64_t)a.n * slabs, kMostBlocks);
+    hipLaunchKernelGGL((k_grad<T>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a, slabs, (const T*)logits, targets, lse, dlogp, entropy, dentropy,
                        (T*)dlogits);
   });
   return launched("token log probabilities' gradient");
@@ -394,8 +597,10 @@ mist_status mist_token_loss(const mist_token_desc* d, const void* logits, const 
   const unsigned blocks = (unsigned)std::min<int64_t>(a.n, kMostBlocks);
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
-    hipLaunchKernelGGL((k_loss<T>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a, (const T*)logits, targets, weights, weight, logp,
-                       (T*)dlogits);
+    with_block<T>(d->rows, [&](auto threads, auto vectors) {
+      hipLaunchKernelGGL((k_row<T, threads.value, vectors.value, true>), dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
+                         RowOut{nullptr, logp, nullptr, nullptr, nullptr, nullptr, weights, weight}, (T*)dlogits);
+    });
   });
   return launched("token loss");
 }
