@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mist_ops.h"
 
@@ -110,51 +111,70 @@ struct Join {
   }
 };
 
-// A chunk of a row in the registers of its block: N vectors of 16 bytes a thread, in turn over the threads, and what is
-// left over a whole vector, one value a thread.  What is not there is -inf.  The values stay in their type between the passes over
-// them (the empty assembly keeps the compiler from holding them converted, which takes twice the registers of 16-bit values).
+// A chunk of a row in the registers of its block: vectors of 16 bytes at whole multiples of 16 in memory, N a thread, in turn
+// over the threads, and what lies before the first and after the last, one value a thread.  (50257 16-bit values a row, most off
+// alignment: 163 us for 8192 aligned rows, 221 with vectors from the row's first value on.)  What is not there is -inf.  The
+// values stay in their type between the passes over them (the empty assembly keeps the compiler from holding them converted, which takes
+// twice the registers of 16-bit values).
 typedef uint32_t Raw __attribute__((ext_vector_type(4)));
 
-template <class T, int THREADS, int N>
+template <class T, int THREADS, int N, bool ALIGN = true>
 struct Chunk {
   static constexpr int kV = 16 / sizeof(T), kAll = THREADS * N * kV;
   typedef T V __attribute__((ext_vector_type(kV)));
   typedef typename mist::Vec<T, kV>::type Anywhere;
   Raw v[N];
-  float last;
-  __device__ __forceinline__ static int place(int j) {
+  float odd;
+  int n, head;  // values, and those before the first vector
+
+  __device__ __forceinline__ int place(int j) const {
     int at = threadIdx.x;
     asm("" : "+v"(at));  // formed anew where it is used, rather than N of them held
-    return (j * THREADS + at) * kV;
+    return head + (j * THREADS + at) * kV;
   }
-  __device__ __forceinline__ static int last_place(int n) { return n / kV * kV + (int)threadIdx.x; }
-  __device__ __forceinline__ void load(const T* x, int n) {
+  // of the odd value; n or more: none
+  __device__ __forceinline__ int odd_place() const {
+    const int t = threadIdx.x;
+    return t < head ? t : n - (n - head) % kV + t - head;
+  }
+  __device__ __forceinline__ bool any(int j) const { return head + (j * THREADS + 1) * kV <= n; }  // the j-th vector of some thread
+  __device__ __forceinline__ void load(const T* x, int count, bool read = true) {
+    n = count;
+    head = !ALIGN ? 0 : min(n, (int)(-(reinterpret_cast<uintptr_t>(x) / sizeof(T)) % kV));
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       V r = (T)-HUGE_VALF;
       const int at = place(j);
-      if (at + kV <= n) r = *(const Anywhere*)(x + (uint32_t)at);
+      if (read && at + kV <= n) r = *(const std::conditional_t<ALIGN, V, Anywhere>*)(x + (uint32_t)at);
       v[j] = __builtin_bit_cast(Raw, r);
     }
-    last = last_place(n) < n ? (float)x[last_place(n)] : -HUGE_VALF;
+    odd = read && odd_place() < n ? (float)x[odd_place()] : -HUGE_VALF;
   }
-  // f(value, its place in the chunk); whole vectors that no thread has are passed over
+  // f(value, its place in the chunk), of the vectors in which some value passes `where`; vectors that no thread has are passed over
   template <class F>
-  __device__ __forceinline__ void each(int n, F&& f) {
+  __device__ __forceinline__ void each(F&& f) {
+    each(f, [](float) { return true; });
+  }
+  template <class F, class W>
+  __device__ __forceinline__ void each(F&& f, W&& where) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (j * THREADS * kV >= n) continue;
+      if (!any(j)) continue;
       asm("" : "+v"(v[j]));
       const V r = __builtin_bit_cast(V, v[j]);
+      bool some = false;
+#pragma unroll
+      for (int k = 0; k < kV; ++k) some |= where((float)r[k]);
+      if (!some) continue;
       const int at = place(j);
 #pragma unroll
       for (int k = 0; k < kV; ++k) f((float)r[k], at + k);
     }
-    f(last, last_place(n));
+    f(odd, odd_place());
   }
   // y = f(value)
   template <class F>
-  __device__ __forceinline__ void store(T* y, int n, F&& f) {
+  __device__ __forceinline__ void store(T* y, F&& f) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int at = place(j);
@@ -166,11 +186,12 @@ struct Chunk {
       for (int k = 0; k < kV; ++k) q[k] = (T)f((float)r[k]);
       *(Anywhere*)(y + (uint32_t)at) = q;
     }
-    if (last_place(n) < n) y[last_place(n)] = (T)f(last);
+    if (odd_place() < n) y[odd_place()] = (T)f(odd);
   }
   // whether this thread holds a place
-  __device__ __forceinline__ static bool mine(int at, int n) {
-    return at >= n / kV * kV ? at - n / kV * kV == (int)threadIdx.x : at / kV % THREADS == (int)threadIdx.x;
+  __device__ __forceinline__ bool mine(int at) const {
+    const int tail = n - (n - head) % kV, t = threadIdx.x;
+    return at < head ? at == t : at >= tail ? at - tail + head == t : (at - head) / kV % THREADS == t;
   }
 };
 
@@ -190,29 +211,29 @@ struct Top {
 // too many (equal values, or a row with NaN, whose lanes' maxima say nothing) the largest are taken one by one.
 // low: of the row, the thread's largest value.
 template <class T, int THREADS, int N>
-__device__ void join_top(Chunk<T, THREADS, N>& c, int n, uint32_t base, int top, float low, bool plain, Top& t, Join<THREADS / 64>& join) {
+__device__ __forceinline__ void join_top(Chunk<T, THREADS, N>& c, const T* x, uint32_t base, int top, float low, bool plain, Top& t, Join<THREADS / 64>& join) {
   constexpr int kWaves = THREADS / 64;
   const int tid = threadIdx.x, lane = tid % 64;
   const uint64_t least = t.best[top - 1];  // of what is there
-  float bound = -HUGE_VALF, x = low;
+  float bound = -HUGE_VALF, left = low;
   for (int k = 0; k < (top + kWaves - 1) / kWaves; ++k) {
-    bound = wave_max(x);
+    bound = wave_max(left);
     if (bound == -HUGE_VALF) break;
-    if (lane == __ffsll((unsigned long long)__ballot(x == bound)) - 1) x = -HUGE_VALF;
+    if (lane == __ffsll((unsigned long long)__ballot(left == bound)) - 1) left = -HUGE_VALF;
   }
   bound = join.of_waves(bound, [](float p, float q) { return fminf(p, q); });  // a barrier: t.best has been read
   if (tid == 0) t.count = 0;
   __syncthreads();
   if (plain && low >= bound) {
-    c.each(n, [&](float v, int at) {
-      if (v >= bound && v != -HUGE_VALF && at < n) {
+    c.each([&](float v, int at) {
+      if (v >= bound && v != -HUGE_VALF) {
         const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
         if (key > least) {
           const int i = atomicAdd(&t.count, 1);
           if (i < kCandidates) t.list[i] = key;
         }
       }
-    });
+    }, [&](float v) { return v >= bound; });
   }
   __syncthreads();
   int count = t.count;
@@ -222,11 +243,11 @@ __device__ void join_top(Chunk<T, THREADS, N>& c, int n, uint32_t base, int top,
     count = 0;
     for (int k = 0; k < top; ++k) {
       uint64_t best = 0;
-      c.each(n, [&](float v, int at) {
-        const uint32_t rank = rank_of(v);
-        const uint64_t key = rank && at < n ? key_of(rank, base + (uint32_t)at) : 0;
+      for (int at = tid; at < c.n; at += THREADS) {  // from memory: the registers hold the other path's row
+        const uint32_t rank = rank_of((float)x[at]);
+        const uint64_t key = rank ? key_of(rank, base + (uint32_t)at) : 0;
         if (key > best && key < last) best = key;
-      });
+      }
       best = wave_max_key(best);
       if (kWaves > 1) {
         if (lane == 0) t.part[tid / 64] = best;
@@ -280,12 +301,14 @@ struct RowOut {
   float weight;
 };
 
-// A row a block.  LOSS: logp and the gradient, otherwise the row's results.
-template <class T, int THREADS, int N, bool LOSS>
-__global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits, const void* targets, RowOut o, T* dlogits) {
+// A row a block: its results, with alternatives, or logp and the gradient.
+enum Mode { kStats, kTop, kLoss };
+
+template <class T, int THREADS, int N, Mode MODE>
+__global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_row(TokenArgs a, const T* logits, const void* targets, RowOut o, T* dlogits) {
   using C = Chunk<T, THREADS, N>;
   __shared__ float2 part[2][THREADS / 64];
-  __shared__ Top top;
+  __shared__ std::conditional_t<MODE == kTop, Top, int> top;
   Join<THREADS / 64> join{part, 0};
   for (int32_t t = blockIdx.x; t < a.n; t += gridDim.x) {
     const T* x = logits + logits_offset(a, t);
@@ -293,7 +316,7 @@ __global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits
     const bool here = target >= 0 && at >= 0 && at < a.rows;
     const float xt = here ? (float)x[at] : -HUGE_VALF;
     Stats r{-HUGE_VALF, 0.0f, 0.0f, here ? xt * a.scale : -HUGE_VALF};
-    if (!LOSS && a.top) {
+    if constexpr (MODE == kTop) {
       if (threadIdx.x < (unsigned)a.top) top.best[threadIdx.x] = 0;
       __syncthreads();
     }
@@ -303,7 +326,7 @@ __global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits
       const int n = (int)min((int64_t)C::kAll, a.rows - base);
       c.load(x + base, n);
       float low = -HUGE_VALF;
-      c.each(n, [&](float v, int) { low = fmaxf(low, v); });
+      c.each([&](float v, int) { low = fmaxf(low, v); });
       const float m = fmaxf(r.m, join.of_waves(wave_max(low), [](float p, float q) { return fmaxf(p, q); }) * a.scale);
       const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
       if (base) {
@@ -312,22 +335,22 @@ __global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits
         s *= f;
       }
       r.m = m;
-      c.each(n, [&](float v, int) {
+      c.each([&](float v, int) {
         const float d = fmaf(v, a.scale, -from), e = fast_exp(d);
         s += e;
-        if (!LOSS) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
+        if (MODE != kLoss) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
       });
-      if (!LOSS && a.top) {
+      if constexpr (MODE == kTop) {
         const float odd = s != s ? 1.0f : 0.0f;
         const bool plain = !(join.sum(odd, 0.0f).x > 0.0f);
-        join_top(c, n, (uint32_t)base, a.top, low, plain, top, join);
+        join_top(c, x + base, (uint32_t)base, a.top, low, plain, top, join);
       }
     }
     const float2 su = join.sum(s, u);
     r.s = su.x, r.u = su.y;
     const float l = lse_of(r);
     if (threadIdx.x == 0) {
-      if (LOSS) {
+      if (MODE == kLoss) {
         o.logp[t] = logp_of(r.z, l, target);
       } else if (o.stats) {
         *(float4*)(o.stats + (int64_t)t * 4) = float4{r.m, r.s, r.u, r.z};
@@ -337,7 +360,7 @@ __global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits
         if (o.entropy) o.entropy[t] = entropy_of(r);
       }
     }
-    if constexpr (LOSS) {
+    if constexpr (MODE == kLoss) {
       const Slope g = slope_of(l, a.scale, target < 0 ? 0.0f : -(o.weights ? o.weight * o.weights[t] : o.weight), 0.0f, 0.0f);
       const bool zero = flat(g);
       T* y = dlogits + grad_offset(a, t);
@@ -346,11 +369,11 @@ __global__ __launch_bounds__(THREADS, 8) void k_row(TokenArgs a, const T* logits
       for (int64_t base = final; base >= 0; base -= C::kAll) {
         const int n = (int)min((int64_t)C::kAll, a.rows - base);
         if (base != final) c.load(x + base, n);
-        c.store(y + base, n, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
+        c.store(y + base, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
         const int64_t k = at - base;
-        if (here && k >= 0 && k < n && C::mine((int)k, n)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
+        if (here && k >= 0 && k < n && c.mine((int)k)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
       }
-    } else if (a.top) {
+    } else if constexpr (MODE == kTop) {
       if (threadIdx.x < (unsigned)a.top) {
         const uint64_t best = top.best[threadIdx.x];
         const float z = of_rank((uint32_t)(best >> 32)) * a.scale;
@@ -417,7 +440,7 @@ constexpr int kGradVectors = 2;
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_grad(TokenArgs a, int32_t slabs, const T* logits, const void* targets, const float* lse, const float* dlogp,
                                                    const float* entropy, const float* dentropy, T* dlogits) {
-  using C = Chunk<T, kThreads, kGradVectors>;
+  using C = Chunk<T, kThreads, kGradVectors, false>;
   for (int64_t i = blockIdx.x; i < (int64_t)a.n * slabs; i += gridDim.x) {
     const int32_t t = (int32_t)(i / slabs);
     const int64_t base = i % slabs * C::kAll;
@@ -428,10 +451,10 @@ __global__ __launch_bounds__(kThreads) void k_grad(TokenArgs a, int32_t slabs, c
     const T* x = logits + logits_offset(a, t) + base;
     T* y = dlogits + grad_offset(a, t) + base;
     C c;
-    if (!zero) c.load(x, n);
-    const bool owner = here && C::mine((int)at, n);
+    c.load(x, n, !zero);
+    const bool owner = here && c.mine((int)at);
     const float xt = owner && !zero ? (float)x[at] : 0.0f;
-    c.store(y, n, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
+    c.store(y, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
     if (owner && !zero) y[at] = (T)(slope_at(g, xt, a.scale) + g.up);
   }
 }
@@ -442,7 +465,8 @@ void with_block(int64_t rows, F&& f) {
   constexpr int kN = 8, kWave = 64 * kN * 16 / (int)sizeof(T);
   if (rows <= kWave) f(std::integral_constant<int, 64>{}, std::integral_constant<int, kN>{});
   else if (rows <= 4 * kWave) f(std::integral_constant<int, 256>{}, std::integral_constant<int, kN>{});
-  else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, kN>{});
+  else if (rows <= 8 * kWave) f(std::integral_constant<int, 512>{}, std::integral_constant<int, kN>{});
+  else f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2 * kN>{});
 }
 
 mist_status check(const mist_token_desc* d) {
@@ -516,7 +540,8 @@ mist_status forward(const mist_token_desc* d, const void* logits, const void* ta
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
     with_block<T>(d->rows, [&](auto threads, auto vectors) {
-      hipLaunchKernelGGL((k_row<T, threads.value, vectors.value, false>), dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
+      const auto kernel = a.top ? k_row<T, threads.value, vectors.value, kTop> : k_row<T, threads.value, vectors.value, kStats>;
+      hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
                          RowOut{stats, logp, lse, entropy, top_ids, top_logp, nullptr, 0.0f}, (T*)nullptr);
     });
   });
@@ -573,7 +598,7 @@ mist_status mist_token_grad(const mist_token_desc* d, const void* logits, const 
   if (const mist_status st = check_grad(d, logits, dlogits)) return st;
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
-    constexpr int kSlab = Chunk<T, kThreads, kGradVectors>::kAll;
+    constexpr int kSlab = Chunk<T, kThreads, kGradVectors, false>::kAll;
     const int32_t slabs = (int32_t)((d->rows + kSlab - 1) / kSlab);
     const unsigned blocks = (unsigned)std::min<int64_t>((int64_t)a.n * slabs, kMostBlocks);
     hipLaunchKernelGGL((k_grad<T>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a, slabs, (const T*)logits, targets, lse, dlogp, entropy, dentropy,
@@ -598,7 +623,7 @@ mist_status mist_token_loss(const mist_token_desc* d, const void* logits, const 
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
     with_block<T>(d->rows, [&](auto threads, auto vectors) {
-      hipLaunchKernelGGL((k_row<T, threads.value, vectors.value, true>), dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
+      hipLaunchKernelGGL((k_row<T, threads.value, vectors.value, kLoss>), dim3(blocks), dim3(threads.value), 0, (hipStream_t)stream, a, (const T*)logits, targets,
                          RowOut{nullptr, logp, nullptr, nullptr, nullptr, nullptr, weights, weight}, (T*)dlogits);
     });
   });

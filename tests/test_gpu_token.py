@@ -293,12 +293,21 @@ def test_strides(torch, kind):
         targets = wide[:, 2:7] % x.shape[-1]
         solid = x.contiguous()
         r, want = mist.token_logprob(x, targets, entropy=True, top=3), mist.token_logprob(solid, targets.contiguous(), entropy=True, top=3)
-        assert all(torch.equal(a, b) for a, b in zip(r, want))
+        assert torch.equal(r.top_ids, want.top_ids)   # sums are in an order that goes by the rows' alignment too
+        truth = Truth(torch, solid, targets, 1.0)
+        for got in (r, want):
+            within(got.lse, truth.lse, truth.e_lse, "lse")
+            within(got.logp, truth.logp, truth.e_logp, "logp")
+            within(got.entropy, truth.entropy, truth.e_entropy, "entropy")
         room = torch.full((3, 7, x.shape[-1] + 5), 7.0, device="cuda", dtype=T)
         out = room[:, 1:6, 2:-3]
         logp, _ = mist.token_loss(x, targets, 0.5, dlogits=out)
         logp2, d = mist.token_loss(solid, targets.contiguous(), 0.5)
-        assert torch.equal(logp, logp2) and torch.equal(out, d)
+        grad, slack = truth.grad(torch, torch.full((3, 5), -0.5, device="cuda"), torch.zeros(3, 5, device="cuda"), 1.0, kind)
+        for got in (out, d):
+            within(got, grad.reshape(got.shape), slack.reshape(got.shape), "dlogits")
+        for got in (logp, logp2):
+            within(got, truth.logp, truth.e_logp, "logp")
         out.fill_(7.0)
         assert bool((room == 7.0).all())
         mist.token_grad(x, targets, r.lse, dlogp=logp, dlogits=out)
