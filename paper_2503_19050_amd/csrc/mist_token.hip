@@ -81,32 +81,30 @@ template <int WAVES>
 struct Join {
   float2 (*part)[WAVES];
   int turn;
-  __device__ __forceinline__ float2 get(float a, float b) {
+  __device__ __forceinline__ void put(float a, float b) {
     float2* p = part[turn];
     turn ^= 1;
     if (threadIdx.x % 64 == 0) p[threadIdx.x / 64] = float2{a, b};
     __syncthreads();
-    return float2{0.0f, 0.0f};
   }
   __device__ __forceinline__ float2 sum(float a, float b) {
     a = wave_sum(a);
     b = wave_sum(b);
     if (WAVES == 1) return float2{a, b};
     const float2* p = part[turn];
-    get(a, b);
+    put(a, b);
     float2 s = p[0];
 #pragma unroll
     for (int k = 1; k < WAVES; ++k) s.x += p[k].x, s.y += p[k].y;
     return s;
   }
-  template <class J>
-  __device__ __forceinline__ float of_waves(float x, J join) {
+  __device__ __forceinline__ float2 most_and_least(float2 x) {
     if (WAVES == 1) return x;
     const float2* p = part[turn];
-    get(x, 0.0f);
-    x = p[0].x;
+    put(x.x, x.y);
+    x = p[0];
 #pragma unroll
-    for (int k = 1; k < WAVES; ++k) x = join(x, p[k].x);
+    for (int k = 1; k < WAVES; ++k) x = float2{fmaxf(x.x, p[k].x), fminf(x.y, p[k].y)};
     return x;
   }
 };
@@ -195,87 +193,88 @@ struct Chunk {
   }
 };
 
+// Alternatives.  At least q = ceil(top / waves) lanes of each wave have a value of at least the wave's q-th largest lane
+// maximum, so the least of these over the waves bounds a row's top-th largest value from below, and the few values from there on (and
+// every NaN) are the candidates.  A candidate's place is the number of larger ones.  Where there are too many (equal values
+// in many places) the largest are taken one by one, with a pass each.
 constexpr int kCandidates = 512;
 
-// The `top` largest keys of a row, by chunks.
 struct Top {
-  uint64_t list[kCandidates + MIST_TOKEN_MAX_TOP];
-  uint64_t best[MIST_TOKEN_MAX_TOP];  // the largest so far, in order; 0: none
-  uint64_t part[16];
+  uint64_t list[kCandidates];
+  uint64_t best[MIST_TOKEN_MAX_TOP];  // of the chunks before, in order; 0: none
+  uint64_t part[8];
   int count;
 };
 
-// Joins a chunk into t.best.  At least ceil(top / waves) lanes of each wave have a value of at least the wave's
-// ceil(top / waves)-th largest lane maximum, so the least of these over the waves bounds the row's top-th largest value from below:
-// the few values from there on are the candidates, and each one's place is the number of larger ones.  Where there are
-// too many (equal values, or a row with NaN, whose lanes' maxima say nothing) the largest are taken one by one.
-// low: of the row, the thread's largest value.
-template <class T, int THREADS, int N>
-__device__ __forceinline__ void join_top(Chunk<T, THREADS, N>& c, const T* x, uint32_t base, int top, float low, bool plain, Top& t, Join<THREADS / 64>& join) {
-  constexpr int kWaves = THREADS / 64;
-  const int tid = threadIdx.x, lane = tid % 64;
-  const uint64_t least = t.best[top - 1];  // of what is there
-  float bound = -HUGE_VALF, left = low;
-  for (int k = 0; k < (top + kWaves - 1) / kWaves; ++k) {
-    bound = wave_max(left);
+// The wave's q-th largest value (or less, where several are equal to it).
+__device__ __forceinline__ float wave_bound(float x, int q) {
+  if (q > 6) {  // by the number of larger lanes: 64 steps that do not wait for each other
+    int larger = 0;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) larger += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), k)) > x;
+    return -wave_max(larger < q ? -x : -HUGE_VALF);
+  }
+  float bound = -HUGE_VALF;
+  for (int k = 0; k < q; ++k) {
+    bound = wave_max(x);
     if (bound == -HUGE_VALF) break;
-    if (lane == __ffsll((unsigned long long)__ballot(left == bound)) - 1) left = -HUGE_VALF;
+    if ((int)threadIdx.x % 64 == __ffsll((unsigned long long)__ballot(x == bound)) - 1) x = -HUGE_VALF;
   }
-  bound = join.of_waves(bound, [](float p, float q) { return fminf(p, q); });  // a barrier: t.best has been read
-  if (tid == 0) t.count = 0;
-  __syncthreads();
-  if (plain && low >= bound) {
-    c.each([&](float v, int at) {
-      if (v >= bound && v != -HUGE_VALF) {
-        const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
-        if (key > least) {
-          const int i = atomicAdd(&t.count, 1);
-          if (i < kCandidates) t.list[i] = key;
-        }
+  return bound;
+}
+
+// The values from bound on with keys above least join the list.
+template <class C>
+__device__ __forceinline__ void add_candidates(C& c, uint32_t base, float bound, uint64_t least, Top& t) {
+  c.each([&](float v, int at) {
+    if (!(v < bound) && v != -HUGE_VALF) {
+      const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
+      if (key > least) {
+        const int i = atomicAdd(&t.count, 1);
+        if (i < kCandidates) t.list[i] = key;
       }
-    }, [&](float v) { return v >= bound; });
-  }
-  __syncthreads();
+    }
+  }, [&](float v) { return !(v < bound); });
+}
+
+// f(place, key) of the `top` largest of a chunk's candidates (those of the whole block are in the list) and of the chunks
+// before; places without one are left out.  All threads come; x, n: the chunk, where the list was too short.
+template <int THREADS, class T, class F>
+__device__ __forceinline__ void take_top(const T* x, int n, uint32_t base, int top, Top& t, F&& f) {
+  const int tid = threadIdx.x;
   int count = t.count;
-  if (!plain || count > kCandidates) {
+  if (count > kCandidates) {
     __syncthreads();
     uint64_t last = ~0ull;
     count = 0;
     for (int k = 0; k < top; ++k) {
       uint64_t best = 0;
-      for (int at = tid; at < c.n; at += THREADS) {  // from memory: the registers hold the other path's row
+      for (int at = tid; at < n; at += THREADS) {
         const uint32_t rank = rank_of((float)x[at]);
         const uint64_t key = rank ? key_of(rank, base + (uint32_t)at) : 0;
         if (key > best && key < last) best = key;
       }
       best = wave_max_key(best);
-      if (kWaves > 1) {
-        if (lane == 0) t.part[tid / 64] = best;
+      if (THREADS > 64) {
+        if (tid % 64 == 0) t.part[tid / 64] = best;
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) best = std::max(best, t.part[w]);
+        for (int w = 0; w < THREADS / 64; ++w) best = std::max(best, t.part[w]);
       }
-      if (tid == 0 && best) t.list[k] = best;
+      if (tid == 0) t.list[k] = best;
       __syncthreads();
       if (!best) break;
       last = best;
       ++count;
     }
   }
-  // the former best join the candidates
-  if (base) {
-    if (tid < top) t.list[count + tid] = t.best[tid];
-    count += top;
-  }
-  __syncthreads();
-  if (tid < top) t.best[tid] = 0;
-  __syncthreads();
-  for (int i = tid; i < count; i += THREADS) {
-    const uint64_t key = t.list[i];
+  const int before = base ? top : 0;
+  for (int i = tid; i < count + before; i += THREADS) {
+    const uint64_t key = i < count ? t.list[i] : t.best[i - count];
     int larger = 0;
     for (int k = 0; k < count; ++k) larger += t.list[k] > key;
-    if (key && larger < top) t.best[larger] = key;
+    for (int k = 0; k < before; ++k) larger += t.best[k] > key;
+    if (key && larger < top) f(larger, key);
   }
-  __syncthreads();
 }
 
 // A row's gradient, p (c0 + c1 log p) + [j = target] up with scale in the factors.  One without factors is zeros, whatever the
@@ -317,8 +316,13 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
     const float xt = here ? (float)x[at] : -HUGE_VALF;
     Stats r{-HUGE_VALF, 0.0f, 0.0f, here ? xt * a.scale : -HUGE_VALF};
     if constexpr (MODE == kTop) {
-      if (threadIdx.x < (unsigned)a.top) top.best[threadIdx.x] = 0;
-      __syncthreads();
+      if (threadIdx.x == 0) top.count = 0;
+      if (threadIdx.x < (unsigned)a.top) {
+        top.best[threadIdx.x] = 0;
+        o.top_ids[(int64_t)t * a.top + threadIdx.x] = -1;
+        o.top_logp[(int64_t)t * a.top + threadIdx.x] = -HUGE_VALF;
+      }
+      if (THREADS == 64) __syncthreads();  // larger blocks meet in their joins
     }
     C c;
     float s = 0.0f, u = 0.0f;
@@ -327,7 +331,11 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       c.load(x + base, n);
       float low = -HUGE_VALF;
       c.each([&](float v, int) { low = fmaxf(low, v); });
-      const float m = fmaxf(r.m, join.of_waves(wave_max(low), [](float p, float q) { return fmaxf(p, q); }) * a.scale);
+      float2 w = {wave_max(low), 0.0f};
+      if (MODE == kTop) w.y = wave_bound(low, (a.top + THREADS / 64 - 1) / (THREADS / 64));
+      w = join.most_and_least(w);
+      const float m = fmaxf(r.m, w.x * a.scale);
+      if constexpr (MODE == kTop) add_candidates(c, (uint32_t)base, w.y, base ? top.best[a.top - 1] : 0, top);
       const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
       if (base) {
         const float d = r.m == -HUGE_VALF ? 0.0f : r.m - from, f = fast_exp(d);  // where nothing was visible s and u are 0
@@ -341,9 +349,17 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
         if (MODE != kLoss) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
       });
       if constexpr (MODE == kTop) {
-        const float odd = s != s ? 1.0f : 0.0f;
-        const bool plain = !(join.sum(odd, 0.0f).x > 0.0f);
-        join_top(c, x + base, (uint32_t)base, a.top, low, plain, top, join);
+        if (base + C::kAll < a.rows) {  // more chunks
+          uint64_t mine[2] = {0, 0};
+          int place[2] = {-1, -1}, k = 0;
+          __syncthreads();
+          take_top<THREADS>(x + base, n, (uint32_t)base, a.top, top, [&](int at, uint64_t key) { place[k & 1] = at, mine[k++ & 1] = key; });
+          __syncthreads();
+          if (threadIdx.x == 0) top.count = 0;
+          for (int i = 0; i < 2; ++i)
+            if (place[i] >= 0) top.best[place[i]] = mine[i];
+          __syncthreads();
+        }
       }
     }
     const float2 su = join.sum(s, u);
@@ -374,12 +390,13 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
         if (here && k >= 0 && k < n && c.mine((int)k)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
       }
     } else if constexpr (MODE == kTop) {
-      if (threadIdx.x < (unsigned)a.top) {
-        const uint64_t best = top.best[threadIdx.x];
-        const float z = of_rank((uint32_t)(best >> 32)) * a.scale;
-        o.top_ids[(int64_t)t * a.top + threadIdx.x] = best ? (int32_t)(~(uint32_t)best + (uint32_t)a.vocab_begin) : -1;
-        o.top_logp[(int64_t)t * a.top + threadIdx.x] = !best ? -HUGE_VALF : o.stats ? z : z - l;
-      }
+      if (THREADS == 64) __syncthreads();  // else the sums' join was the barrier after the last candidate
+      const int64_t base = (a.rows - 1) / C::kAll * C::kAll;
+      take_top<THREADS>(x + base, (int)(a.rows - base), (uint32_t)base, a.top, top, [&](int at, uint64_t key) {
+        const float z = of_rank((uint32_t)(key >> 32)) * a.scale;
+        o.top_ids[(int64_t)t * a.top + at] = (int32_t)(~(uint32_t)key + (uint32_t)a.vocab_begin);
+        o.top_logp[(int64_t)t * a.top + at] = o.stats ? z : z - l;
+      });
       __syncthreads();
     }
   }
