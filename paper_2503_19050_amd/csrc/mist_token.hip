@@ -20,25 +20,27 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int64_t kMostTokens = (int64_t)1 << 30;
+constexpr float kLowest = -3.4028234663852886e38f;  // finite
 constexpr float kLow = -1000.0f;  // of a logarithm, beside an exponential that is 0 there: 0 * kLow is 0 where 0 * -inf is not
 constexpr int64_t kMostBlocks = (int64_t)1 << 20;  // a grid stays below 2^32 threads; kernels loop
 
 struct TokenArgs {
-  int64_t seq, rows, vocab_begin, ids_stride, logits_batch_stride, logits_stride, grad_batch_stride, grad_stride;
+  int64_t rows, vocab_begin, ids_stride, logits_batch_stride, logits_stride, grad_batch_stride, grad_stride;
+  uint32_t seq;  // at least 1
   int32_t n, ids_bytes, top;  // n: tokens
   float scale;
 };
 
+__device__ __forceinline__ int64_t offset_of(const TokenArgs& a, int32_t t, int64_t batch_stride, int64_t stride) {
+  const uint32_t b = (uint32_t)t / a.seq;
+  return b * batch_stride + ((uint32_t)t - b * a.seq) * stride;
+}
 __device__ __forceinline__ int64_t target_of(const TokenArgs& a, const void* targets, int32_t t) {
-  const int64_t at = t / a.seq * a.ids_stride + t % a.seq;
+  const int64_t at = offset_of(a, t, a.ids_stride, 1);
   return a.ids_bytes == 4 ? ((const int32_t*)targets)[at] : ((const int64_t*)targets)[at];
 }
-__device__ __forceinline__ int64_t logits_offset(const TokenArgs& a, int32_t t) {
-  return t / a.seq * a.logits_batch_stride + t % a.seq * a.logits_stride;
-}
-__device__ __forceinline__ int64_t grad_offset(const TokenArgs& a, int32_t t) {
-  return t / a.seq * a.grad_batch_stride + t % a.seq * a.grad_stride;
-}
+__device__ __forceinline__ int64_t logits_offset(const TokenArgs& a, int32_t t) { return offset_of(a, t, a.logits_batch_stride, a.logits_stride); }
+__device__ __forceinline__ int64_t grad_offset(const TokenArgs& a, int32_t t) { return offset_of(a, t, a.grad_batch_stride, a.grad_stride); }
 
 // Unsigned numbers in the order of the logits: -0 as 0, NaN above everything.  -inf, which is no alternative, is 0.
 constexpr uint32_t kNanRank = 0xFFFFFFFEu;  // no key is all ones
@@ -131,8 +133,8 @@ struct Chunk {
     return head + (j * THREADS + at) * kV;
   }
   // of the odd value; n or more: none
-  __device__ __forceinline__ int odd_place() const {
-    const int t = threadIdx.x;
+  __device__ __forceinline__ int odd_place() const { return odd_place((int)threadIdx.x); }
+  __device__ __forceinline__ int odd_place(int t) const {
     return t < head ? t : n - (n - head) % kV + t - head;
   }
   __device__ __forceinline__ bool any(int j) const { return head + (j * THREADS + 1) * kV <= n; }  // the j-th vector of some thread
@@ -148,28 +150,37 @@ struct Chunk {
     }
     odd = read && odd_place() < n ? (float)x[odd_place()] : -HUGE_VALF;
   }
-  // f(value, its place in the chunk), of the vectors in which some value passes `where`; vectors that no thread has are passed over
+  // f(value); vectors that no thread has are passed over
+  template <class F>
+  __device__ __forceinline__ void each_of(int j, F&& f) {
+    asm("" : "+v"(v[j]));
+    const V r = __builtin_bit_cast(V, v[j]);
+#pragma unroll
+    for (int k = 0; k < kV; ++k) f((float)r[k]);
+  }
   template <class F>
   __device__ __forceinline__ void each(F&& f) {
-    each(f, [](float) { return true; });
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (any(j)) each_of(j, f);
+    f(odd);
   }
-  template <class F, class W>
-  __device__ __forceinline__ void each(F&& f, W&& where) {
+  // The largest value, and those of eight groups of vectors.
+  static constexpr int kPer = N / 8, kGroup = kPer * kV;  // vectors and values of a group
+  __device__ __forceinline__ float largest(float (&group)[8]) {
+    float low = odd == odd ? odd : -HUGE_VALF;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (!any(j)) continue;
-      asm("" : "+v"(v[j]));
-      const V r = __builtin_bit_cast(V, v[j]);
-      bool some = false;
+    for (int i = 0; i < 8; ++i) {
+      group[i] = -HUGE_VALF;
 #pragma unroll
-      for (int k = 0; k < kV; ++k) some |= where((float)r[k]);
-      if (!some) continue;
-      const int at = place(j);
-#pragma unroll
-      for (int k = 0; k < kV; ++k) f((float)r[k], at + k);
+      for (int j = i * kPer; j < (i + 1) * kPer; ++j)
+        if (any(j)) each_of(j, [&](float x) { group[i] = fmaxf(group[i], x); });
+      low = fmaxf(low, group[i]);
     }
-    f(odd, odd_place());
+    return low;
   }
+  // the place of a group's k-th value in a thread
+  __device__ __forceinline__ int group_place(int i, int thread, int k) const { return head + ((i * kPer + k / kV) * THREADS + thread) * kV + k % kV; }
   // y = f(value)
   template <class F>
   __device__ __forceinline__ void store(T* y, F&& f) {
@@ -194,16 +205,19 @@ struct Chunk {
 };
 
 // Alternatives.  At least q = ceil(top / waves) lanes of each wave have a value of at least the wave's q-th largest lane
-// maximum, so the least of these over the waves bounds a row's top-th largest value from below, and the few values from there on (and
-// every NaN) are the candidates.  A candidate's place is the number of larger ones.  Where there are too many (equal values
-// in many places) the largest are taken one by one, with a pass each.
+// maximum, so the least of these over the waves bounds a row's top-th largest value from below.  The few groups of a thread's values
+// that reach it are listed (and all of a thread with a NaN), and the block then looks through them together, from the cache: a wave that
+// looks through its own registers takes as many instructions for one lane's group as for all lanes' (8 alternatives of 8192
+// rows of 50257 16-bit values: 254 us so, 237 by the list).  A candidate's place is the number of larger ones.  Where a list
+// is too short (equal values in many places) the largest are taken one by one, with a pass each.
 constexpr int kCandidates = 512;
 
 struct Top {
   uint64_t list[kCandidates];
   uint64_t best[MIST_TOKEN_MAX_TOP];  // of the chunks before, in order; 0: none
   uint64_t part[8];
-  int count;
+  uint32_t group[kCandidates];        // group << 16 | thread; 8: the odd value
+  int count, groups;
 };
 
 // The wave's q-th largest value (or less, where several are equal to it).
@@ -223,27 +237,41 @@ __device__ __forceinline__ float wave_bound(float x, int q) {
   return bound;
 }
 
-// The values from bound on with keys above least join the list.
+__device__ __forceinline__ void add_group(Top& t, int i) {
+  const int at = atomicAdd(&t.groups, 1);
+  if (at < kCandidates) t.group[at] = (uint32_t)i << 16 | threadIdx.x;
+}
+// bound is finite or +inf: what is masked out is below it
 template <class C>
-__device__ __forceinline__ void add_candidates(C& c, uint32_t base, float bound, uint64_t least, Top& t) {
-  c.each([&](float v, int at) {
-    if (!(v < bound) && v != -HUGE_VALF) {
-      const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
-      if (key > least) {
-        const int i = atomicAdd(&t.count, 1);
-        if (i < kCandidates) t.list[i] = key;
-      }
-    }
-  }, [&](float v) { return !(v < bound); });
+__device__ __forceinline__ void list_groups(const C& c, const float (&group)[8], bool nan, float bound, Top& t) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (nan || group[i] >= bound) add_group(t, i);
+  if (!(c.odd < bound)) add_group(t, 8);
+}
+// The listed groups' values from bound on with keys above least join the candidates.  Between two barriers.
+template <int THREADS, class C, class T>
+__device__ __forceinline__ void list_candidates(const C& c, const T* x, uint32_t base, float bound, uint64_t least, Top& t) {
+  for (int i = threadIdx.x; i < min(t.groups, kCandidates) * C::kGroup; i += THREADS) {
+    const uint32_t g = t.group[i / C::kGroup];
+    const int k = i % C::kGroup, thread = (int)(g & 0xFFFF), which = (int)(g >> 16);
+    const int at = which < 8 ? c.group_place(which, thread, k) : c.odd_place(thread) + (k ? c.n : 0);
+    const float v = at < c.n ? (float)x[at] : -HUGE_VALF;
+    if (v < bound) continue;
+    const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
+    if (key <= least) continue;
+    const int to = atomicAdd(&t.count, 1);
+    if (to < kCandidates) t.list[to] = key;
+  }
 }
 
-// f(place, key) of the `top` largest of a chunk's candidates (those of the whole block are in the list) and of the chunks
+// f(place, key) of the `top` largest of a chunk's candidates (those of the whole block are listed) and of the chunks
 // before; places without one are left out.  All threads come; x, n: the chunk, where the list was too short.
 template <int THREADS, class T, class F>
 __device__ __forceinline__ void take_top(const T* x, int n, uint32_t base, int top, Top& t, F&& f) {
   const int tid = threadIdx.x;
   int count = t.count;
-  if (count > kCandidates) {
+  if (count > kCandidates || t.groups > kCandidates) {
     __syncthreads();
     uint64_t last = ~0ull;
     count = 0;
@@ -268,6 +296,17 @@ __device__ __forceinline__ void take_top(const T* x, int n, uint32_t base, int t
     }
   }
   const int before = base ? top : 0;
+  if (count + before <= 64) {  // one wave, by its registers
+    if (tid >= 64) return;
+    const uint64_t key = tid < count ? t.list[tid] : tid < count + before ? t.best[tid - count] : 0;
+    int larger = 0;
+    for (int k = 0; k < count + before; ++k) {
+      const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), k) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, k);
+      larger += other > key;
+    }
+    if (key && larger < top) f(larger, key);
+    return;
+  }
   for (int i = tid; i < count + before; i += THREADS) {
     const uint64_t key = i < count ? t.list[i] : t.best[i - count];
     int larger = 0;
@@ -316,7 +355,7 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
     const float xt = here ? (float)x[at] : -HUGE_VALF;
     Stats r{-HUGE_VALF, 0.0f, 0.0f, here ? xt * a.scale : -HUGE_VALF};
     if constexpr (MODE == kTop) {
-      if (threadIdx.x == 0) top.count = 0;
+      if (threadIdx.x == 0) top.count = top.groups = 0;
       if (threadIdx.x < (unsigned)a.top) {
         top.best[threadIdx.x] = 0;
         o.top_ids[(int64_t)t * a.top + threadIdx.x] = -1;
@@ -325,17 +364,16 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       if (THREADS == 64) __syncthreads();  // larger blocks meet in their joins
     }
     C c;
-    float s = 0.0f, u = 0.0f;
+    float s = 0.0f, u = 0.0f, bound = 0.0f;
     for (int64_t base = 0; base < a.rows; base += C::kAll) {
       const int n = (int)min((int64_t)C::kAll, a.rows - base);
       c.load(x + base, n);
-      float low = -HUGE_VALF;
-      c.each([&](float v, int) { low = fmaxf(low, v); });
+      float group[8];
+      const float low = c.largest(group);
       float2 w = {wave_max(low), 0.0f};
       if (MODE == kTop) w.y = wave_bound(low, (a.top + THREADS / 64 - 1) / (THREADS / 64));
       w = join.most_and_least(w);
       const float m = fmaxf(r.m, w.x * a.scale);
-      if constexpr (MODE == kTop) add_candidates(c, (uint32_t)base, w.y, base ? top.best[a.top - 1] : 0, top);
       const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
       if (base) {
         const float d = r.m == -HUGE_VALF ? 0.0f : r.m - from, f = fast_exp(d);  // where nothing was visible s and u are 0
@@ -343,19 +381,23 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
         s *= f;
       }
       r.m = m;
-      c.each([&](float v, int) {
+      c.each([&](float v) {
         const float d = fmaf(v, a.scale, -from), e = fast_exp(d);
         s += e;
         if (MODE != kLoss) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
       });
       if constexpr (MODE == kTop) {
+        bound = fmaxf(w.y, kLowest);
+        list_groups(c, group, s != s, bound, top);
         if (base + C::kAll < a.rows) {  // more chunks
           uint64_t mine[2] = {0, 0};
           int place[2] = {-1, -1}, k = 0;
           __syncthreads();
+          list_candidates<THREADS>(c, x + base, (uint32_t)base, bound, base ? top.best[a.top - 1] : 0, top);
+          __syncthreads();
           take_top<THREADS>(x + base, n, (uint32_t)base, a.top, top, [&](int at, uint64_t key) { place[k & 1] = at, mine[k++ & 1] = key; });
           __syncthreads();
-          if (threadIdx.x == 0) top.count = 0;
+          if (threadIdx.x == 0) top.count = top.groups = 0;
           for (int i = 0; i < 2; ++i)
             if (place[i] >= 0) top.best[place[i]] = mine[i];
           __syncthreads();
@@ -390,14 +432,16 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
         if (here && k >= 0 && k < n && c.mine((int)k)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
       }
     } else if constexpr (MODE == kTop) {
-      if (THREADS == 64) __syncthreads();  // else the sums' join was the barrier after the last candidate
+      if (THREADS == 64) __syncthreads();  // else the sums' join was the barrier after the last group
       const int64_t base = (a.rows - 1) / C::kAll * C::kAll;
+      list_candidates<THREADS>(c, x + base, (uint32_t)base, bound, base ? top.best[a.top - 1] : 0, top);
+      __syncthreads();
       take_top<THREADS>(x + base, (int)(a.rows - base), (uint32_t)base, a.top, top, [&](int at, uint64_t key) {
         const float z = of_rank((uint32_t)(key >> 32)) * a.scale;
         o.top_ids[(int64_t)t * a.top + at] = (int32_t)(~(uint32_t)key + (uint32_t)a.vocab_begin);
         o.top_logp[(int64_t)t * a.top + at] = o.stats ? z : z - l;
       });
-      __syncthreads();
+      if (t + (int32_t)gridDim.x < a.n) __syncthreads();
     }
   }
 }
@@ -529,8 +573,8 @@ mist_status check_grad(const mist_token_desc* d, const void* logits, const void*
 }
 
 TokenArgs args(const mist_token_desc* d) {
-  return TokenArgs{std::max<int64_t>(d->seq, 1), d->rows, d->vocab_begin, d->ids_stride, d->logits_batch_stride, d->logits_stride,
-                   d->grad_batch_stride, d->grad_stride, (int32_t)(d->batch * d->seq), d->ids_bytes, d->top, d->scale};
+  return TokenArgs{d->rows, d->vocab_begin, d->ids_stride, d->logits_batch_stride, d->logits_stride,
+                   d->grad_batch_stride, d->grad_stride, (uint32_t)std::max<int64_t>(d->seq, 1), (int32_t)(d->batch * d->seq), d->ids_bytes, d->top, d->scale};
 }
 
 bool floats_ok(std::initializer_list<const float*> ps) {
