@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mist_ops.h"
 
@@ -22,7 +23,7 @@ namespace {
 constexpr int kMostWaves = 16;
 constexpr int64_t kMostTokens = (int64_t)1 << 30;
 constexpr int64_t kMostBlocks = 4096;  // of the forward pass; they take rows in turn
-constexpr int64_t kParts = 1024;       // of the backward pass, about
+constexpr int64_t kPartWaves = 5120;   // of the backward pass, about
 constexpr int64_t kPartRows = 8;       // a part has at least, where there are as many
 constexpr int kSlots = 5;              // gradients summed over tokens
 constexpr int kJoinThreads = 1024;
@@ -53,52 +54,52 @@ __device__ __forceinline__ Float8 masked(Float8 x, int64_t left) {
   return x;
 }
 
-// Sums over the block.  Two buffers in turn: a wave writes one only after every wave has read its last values.
+// The sum over the rows that lie beside each other in a wave.
+template <int L>
+__device__ __forceinline__ Float8 over_rows(Float8 x) {
+  if (L < 64) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (L == 16) x[k] = mist::join_pairs_of_16(x[k], [](float p, float q) { return p + q; });
+      x[k] = mist::join_pairs_of_32(x[k], [](float p, float q) { return p + q; });
+    }
+  }
+  return x;
+}
+
+// Sums over a row's lanes: L of a wave (16 or 32: rows of up to 128 or 256 columns lie beside each other in it), or all waves of the block.
+// Waves meet in two places in turn: one writes a place only after every wave has read its last values.
+template <int L>
 struct Join {
   float2* part;  // [2][kMostWaves]
   int waves, turn;
-  __device__ __forceinline__ float2 sum(float a, float b) {
-    a = wave_sum(a);
-    b = wave_sum(b);
-    if (waves == 1) return float2{a, b};
+  __device__ __forceinline__ const float2* meet(float a, float b) {
     float2* p = part + turn * kMostWaves;
     turn ^= 1;
     if (threadIdx.x % 64 == 0) p[threadIdx.x / 64] = float2{a, b};
     __syncthreads();
+    return p;
+  }
+  __device__ __forceinline__ float2 sum(float a, float b) {
+    a = wave_sum<L>(a);
+    b = wave_sum<L>(b);
+    if (L < 64 || waves == 1) return float2{a, b};
+    const float2* p = meet(a, b);
     float2 s = p[0];
     for (int k = 1; k < waves; ++k) s.x += p[k].x, s.y += p[k].y;
     return s;
   }
 };
 
-struct Moments {
-  float mean, r;
-};
-// The variance is of the distances from the mean, not a difference of squares.
-template <int U>
-__device__ __forceinline__ Moments moments(const BlockArgs& a, Join& join, const Float8* x, const int* left) {
-  float mean = 0.0f, s = 0.0f;
-  if (a.layer) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) s += sum8(x[u]);
-    mean = join.sum(s, 0.0f).x * a.inv_hidden;
-    s = 0.0f;
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const Float8 d = masked(x[u] - mean, left[u]);
-    s += sum8(d * d);
-  }
-  return Moments{mean, 1.0f / sqrtf(join.sum(s, 0.0f).x * a.inv_hidden + a.eps)};
-}
-
-template <int U>
+// A thread's columns.
+template <int U, int L>
 struct Columns {
   int col[U], left[U];
   __device__ __forceinline__ explicit Columns(const BlockArgs& a) {
+    const int lane = L < 64 ? (int)threadIdx.x % L : (int)threadIdx.x, all = L < 64 ? L : (int)blockDim.x;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      col[u] = (u * (int)blockDim.x + (int)threadIdx.x) * 8;
+      col[u] = (u * all + lane) * 8;
       left[u] = (int)a.hidden - col[u];  // none where <= 0
     }
   }
@@ -109,46 +110,121 @@ __device__ __forceinline__ void each(F&& f) {
   for (int u = 0; u < U; ++u) f(u);
 }
 
+struct Moments {
+  float mean, r;
+};
+// The variance is of the distances from the mean, not a difference of squares: of each wave's values from that wave's mean, and of
+// the waves' means, so that the waves meet once.
+template <int U, int L>
+__device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, const Columns<U, L>& c, const Float8* x) {
+  float s = 0.0f, q = 0.0f;
+  if (!a.layer) {
+    each<U>([&](int u) { s += sum8(x[u] * x[u]); });
+    return Moments{0.0f, 1.0f / sqrtf(join.sum(s, 0.0f).x * a.inv_hidden + a.eps)};
+  }
+  each<U>([&](int u) { s += sum8(x[u]); });
+  s = wave_sum<L>(s);
+  auto count = [&](int wave) {  // columns of a wave
+    int n = 0;
+    each<U>([&](int u) { n += min(max((int)a.hidden - (u * (int)blockDim.x + wave * 64) * 8, 0), 512); });
+    return (float)n;
+  };
+  const bool alone = L < 64 || join.waves == 1;
+  const float near = alone ? s * a.inv_hidden : s / count((int)threadIdx.x / 64);
+  each<U>([&](int u) {
+    const Float8 d = masked(x[u] - near, c.left[u]);
+    q += sum8(d * d);
+  });
+  q = wave_sum<L>(q);
+  float mean = near;
+  if (!alone) {
+    const float2* p = join.meet(s, q);
+    mean = 0.0f, q = 0.0f;
+    for (int k = 0; k < join.waves; ++k) mean += p[k].x;
+    mean *= a.inv_hidden;
+    for (int k = 0; k < join.waves; ++k) {
+      const float n = count(k), d = p[k].x / n - mean;
+      q += fmaf(n * d, d, p[k].y);
+    }
+  }
+  return Moments{mean, 1.0f / sqrtf(q * a.inv_hidden + a.eps)};
+}
+
+// Rows of one reading, before they are converted.
 template <class A, class R, int U>
-__global__ __launch_bounds__(kMostWaves * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
+struct Input {
+  mist::Raw8<R> x[U];
+  mist::Raw8<A> b[U];
+};
+
+// Waves of the largest block of a kernel: rows beside each other in one, and what more than eight need, 128 registers at most, is not
+// asked of smaller ones.
+constexpr int most_waves(int u, int l, bool wide) { return l < 64 ? 1 : u == 1 && !wide ? kMostWaves / 2 : kMostWaves; }
+
+// The next row is read before the sums of this one are waited for, where the registers are there.
+template <class A, class R, int U, int L, bool WIDE>
+__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
+  constexpr int kRows = 64 / L;  // of a block at a time
   __shared__ float2 part[2 * kMostWaves];
-  Join join{part, (int)blockDim.x / 64, 0};
-  const Columns<U> c(a);
+  Join<L> join{part, (int)blockDim.x / 64, 0};
+  const Columns<U, L> c(a);
   Float8 w[U] = {}, wb[U] = {}, pw[U] = {}, pb[U] = {}, gate[U];
   each<U>([&](int u) {
     if (a.weight) w[u] = load_weight(a.weight, a.weight_type, c.col[u], c.left[u]);
     if (a.bias) wb[u] = load_weight(a.bias, a.weight_type, c.col[u], c.left[u]);
     if (a.post_weight) pw[u] = load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]);
     if (a.post_bias) pb[u] = load_weight(a.post_bias, a.weight_type, c.col[u], c.left[u]);
-    gate[u] = 1.0f;
-    if (a.gate && !a.gate_stride) gate[u] = load_weight(a.gate, a.weight_type, c.col[u], c.left[u]);
+    gate[u] = a.block_scale;
+    if (a.gate && !a.gate_stride) gate[u] *= load_weight(a.gate, a.weight_type, c.col[u], c.left[u]);
   });
-  for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
+  const int sub = L < 64 ? (int)threadIdx.x / L : 0;
+  auto read = [&](int64_t t0) {
+    const int64_t t = min(t0 + sub, a.n - 1);
+    Input<A, R, U> in;
+    each<U>([&](int u) {
+      in.x[u] = mist::load_raw8(x + t * a.x_stride + c.col[u], c.left[u]);
+      if (block) in.b[u] = mist::load_raw8(block + t * a.block_stride + c.col[u], c.left[u]);
+    });
+    return in;
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  Input<A, R, U> in;
+  if (U == 1) in = read((int64_t)blockIdx.x * kRows);
+  for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.n; t0 += step) {
+    const int64_t t = t0 + sub;
+    const bool there = L == 64 || t < a.n;
+    Input<A, R, U> now;
+    if constexpr (U == 1) {
+      now = in;
+      if (t0 + step < a.n) in = read(t0 + step);
+    } else {
+      now = read(t0);
+    }
     Float8 v[U];
-    each<U>([&](int u) { v[u] = load8(x + t * a.x_stride + c.col[u], c.left[u]); });
+    each<U>([&](int u) { v[u] = mist::wide8<R>(now.x[u]); });
     Moments before{0.0f, 1.0f}, after{0.0f, 1.0f};
     if (block) {
       Float8 b[U];
       each<U>([&](int u) {
-        b[u] = load8(block + t * a.block_stride + c.col[u], c.left[u]);
-        if (a.gate_stride) gate[u] = load_weight(a.gate, a.weight_type, t / a.seq * a.gate_stride + c.col[u], c.left[u]);
+        b[u] = mist::wide8<A>(now.b[u]);
+        if (a.gate_stride) gate[u] = a.block_scale * load_weight(a.gate, a.weight_type, min(t, a.n - 1) / a.seq * a.gate_stride + c.col[u], c.left[u]);
       });
       if (a.post_weight) {
-        before = moments<U>(a, join, b, c.left);
+        before = moments<U, L>(a, join, c, b);
         each<U>([&](int u) { b[u] = (b[u] - before.mean) * before.r * pw[u] + pb[u]; });
       }
       each<U>([&](int u) {
-        v[u] = a.res_scale * v[u] + a.block_scale * (b[u] * gate[u]);
-        store8(y + t * a.y_stride + c.col[u], c.left[u], v[u]);
-        // the norm is of y as it is stored
-        v[u] = masked(__builtin_convertvector(__builtin_convertvector(v[u], typename mist::Vec<R, 8>::type), Float8), c.left[u]);
+        v[u] = a.res_scale * v[u] + b[u] * gate[u];
+        if (there) store8(y + t * a.y_stride + c.col[u], c.left[u], v[u]);
+        // the norm is of y as it is stored: formed again from it, h has the same bits
+        v[u] = masked(mist::wide8<R>(__builtin_convertvector(v[u], mist::Raw8<R>)), c.left[u]);
       });
     }
     if (h) {
-      after = moments<U>(a, join, v, c.left);
-      each<U>([&](int u) { store8(h + t * a.h_stride + c.col[u], c.left[u], (v[u] - after.mean) * after.r * w[u] + wb[u]); });
+      after = moments<U, L>(a, join, c, v);
+      if (there) each<U>([&](int u) { store8(h + t * a.h_stride + c.col[u], c.left[u], (v[u] - after.mean) * after.r * w[u] + wb[u]); });
     }
-    if (threadIdx.x == 0) *(float4*)(stats + t * 4) = float4{before.mean, before.r, after.mean, after.r};
+    if (there && c.col[0] == 0) *(float4*)(stats + t * 4) = float4{before.mean, before.r, after.mean, after.r};
   }
 }
 
@@ -167,92 +243,143 @@ struct BackArgs {
   int32_t accumulate;
 };
 
-template <class A, class R, int U, bool MORE>
-__global__ __launch_bounds__(kMostWaves * 64) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy,
-                                                              R* dx, A* dblock) {
+template <class A, class R, int U>
+struct BackInput {
+  mist::Raw8<R> y[U], dy[U];
+  mist::Raw8<A> b[U], dh[U];
+  float4 st;
+};
+
+// With e the gradient of gate v (v = n post_weight + post_bias) over a sequence's tokens, the sums of e and of e n are all
+// that the gradients of gate, post_weight and post_bias need: two sums a column for three.
+template <class A, class R, int U, int L, bool WIDE, bool MORE>
+__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
+                                                                          A* dblock) {
+  constexpr bool kAhead = U == 1 && !(MORE && WIDE);
+  constexpr int kRows = 64 / L;
   __shared__ float2 shared[2 * kMostWaves];
   const BlockArgs& a = k.a;
-  Join join{shared, (int)blockDim.x / 64, 0};
-  const Columns<U> c(a);
-  Float8 w[U] = {}, pw[U] = {}, pb[U] = {}, gate[U];
-  Float8 sw[U] = {}, sb[U] = {}, spw[U] = {}, spb[U] = {}, sg[U] = {};
+  Join<L> join{shared, (int)blockDim.x / 64, 0};
+  const Columns<U, L> c(a);
+  Float8 w[U] = {}, gp[U];  // gp: gate post_weight
+  Float8 sw[U] = {}, sb[U] = {}, sen[U], se[U];
   each<U>([&](int u) {
     if (a.weight) w[u] = load_weight(a.weight, a.weight_type, c.col[u], c.left[u]);
-    if (MORE && a.post_weight) pw[u] = load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]);
-    if (MORE && a.post_bias) pb[u] = load_weight(a.post_bias, a.weight_type, c.col[u], c.left[u]);
-    gate[u] = 1.0f;
-    if (MORE && a.gate && !a.gate_stride) gate[u] = load_weight(a.gate, a.weight_type, c.col[u], c.left[u]);
   });
+  auto post_weight = [&](int u) { return a.post_weight ? load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]) : Float8(1.0f); };
+  auto gate = [&](int u, int64_t s) { return a.gate ? load_weight(a.gate, a.weight_type, s * a.gate_stride + c.col[u], c.left[u]) : Float8(1.0f); };
+  const int sub = L < 64 ? (int)threadIdx.x / L : 0;
   const int64_t part = blockIdx.x, first = part / k.parts.pieces * k.parts.seqs, row0 = part % k.parts.pieces * k.parts.rows;
-  for (int64_t s = first; s < min(first + k.parts.seqs, k.parts.batch); ++s) {
-    if (MORE && a.gate_stride) each<U>([&](int u) { gate[u] = load_weight(a.gate, a.weight_type, s * a.gate_stride + c.col[u], c.left[u]); });
-    for (int64_t r = row0; r < min(row0 + k.parts.rows, k.parts.seq); ++r) {
-      const int64_t t = s * k.parts.seq + r;
-      const float4 st = *(const float4*)(stats + t * 4);
-      Float8 d[U], b[U];
-      each<U>([&](int u) { d[u] = dy ? load8(dy + t * k.dy_stride + c.col[u], c.left[u]) : Float8{}; });
-      if (block) each<U>([&](int u) { b[u] = load8(block + t * a.block_stride + c.col[u], c.left[u]); });
+  const int64_t last = min(first + k.parts.seqs, k.parts.batch), row1 = min(row0 + k.parts.rows, k.parts.seq);
+  auto read = [&](int64_t s, int64_t r0) {
+    const int64_t t = s * k.parts.seq + min(r0 + sub, row1 - 1);
+    BackInput<A, R, U> in;
+    each<U>([&](int u) {
+      if (dh) in.dh[u] = mist::load_raw8(dh + t * k.dh_stride + c.col[u], c.left[u]);
+      if (dh) in.y[u] = mist::load_raw8(y + t * a.y_stride + c.col[u], c.left[u]);
+      if (dy) in.dy[u] = mist::load_raw8(dy + t * k.dy_stride + c.col[u], c.left[u]);
+      if (MORE && block) in.b[u] = mist::load_raw8(block + t * a.block_stride + c.col[u], c.left[u]);
+    });
+    in.st = *(const float4*)(stats + t * 4);
+    return in;
+  };
+  BackInput<A, R, U> in;
+  if (kAhead) in = read(first, row0);
+  for (int64_t s = first; s < last; ++s) {
+    each<U>([&](int u) {
+      if (MORE) gp[u] = gate(u, s) * post_weight(u);
+      sen[u] = se[u] = 0.0f;
+    });
+    for (int64_t r0 = row0; r0 < row1; r0 += kRows) {
+      const int64_t t = s * k.parts.seq + r0 + sub;
+      const bool there = L == 64 || r0 + sub < row1;
+      BackInput<A, R, U> now;
+      if constexpr (kAhead) {
+        now = in;
+        if (r0 + kRows < row1) in = read(s, r0 + kRows);
+        else if (s + 1 < last) in = read(s + 1, row0);
+      } else {
+        now = read(s, r0);
+      }
+      const float4 st = now.st;
+      Float8 d[U];
+      each<U>([&](int u) { d[u] = dy ? mist::wide8<R>(now.dy[u]) : Float8(0.0f); });
       if (dh) {
         Float8 g[U], n[U];
         float p = 0.0f, q = 0.0f;
         each<U>([&](int u) {
-          g[u] = load8(dh + t * k.dh_stride + c.col[u], c.left[u]);
-          n[u] = (load8(y + t * a.y_stride + c.col[u], c.left[u]) - st.z) * st.w;
-          sb[u] += g[u];
-          sw[u] += g[u] * n[u];
+          g[u] = mist::wide8<A>(now.dh[u]);
+          n[u] = (mist::wide8<R>(now.y[u]) - st.z) * st.w;
+          if (there) {
+            sb[u] += g[u];
+            sw[u] += g[u] * n[u];
+          }
           g[u] *= w[u];
           p += sum8(g[u]);
-          q += sum8(g[u] * n[u]);
+          q += sum8(masked(g[u] * n[u], c.left[u]));
         });
         const float2 m = join.sum(p, q);
         const float mean = a.layer ? m.x * a.inv_hidden : 0.0f, along = m.y * a.inv_hidden;
         each<U>([&](int u) { d[u] += st.w * (g[u] - mean - n[u] * along); });
       }
-      if (dx) each<U>([&](int u) { store8(dx + t * k.dx_stride + c.col[u], c.left[u], a.res_scale * d[u]); });
+      if (dx && there) each<U>([&](int u) { store8(dx + t * k.dx_stride + c.col[u], c.left[u], a.res_scale * d[u]); });
       if (block) {
         each<U>([&](int u) { d[u] *= a.block_scale; });
         if (MORE) {
+          Float8 n[U];
+          each<U>([&](int u) {
+            n[u] = masked((mist::wide8<A>(now.b[u]) - st.x) * st.y, c.left[u]);
+            if (there) {
+              se[u] += d[u];
+              sen[u] += d[u] * n[u];
+            }
+            d[u] = masked(d[u] * gp[u], c.left[u]);
+          });
           if (a.post_weight) {
             float p = 0.0f, q = 0.0f;
             each<U>([&](int u) {
-              b[u] = masked((b[u] - st.x) * st.y, c.left[u]);
-              sg[u] += d[u] * (b[u] * pw[u] + pb[u]);
-              d[u] = masked(d[u] * gate[u], c.left[u]);
-              spb[u] += d[u];
-              spw[u] += d[u] * b[u];
-              d[u] *= pw[u];
               p += sum8(d[u]);
-              q += sum8(d[u] * b[u]);
+              q += sum8(d[u] * n[u]);
             });
             const float2 m = join.sum(p, q);
             const float mean = a.layer ? m.x * a.inv_hidden : 0.0f, along = m.y * a.inv_hidden;
-            each<U>([&](int u) { d[u] = st.y * (d[u] - mean - b[u] * along); });
-          } else {
-            each<U>([&](int u) {
-              sg[u] += d[u] * b[u];
-              d[u] *= gate[u];
-            });
+            each<U>([&](int u) { d[u] = st.y * (d[u] - mean - n[u] * along); });
           }
         }
-        if (dblock) each<U>([&](int u) { store8(dblock + t * k.dblock_stride + c.col[u], c.left[u], d[u]); });
+        if (dblock && there) each<U>([&](int u) { store8(dblock + t * k.dblock_stride + c.col[u], c.left[u], d[u]); });
       }
     }
-    if (MORE && k.dgate) {
+    if (MORE) {
       each<U>([&](int u) {
+        se[u] = over_rows<L>(se[u]);
+        sen[u] = over_rows<L>(sen[u]);
+        if (sub) return;
+        const Float8 g = gate(u, s);
+        const int64_t at = part * a.hidden + c.col[u];
+        auto add = [&](float* p, Float8 x) {  // the part's sum over its sequences
+          if (s > first) x += load8(p + at, c.left[u]);
+          store8(p + at, c.left[u], x);
+        };
+        if (k.slot[2]) add(k.slot[2], g * sen[u]);
+        if (k.slot[3]) add(k.slot[3], g * se[u]);
+        if (!k.slot[4] && !k.dgate) return;
+        Float8 x = sen[u];
+        if (a.post_weight) x *= post_weight(u);
+        if (a.post_bias) x += load_weight(a.post_bias, a.weight_type, c.col[u], c.left[u]) * se[u];
+        if (k.slot[4]) add(k.slot[4], x);
+        if (!k.dgate) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (i < c.left[u]) store_weight(k.dgate, a.weight_type, s * k.dgate_stride + c.col[u] + i, sg[u][i], k.accumulate);
-        sg[u] = 0.0f;
+          if (i < c.left[u]) store_weight(k.dgate, a.weight_type, s * k.dgate_stride + c.col[u] + i, x[i], k.accumulate);
       });
     }
   }
   each<U>([&](int u) {
     const int64_t at = part * a.hidden + c.col[u];
-    if (k.slot[0]) store8(k.slot[0] + at, c.left[u], sw[u]);
-    if (k.slot[1]) store8(k.slot[1] + at, c.left[u], sb[u]);
-    if (MORE && k.slot[2]) store8(k.slot[2] + at, c.left[u], spw[u]);
-    if (MORE && k.slot[3]) store8(k.slot[3] + at, c.left[u], spb[u]);
-    if (MORE && k.slot[4]) store8(k.slot[4] + at, c.left[u], sg[u]);
+    sw[u] = over_rows<L>(sw[u]);
+    sb[u] = over_rows<L>(sb[u]);
+    if (k.slot[0] && !sub) store8(k.slot[0] + at, c.left[u], sw[u]);
+    if (k.slot[1] && !sub) store8(k.slot[1] + at, c.left[u], sb[u]);
   });
 }
 
@@ -347,18 +474,24 @@ bool weights_ok(const mist_block_desc* d, std::initializer_list<const void*> ps)
   return true;
 }
 
+int lanes(int64_t hidden) { return hidden <= 128 ? 16 : hidden <= 256 ? 32 : 64; }
 int units(int64_t hidden) { return hidden > kMostWaves * 512 ? 2 : 1; }
 unsigned threads(int64_t hidden) { return (unsigned)((hidden + units(hidden) * 512 - 1) / (units(hidden) * 512) * 64); }
 
-// f(activation type, residual type, columns a thread / 8)
+// f(activation type, residual type, columns a thread / 8, lanes a row, more than eight waves)
 template <class F>
 void with_kernel(const mist_block_desc* d, F&& f) {
   mist::with_type(d->type, [&](auto x) {
     using A = typename decltype(x)::type;
     auto run = [&](auto r) {
       using R = typename decltype(r)::type;
-      if (units(d->hidden) == 2) f(A{}, R{}, std::integral_constant<int, 2>{});
-      else f(A{}, R{}, std::integral_constant<int, 1>{});
+      using One = std::integral_constant<int, 1>;
+      using Wave = std::integral_constant<int, 64>;
+      if (units(d->hidden) == 2) f(A{}, R{}, std::integral_constant<int, 2>{}, Wave{}, std::true_type{});
+      else if (lanes(d->hidden) == 32) f(A{}, R{}, One{}, std::integral_constant<int, 32>{}, std::false_type{});
+      else if (lanes(d->hidden) == 16) f(A{}, R{}, One{}, std::integral_constant<int, 16>{}, std::false_type{});
+      else if (threads(d->hidden) > kMostWaves / 2 * 64) f(A{}, R{}, One{}, Wave{}, std::true_type{});
+      else f(A{}, R{}, One{}, Wave{}, std::false_type{});
     };
     if (d->res_type == d->type) run(x);
     else run(mist::Elem<MIST_F32>{});
@@ -375,10 +508,11 @@ Parts parts_of(const mist_block_desc* d, bool by_sequence) {
   p.batch = by_sequence ? d->batch : 1;
   p.seq = by_sequence ? d->seq : d->batch * d->seq;
   if (!p.batch || !p.seq) return p;
-  p.pieces = std::clamp<int64_t>(kParts / p.batch, 1, (p.seq + kPartRows - 1) / kPartRows);
+  const int64_t parts = kPartWaves / (threads(d->hidden) / 64), least = kPartRows * 64 / lanes(d->hidden);
+  p.pieces = std::clamp<int64_t>(parts / p.batch, 1, (p.seq + least - 1) / least);
   p.rows = (p.seq + p.pieces - 1) / p.pieces;
   p.pieces = (p.seq + p.rows - 1) / p.rows;
-  p.seqs = p.pieces > 1 ? 1 : std::max<int64_t>((p.batch + kParts - 1) / kParts, std::min<int64_t>((kPartRows + p.seq - 1) / p.seq, p.batch));
+  p.seqs = p.pieces > 1 ? 1 : std::max<int64_t>((p.batch + parts - 1) / parts, std::min<int64_t>((least + p.seq - 1) / p.seq, p.batch));
   p.n = (p.batch + p.seqs - 1) / p.seqs * p.pieces;
   return p;
 }
@@ -430,10 +564,10 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   if (const mist_status st = check_tensors(d, {{x, d->x_stride, d->res_type, false, {}}, {block, d->block_stride, d->type, false, {}},
                                                {y, d->y_stride, d->res_type, true, {x, block}}, {h, d->h_stride, d->type, true, {}}}))
     return st;
-  with_kernel(d, [&](auto e, auto f, auto u) {
+  with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
     using A = decltype(e);
     using R = decltype(f);
-    hipLaunchKernelGGL((k_forward<A, R, u.value>), dim3((unsigned)std::min<int64_t>(a.n, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
+    hipLaunchKernelGGL((k_forward<A, R, u.value, l.value, wide.value>), dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
                        (const R*)x, (const A*)block, (R*)y, (A*)h, stats);
   });
   return launched("block norm");
@@ -493,10 +627,10 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
   }
   const hipStream_t st = (hipStream_t)stream;
   if (any) {
-    with_kernel(d, [&](auto e, auto f, auto u) {
+    with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
       using A = decltype(e);
       using R = decltype(f);
-      const auto kernel = post_weight || gate ? k_backward<A, R, u.value, true> : k_backward<A, R, u.value, false>;
+      const auto kernel = post_weight || gate ? k_backward<A, R, u.value, l.value, wide.value, true> : k_backward<A, R, u.value, l.value, wide.value, false>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)p.parts.n), dim3(threads(d->hidden)), 0, st, k, (const R*)y, (const A*)block, stats, (const A*)g->dh,
                          (const R*)g->dy, (R*)g->dx, (A*)g->dblock);
     });

@@ -53,6 +53,22 @@ __device__ __forceinline__ Float8 load8(const T* p, int64_t left, float fill = 0
     if (k < left) x[k] = (float)p[k];
   return x;
 }
+// The same as they are stored, zeros for those that are not there: 4 registers of 16-bit values.
+template <class T>
+using Raw8 = T __attribute__((ext_vector_type(8)));
+template <class T>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* p, int64_t left) {
+  if (left >= 8) return *(const typename Vec<T, 8>::type*)p;
+  Raw8<T> x = (T)0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < left) x[k] = p[k];
+  return x;
+}
+template <class T>
+__device__ __forceinline__ Float8 wide8(Raw8<T> x) {
+  return __builtin_convertvector(x, Float8);
+}
 template <class T>
 __device__ __forceinline__ void store8(T* p, int64_t left, Float8 x) {
   if (left >= 8) {
@@ -71,18 +87,29 @@ __device__ __forceinline__ float lanes(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
 }
 template <class J>
+__device__ __forceinline__ float join_pairs_of_16(float x, J join) {
+  const auto q = __builtin_amdgcn_permlane16_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
+  return join(__int_as_float((int)q[0]), __int_as_float((int)q[1]));
+}
+template <class J>
+__device__ __forceinline__ float join_pairs_of_32(float x, J join) {
+  const auto h = __builtin_amdgcn_permlane32_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
+  return join(__int_as_float((int)h[0]), __int_as_float((int)h[1]));
+}
+// Over groups of LANES (16, 32 or 64) neighbouring lanes.
+template <int LANES = 64, class J>
 __device__ __forceinline__ float wave_join(float x, J join) {
   x = join(x, lanes<0xB1>(x));   // pairs
   x = join(x, lanes<0x4E>(x));   // fours
   x = join(x, lanes<0x141>(x));  // eights: mirrored
   x = join(x, lanes<0x140>(x));  // sixteens: mirrored
-  const auto q = __builtin_amdgcn_permlane16_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
-  x = join(__int_as_float((int)q[0]), __int_as_float((int)q[1]));
-  const auto h = __builtin_amdgcn_permlane32_swap((unsigned)__float_as_int(x), (unsigned)__float_as_int(x), false, false);
-  return join(__int_as_float((int)h[0]), __int_as_float((int)h[1]));
+  if (LANES >= 32) x = join_pairs_of_16(x, join);
+  if (LANES >= 64) x = join_pairs_of_32(x, join);
+  return x;
 }
+template <int LANES = 64>
 __device__ __forceinline__ float wave_sum(float x) {
-  return wave_join(x, [](float a, float b) { return a + b; });
+  return wave_join<LANES>(x, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float wave_max(float x) {
   return wave_join(x, [](float a, float b) { return fmaxf(a, b); });
