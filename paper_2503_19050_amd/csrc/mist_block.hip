@@ -23,7 +23,9 @@ namespace {
 constexpr int kMostWaves = 16;
 constexpr int64_t kMostTokens = (int64_t)1 << 30;
 constexpr int64_t kMostBlocks = 4096;  // of the forward pass; they take rows in turn
-constexpr int64_t kPartWaves = 5120;   // of the backward pass, about
+#ifndef PM
+#define PM 1
+#endif
 constexpr int64_t kPartRows = 8;       // a part has at least, where there are as many
 constexpr int kSlots = 5;              // gradients summed over tokens
 constexpr int kJoinThreads = 1024;
@@ -71,8 +73,19 @@ __device__ __forceinline__ Float8 over_rows(Float8 x) {
 // Waves meet in two places in turn: one writes a place only after every wave has read its last values.
 template <int L>
 struct Join {
-  float2* part;  // [2][kMostWaves]
+  float2* part;   // [2][kMostWaves]
+  float2* count;  // [kMostWaves]: columns of each wave, and one over them
   int waves, turn;
+  template <int U>
+  __device__ __forceinline__ void count_columns(const BlockArgs& a) {
+    if (!a.layer || L < 64 || waves == 1) return;
+    if ((int)threadIdx.x < waves) {
+      int n = 0;
+      for (int u = 0; u < U; ++u) n += min(max((int)a.hidden - (u * (int)blockDim.x + (int)threadIdx.x * 64) * 8, 0), 512);
+      count[threadIdx.x] = float2{(float)n, 1.0f / (float)n};
+    }
+    __syncthreads();
+  }
   __device__ __forceinline__ const float2* meet(float a, float b) {
     float2* p = part + turn * kMostWaves;
     turn ^= 1;
@@ -84,10 +97,13 @@ struct Join {
     a = wave_sum<L>(a);
     b = wave_sum<L>(b);
     if (L < 64 || waves == 1) return float2{a, b};
-    const float2* p = meet(a, b);
-    float2 s = p[0];
-    for (int k = 1; k < waves; ++k) s.x += p[k].x, s.y += p[k].y;
-    return s;
+    const float2 s = of_waves(meet(a, b));
+    return float2{wave_sum<16>(s.x), wave_sum<16>(s.y)};
+  }
+  // a wave's value for each of 16 lanes, in every 16 lanes; zeros past the last wave
+  __device__ __forceinline__ float2 of_waves(const float2* p) const {
+    const int k = (int)threadIdx.x % 16;
+    return k < waves ? p[k] : float2{0.0f, 0.0f};
   }
 };
 
@@ -110,6 +126,22 @@ __device__ __forceinline__ void each(F&& f) {
   for (int u = 0; u < U; ++u) f(u);
 }
 
+// A thread's values of a weight, `none` without one: in registers, or read where they are used by rows of more than 8192 columns.
+template <int U, int L>
+struct Weights {
+  const void* p;
+  const Columns<U, L>& c;
+  int32_t type;
+  float none;
+  Float8 held;
+  __device__ __forceinline__ Weights(const BlockArgs& a, const void* weight, const Columns<U, L>& columns, float without)
+      : p(weight), c(columns), type(a.weight_type), none(without) {
+    if (U == 1) held = read(0);
+  }
+  __device__ __forceinline__ Float8 read(int u) const { return p ? load_weight(p, type, c.col[u], c.left[u]) : Float8(none); }
+  __device__ __forceinline__ Float8 operator()(int u) const { return U == 1 ? held : read(u); }
+};
+
 struct Moments {
   float mean, r;
 };
@@ -124,13 +156,8 @@ __device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, co
   }
   each<U>([&](int u) { s += sum8(x[u]); });
   s = wave_sum<L>(s);
-  auto count = [&](int wave) {  // columns of a wave
-    int n = 0;
-    each<U>([&](int u) { n += min(max((int)a.hidden - (u * (int)blockDim.x + wave * 64) * 8, 0), 512); });
-    return (float)n;
-  };
   const bool alone = L < 64 || join.waves == 1;
-  const float near = alone ? s * a.inv_hidden : s / count((int)threadIdx.x / 64);
+  const float near = s * (alone ? a.inv_hidden : join.count[threadIdx.x / 64].y);
   each<U>([&](int u) {
     const Float8 d = masked(x[u] - near, c.left[u]);
     q += sum8(d * d);
@@ -138,14 +165,10 @@ __device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, co
   q = wave_sum<L>(q);
   float mean = near;
   if (!alone) {
-    const float2* p = join.meet(s, q);
-    mean = 0.0f, q = 0.0f;
-    for (int k = 0; k < join.waves; ++k) mean += p[k].x;
-    mean *= a.inv_hidden;
-    for (int k = 0; k < join.waves; ++k) {
-      const float n = count(k), d = p[k].x / n - mean;
-      q += fmaf(n * d, d, p[k].y);
-    }
+    const float2 p = join.of_waves(join.meet(s, q)), n = join.of_waves(join.count);
+    mean = wave_sum<16>(p.x) * a.inv_hidden;
+    const float d = p.x * n.y - mean;
+    q = wave_sum<16>(fmaf(n.x * d, d, p.y));
   }
   return Moments{mean, 1.0f / sqrtf(q * a.inv_hidden + a.eps)};
 }
@@ -162,21 +185,16 @@ struct Input {
 constexpr int most_waves(int u, int l, bool wide) { return l < 64 ? 1 : u == 1 && !wide ? kMostWaves / 2 : kMostWaves; }
 
 // The next row is read before the sums of this one are waited for, where the registers are there.
-template <class A, class R, int U, int L, bool WIDE>
+// MORE: a norm before, or a gate.
+template <class A, class R, int U, int L, bool WIDE, bool MORE>
 __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
   constexpr int kRows = 64 / L;  // of a block at a time
-  __shared__ float2 part[2 * kMostWaves];
-  Join<L> join{part, (int)blockDim.x / 64, 0};
+  __shared__ float2 part[3 * kMostWaves];
+  Join<L> join{part, part + 2 * kMostWaves, (int)blockDim.x / 64, 0};
+  join.template count_columns<U>(a);
   const Columns<U, L> c(a);
-  Float8 w[U] = {}, wb[U] = {}, pw[U] = {}, pb[U] = {}, gate[U];
-  each<U>([&](int u) {
-    if (a.weight) w[u] = load_weight(a.weight, a.weight_type, c.col[u], c.left[u]);
-    if (a.bias) wb[u] = load_weight(a.bias, a.weight_type, c.col[u], c.left[u]);
-    if (a.post_weight) pw[u] = load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]);
-    if (a.post_bias) pb[u] = load_weight(a.post_bias, a.weight_type, c.col[u], c.left[u]);
-    gate[u] = a.block_scale;
-    if (a.gate && !a.gate_stride) gate[u] *= load_weight(a.gate, a.weight_type, c.col[u], c.left[u]);
-  });
+  const Weights<U, L> w(a, a.weight, c, 1.0f), wb(a, a.bias, c, 0.0f), pw(a, MORE ? a.post_weight : nullptr, c, 1.0f), pb(a, MORE ? a.post_bias : nullptr, c, 0.0f);
+  const Weights<U, L> shared_gate(a, !MORE || a.gate_stride ? nullptr : a.gate, c, 1.0f);
   const int sub = L < 64 ? (int)threadIdx.x / L : 0;
   auto read = [&](int64_t t0) {
     const int64_t t = min(t0 + sub, a.n - 1);
@@ -207,14 +225,15 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_forward(BlockAr
       Float8 b[U];
       each<U>([&](int u) {
         b[u] = mist::wide8<A>(now.b[u]);
-        if (a.gate_stride) gate[u] = a.block_scale * load_weight(a.gate, a.weight_type, min(t, a.n - 1) / a.seq * a.gate_stride + c.col[u], c.left[u]);
       });
-      if (a.post_weight) {
+      const int64_t gate_row = MORE && a.gate_stride ? min(t, a.n - 1) / a.seq * a.gate_stride : 0;
+      if (MORE && a.post_weight) {
         before = moments<U, L>(a, join, c, b);
-        each<U>([&](int u) { b[u] = (b[u] - before.mean) * before.r * pw[u] + pb[u]; });
+        each<U>([&](int u) { b[u] = (b[u] - before.mean) * before.r * pw(u) + pb(u); });
       }
       each<U>([&](int u) {
-        v[u] = a.res_scale * v[u] + b[u] * gate[u];
+        if (MORE) b[u] *= a.gate_stride ? load_weight(a.gate, a.weight_type, gate_row + c.col[u], c.left[u]) : shared_gate(u);
+        v[u] = a.res_scale * v[u] + a.block_scale * b[u];
         if (there) store8(y + t * a.y_stride + c.col[u], c.left[u], v[u]);
         // the norm is of y as it is stored: formed again from it, h has the same bits
         v[u] = masked(mist::wide8<R>(__builtin_convertvector(v[u], mist::Raw8<R>)), c.left[u]);
@@ -222,7 +241,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_forward(BlockAr
     }
     if (h) {
       after = moments<U, L>(a, join, c, v);
-      if (there) each<U>([&](int u) { store8(h + t * a.h_stride + c.col[u], c.left[u], (v[u] - after.mean) * after.r * w[u] + wb[u]); });
+      if (there) each<U>([&](int u) { store8(h + t * a.h_stride + c.col[u], c.left[u], (v[u] - after.mean) * after.r * w(u) + wb(u)); });
     }
     if (there && c.col[0] == 0) *(float4*)(stats + t * 4) = float4{before.mean, before.r, after.mean, after.r};
   }
@@ -259,13 +278,11 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
   constexpr int kRows = 64 / L;
   __shared__ float2 shared[2 * kMostWaves];
   const BlockArgs& a = k.a;
-  Join<L> join{shared, (int)blockDim.x / 64, 0};
+  Join<L> join{shared, nullptr, (int)blockDim.x / 64, 0};
   const Columns<U, L> c(a);
-  Float8 w[U] = {}, gp[U];  // gp: gate post_weight
+  const Weights<U, L> w(a, a.weight, c, 1.0f);
+  Float8 gp[U];  // gate post_weight
   Float8 sw[U] = {}, sb[U] = {}, sen[U], se[U];
-  each<U>([&](int u) {
-    if (a.weight) w[u] = load_weight(a.weight, a.weight_type, c.col[u], c.left[u]);
-  });
   auto post_weight = [&](int u) { return a.post_weight ? load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]) : Float8(1.0f); };
   auto gate = [&](int u, int64_t s) { return a.gate ? load_weight(a.gate, a.weight_type, s * a.gate_stride + c.col[u], c.left[u]) : Float8(1.0f); };
   const int sub = L < 64 ? (int)threadIdx.x / L : 0;
@@ -314,7 +331,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
             sb[u] += g[u];
             sw[u] += g[u] * n[u];
           }
-          g[u] *= w[u];
+          g[u] *= w(u);
           p += sum8(g[u]);
           q += sum8(masked(g[u] * n[u], c.left[u]));
         });
@@ -503,12 +520,12 @@ mist_status launched(const char* what) {
   return e == hipSuccess ? MIST_OK : hip_failed(e, what);
 }
 
-Parts parts_of(const mist_block_desc* d, bool by_sequence) {
+Parts parts_of(const mist_block_desc* d, bool by_sequence, bool more) {
   Parts p{};
   p.batch = by_sequence ? d->batch : 1;
   p.seq = by_sequence ? d->seq : d->batch * d->seq;
   if (!p.batch || !p.seq) return p;
-  const int64_t parts = kPartWaves / (threads(d->hidden) / 64), least = kPartRows * 64 / lanes(d->hidden);
+  const int64_t waves = threads(d->hidden) / 64, parts = PM * 256 * std::max<int64_t>(1, (more && waves <= 8 ? 12 : 16) / waves), least = kPartRows * 64 / lanes(d->hidden);
   p.pieces = std::clamp<int64_t>(parts / p.batch, 1, (p.seq + least - 1) / least);
   p.rows = (p.seq + p.pieces - 1) / p.pieces;
   p.pieces = (p.seq + p.rows - 1) / p.rows;
@@ -525,7 +542,7 @@ struct Plan {
 Plan plan_of(const mist_block_desc* d, const mist_block_grads* g) {
   Plan p{};
   const bool by_sequence = d->gate_stride && d->batch > 1;
-  p.parts = parts_of(d, by_sequence);
+  p.parts = parts_of(d, by_sequence, g->dpost_weight || g->dpost_bias || g->dgate);
   const void* out[kSlots] = {g->dweight, g->dbias, g->dpost_weight, g->dpost_bias, g->dgate};
   p.direct = by_sequence && p.parts.pieces == 1;
   for (int i = 0; i < kSlots; ++i) {
@@ -567,7 +584,8 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
     using A = decltype(e);
     using R = decltype(f);
-    hipLaunchKernelGGL((k_forward<A, R, u.value, l.value, wide.value>), dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
+    const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, wide.value, true> : k_forward<A, R, u.value, l.value, wide.value, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
                        (const R*)x, (const A*)block, (R*)y, (A*)h, stats);
   });
   return launched("block norm");
