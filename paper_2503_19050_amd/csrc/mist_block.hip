@@ -23,10 +23,7 @@ namespace {
 constexpr int kMostWaves = 16;
 constexpr int64_t kMostTokens = (int64_t)1 << 30;
 constexpr int64_t kMostBlocks = 4096;  // of the forward pass; they take rows in turn
-#ifndef PM
-#define PM 1
-#endif
-constexpr int64_t kPartRows = 8;       // a part has at least, where there are as many
+constexpr int64_t kPartRows = 4;       // a part has at least, where there are as many
 constexpr int kSlots = 5;              // gradients summed over tokens
 constexpr int kJoinThreads = 1024;
 
@@ -262,6 +259,10 @@ struct BackArgs {
   int32_t accumulate;
 };
 
+// Waves a SIMD of the backward pass without a norm before or a gate.  Five, with a few registers spilled, are worth it to blocks of several
+// waves and 16-bit rows (65536 x 2560: 377 us, 438 with four), not to single waves (65536 x 512: 75 and 66) or fp32 (1000 x 1024: 11.8 and 9.3).
+constexpr int back_waves(int u, int l, bool wide, size_t res_bytes) { return u == 1 && l == 64 && !wide && res_bytes == 2 ? 5 : 4; }
+
 template <class A, class R, int U>
 struct BackInput {
   mist::Raw8<R> y[U], dy[U];
@@ -272,7 +273,7 @@ struct BackInput {
 // With e the gradient of gate v (v = n post_weight + post_bias) over a sequence's tokens, the sums of e and of e n are all
 // that the gradients of gate, post_weight and post_bias need: two sums a column for three.
 template <class A, class R, int U, int L, bool WIDE, bool MORE>
-__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
+__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64, MORE && !WIDE ? 2 : back_waves(U, L, WIDE, sizeof(R))) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
                                                                           A* dblock) {
   constexpr bool kAhead = U == 1 && !(MORE && WIDE);
   constexpr int kRows = 64 / L;
@@ -310,23 +311,22 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
     for (int64_t r0 = row0; r0 < row1; r0 += kRows) {
       const int64_t t = s * k.parts.seq + r0 + sub;
       const bool there = L == 64 || r0 + sub < row1;
-      BackInput<A, R, U> now;
-      if constexpr (kAhead) {
-        now = in;
+      if (!kAhead) in = read(s, r0);
+      const float4 st = in.st;
+      Float8 d[U], g[U], n[U], b[U];
+      each<U>([&](int u) {
+        d[u] = dy ? mist::wide8<R>(in.dy[u]) : Float8(0.0f);
+        if (dh) g[u] = mist::wide8<A>(in.dh[u]);
+        if (dh) n[u] = (mist::wide8<R>(in.y[u]) - st.z) * st.w;
+        if (MORE && block) b[u] = masked((mist::wide8<A>(in.b[u]) - st.x) * st.y, c.left[u]);
+      });
+      if (kAhead) {  // in the registers that have just been read
         if (r0 + kRows < row1) in = read(s, r0 + kRows);
         else if (s + 1 < last) in = read(s + 1, row0);
-      } else {
-        now = read(s, r0);
       }
-      const float4 st = now.st;
-      Float8 d[U];
-      each<U>([&](int u) { d[u] = dy ? mist::wide8<R>(now.dy[u]) : Float8(0.0f); });
       if (dh) {
-        Float8 g[U], n[U];
         float p = 0.0f, q = 0.0f;
         each<U>([&](int u) {
-          g[u] = mist::wide8<A>(now.dh[u]);
-          n[u] = (mist::wide8<R>(now.y[u]) - st.z) * st.w;
           if (there) {
             sb[u] += g[u];
             sw[u] += g[u] * n[u];
@@ -343,12 +343,10 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
       if (block) {
         each<U>([&](int u) { d[u] *= a.block_scale; });
         if (MORE) {
-          Float8 n[U];
           each<U>([&](int u) {
-            n[u] = masked((mist::wide8<A>(now.b[u]) - st.x) * st.y, c.left[u]);
             if (there) {
               se[u] += d[u];
-              sen[u] += d[u] * n[u];
+              sen[u] += d[u] * b[u];
             }
             d[u] = masked(d[u] * gp[u], c.left[u]);
           });
@@ -356,11 +354,11 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
             float p = 0.0f, q = 0.0f;
             each<U>([&](int u) {
               p += sum8(d[u]);
-              q += sum8(d[u] * n[u]);
+              q += sum8(d[u] * b[u]);
             });
             const float2 m = join.sum(p, q);
             const float mean = a.layer ? m.x * a.inv_hidden : 0.0f, along = m.y * a.inv_hidden;
-            each<U>([&](int u) { d[u] = st.y * (d[u] - mean - n[u] * along); });
+            each<U>([&](int u) { d[u] = st.y * (d[u] - mean - b[u] * along); });
           }
         }
         if (dblock && there) each<U>([&](int u) { store8(dblock + t * k.dblock_stride + c.col[u], c.left[u], d[u]); });
@@ -400,7 +398,8 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_backward(BackAr
   });
 }
 
-// The parts' sums, in order: parts[i * count .. ) of `count` rows give row i of out.  One wave's 64 columns a block, 16 shares of the rows.
+// The parts' sums, in an order that goes by their number: parts [i * count, (i + 1) * count) give row i of out.  A block
+// takes 64 columns in 16 shares of the parts, or, of many parts, 16 columns in 64 shares.
 struct JoinJob {
   const float* part;
   void* out;
@@ -411,26 +410,30 @@ struct JoinArgs {
   int64_t hidden;
   int32_t type, accumulate;
 };
+__host__ __device__ __forceinline__ int join_columns(const JoinJob& j) { return j.count >= 256 ? 16 : 64; }
+
 __global__ __launch_bounds__(kJoinThreads) void k_join_parts(JoinArgs k) {
-  constexpr int kShares = kJoinThreads / 64;
-  __shared__ float share[kShares][64];
+  constexpr int kWaves = kJoinThreads / 64;
+  __shared__ float share[kWaves][64];
   const JoinJob j = k.job[blockIdx.y];
-  const int lane = threadIdx.x % 64, mine = threadIdx.x / 64;
-  const int64_t columns = (k.hidden + 63) / 64, per = (j.count + kShares - 1) / kShares;
+  const int width = join_columns(j), lane = (int)threadIdx.x % width, mine = (int)threadIdx.x / width, shares = kJoinThreads / width;
+  const int64_t columns = (k.hidden + width - 1) / width;
   for (int64_t i = blockIdx.x; i < columns * j.rows; i += gridDim.x) {
-    const int64_t row = i / columns, col = i % columns * 64 + lane;
+    const int64_t row = i / columns, col = i % columns * width + lane;
     float s = 0.0f;
     if (col < k.hidden) {
-      const float* p = j.part + (row * j.count) * k.hidden + col;
-      const int64_t end = min(j.count, (mine + 1) * per);
+      const float* p = j.part + row * j.count * k.hidden + col;
 #pragma unroll 8
-      for (int64_t r = mine * per; r < end; ++r) s += p[r * k.hidden];
+      for (int64_t r = mine; r < j.count; r += shares) s += p[r * k.hidden];
     }
+    auto sum = [](float a, float b) { return a + b; };
+    if (width == 16) s = mist::join_pairs_of_32(mist::join_pairs_of_16(s, sum), sum);  // the shares of a wave
     __syncthreads();
-    share[mine][lane] = s;
+    share[threadIdx.x / 64][threadIdx.x % 64] = s;
     __syncthreads();
     if (mine == 0 && col < k.hidden) {
-      for (int w = 1; w < kShares; ++w) s += share[w][lane];
+      s = 0.0f;
+      for (int w = 0; w < kWaves; ++w) s += share[w][lane];
       store_weight(j.out, k.type, row * j.stride + col, s, k.accumulate);
     }
   }
@@ -520,12 +523,17 @@ mist_status launched(const char* what) {
   return e == hipSuccess ? MIST_OK : hip_failed(e, what);
 }
 
+// Waves of the backward pass that a CU holds: one round of blocks of the same work (two to four rounds took 0-5 % more).
+int64_t resident_waves(const mist_block_desc* d, int64_t waves, bool more) {
+  return more && waves <= kMostWaves / 2 ? 12 : 4 * back_waves(units(d->hidden), lanes(d->hidden), waves == 1 || waves > kMostWaves / 2, (size_t)mist::type_bytes(d->res_type));
+}
+
 Parts parts_of(const mist_block_desc* d, bool by_sequence, bool more) {
   Parts p{};
   p.batch = by_sequence ? d->batch : 1;
   p.seq = by_sequence ? d->seq : d->batch * d->seq;
   if (!p.batch || !p.seq) return p;
-  const int64_t waves = threads(d->hidden) / 64, parts = PM * 256 * std::max<int64_t>(1, (more && waves <= 8 ? 12 : 16) / waves), least = kPartRows * 64 / lanes(d->hidden);
+  const int64_t waves = threads(d->hidden) / 64, parts = 256 * std::max<int64_t>(1, resident_waves(d, waves, more) / waves), least = kPartRows * 64 / lanes(d->hidden);
   p.pieces = std::clamp<int64_t>(parts / p.batch, 1, (p.seq + least - 1) / least);
   p.rows = (p.seq + p.pieces - 1) / p.pieces;
   p.pieces = (p.seq + p.rows - 1) / p.rows;
@@ -640,7 +648,7 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
     k.slot[i] = (float*)ws;
     const bool gates = i == 4 && a.gate_stride;
     j.job[jobs++] = JoinJob{k.slot[i], out[i], gates ? p.parts.pieces : p.parts.n, gates ? d->batch : 1, gates ? g->dgate_stride : 0};
-    most = std::max(most, (d->hidden + 63) / 64 * j.job[jobs - 1].rows);
+    most = std::max(most, (d->hidden + join_columns(j.job[jobs - 1]) - 1) / join_columns(j.job[jobs - 1]) * j.job[jobs - 1].rows);
     ws += ((size_t)p.parts.n * d->hidden * 4 + 255) / 256 * 256;
   }
   const hipStream_t st = (hipStream_t)stream;
@@ -648,7 +656,9 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
     with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
       using A = decltype(e);
       using R = decltype(f);
-      const auto kernel = post_weight || gate ? k_backward<A, R, u.value, l.value, wide.value, true> : k_backward<A, R, u.value, l.value, wide.value, false>;
+      const auto kernel = post_weight || gate          ? k_backward<A, R, u.value, l.value, wide.value, true>
+                          : threads(d->hidden) == 64 && l.value == 64 ? k_backward<A, R, u.value, l.value, true, false>
+                                                                      : k_backward<A, R, u.value, l.value, wide.value, false>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)p.parts.n), dim3(threads(d->hidden)), 0, st, k, (const R*)y, (const A*)block, stats, (const A*)g->dh,
                          (const R*)g->dy, (R*)g->dx, (A*)g->dblock);
     });

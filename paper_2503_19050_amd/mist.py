@@ -1005,42 +1005,72 @@ MlpAct = collections.namedtuple("MlpAct", "out up gate")
 
 
 def _no_graph(torch, what, *tensors) -> None:
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        _need(False, "%s: records no gradient; call it under torch.no_grad() and the gradient's call for the gradients" % what)
+    if not torch.is_grad_enabled():
+        return
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            _need(False, "%s: records no gradient; call it under torch.no_grad() and the gradient's call for the gradients" % what)
 
 
 def _here(what, first, *tensors) -> None:
-    _need(first.is_cuda and all(t is None or t.device == first.device for t in tensors), "%s: the tensors must be on one GPU" % what)
+    device = first.device
+    for t in tensors:
+        if t is not None and t.device != device:
+            device = None
+            break
+    if device is None or not first.is_cuda:
+        _need(False, "%s: the tensors must be on one GPU" % what)
+
+
+class _Idle:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return None
+
+
+_IDLE = _Idle()
+
+
+def _pool(torch, other):
+    """New tensors of the pool of the stream that they are used on (other; None: the current one)."""
+    return _IDLE if other is None else torch.cuda.stream(other)
 
 
 def _shaped(what, t, shape, dtype, name) -> None:
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), "%s: %s must be %s of %s" % (what, name, dtype, tuple(shape)))
+    if not (t.dtype == dtype and tuple(t.shape) == tuple(shape)):
+        _need(False, "%s: %s must be %s of %s" % (what, name, dtype, tuple(shape)))
 
 
 def _flat(what, t) -> tuple[int, int]:
     """(rows, their stride) of a tensor whose last dimension is contiguous and whose others are rows at one stride."""
     shape, strides = t.shape, t.stride()
-    _need(len(shape) >= 1, "%s: a tensor without dimensions" % what)
+    if not (len(shape) >= 1):
+        _need(False, "%s: a tensor without dimensions" % what)
     if t.is_contiguous():
         width = shape[-1]
         return (t.numel() // width if width else 0), width
     rows, stride = 1, shape[-1]
     if t.numel() == 0:
         return 0, stride
-    _need(shape[-1] == 1 or strides[-1] == 1, "%s: the last dimension must be contiguous" % what)
+    if not (shape[-1] == 1 or strides[-1] == 1):
+        _need(False, "%s: the last dimension must be contiguous" % what)
     for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if n == 1:
             continue
         if rows == 1:
             stride = s
-        _need(s == stride * rows, "%s: the leading dimensions must be rows at one stride" % what)
+        if not (s == stride * rows):
+            _need(False, "%s: the leading dimensions must be rows at one stride" % what)
         rows *= n
     return rows, stride
 
 
 def _packed(what, t, shape, dtype, name):
     _shaped(what, t, shape, dtype, name)
-    _need(t.is_contiguous(), "%s: %s must be contiguous" % (what, name))
+    if not (t.is_contiguous()):
+        _need(False, "%s: %s must be contiguous" % (what, name))
     return t
 
 
@@ -1049,23 +1079,29 @@ def _token_desc(torch, logits, targets, grad, vocab_begin, scale, top) -> TokenD
     _here(what, logits, targets, grad)
     lshape = logits.shape
     shape = lshape[:-1]
-    _need(len(lshape) in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    if not (len(lshape) in (2, 3)):
+        _need(False, "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
     two = len(lshape) == 3
     ist, id_bytes = 0, 8
     if targets is not None:
         id_bytes = targets.element_size()
-        _need(id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed,
-              "%s: targets must be int32 or int64" % what)
-        _need(targets.shape == shape, "%s: targets must have the logits' shape but for the last dimension" % what)
-        _need(shape[-1] <= 1 or targets.stride(-1) == 1, "%s: the targets of a sequence must be contiguous" % what)
+        if not (id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed):
+            _need(False, "%s: targets must be int32 or int64" % what)
+        if not (targets.shape == shape):
+            _need(False, "%s: targets must have the logits' shape but for the last dimension" % what)
+        if not (shape[-1] <= 1 or targets.stride(-1) == 1):
+            _need(False, "%s: the targets of a sequence must be contiguous" % what)
         ist = targets.stride(0) if two else 0
     lst = logits.stride()
-    _need(lshape[-1] <= 1 or lst[-1] == 1 or logits.numel() == 0, "%s: the last dimension must be contiguous" % what)
+    if not (lshape[-1] <= 1 or lst[-1] == 1 or logits.numel() == 0):
+        _need(False, "%s: the last dimension must be contiguous" % what)
     gst = lst
     if grad is not None:
-        _need(grad.shape == lshape and grad.dtype == logits.dtype, "%s: the gradient must have the logits' shape and type" % what)
+        if not (grad.shape == lshape and grad.dtype == logits.dtype):
+            _need(False, "%s: the gradient must have the logits' shape and type" % what)
         gst = grad.stride()
-        _need(lshape[-1] <= 1 or gst[-1] == 1 or logits.numel() == 0, "%s: the last dimension must be contiguous" % what)
+        if not (lshape[-1] <= 1 or gst[-1] == 1 or logits.numel() == 0):
+            _need(False, "%s: the last dimension must be contiguous" % what)
     return TokenDesc(lshape[0] if two else 1, lshape[-2], lshape[-1], int(vocab_begin), ist, lst[0] if two else 0, lst[-2], gst[0] if two else 0,
                      gst[-2], id_bytes, _type(logits, what), int(top), float(scale))
 
@@ -1073,7 +1109,8 @@ def _token_desc(torch, logits, targets, grad, vocab_begin, scale, top) -> TokenD
 def _top_space(torch, shape, top, device):
     if not top:
         return None, None
-    _need(0 < top <= TOKEN_MAX_TOP, "token log probabilities: top must be in 0..%d" % TOKEN_MAX_TOP)
+    if not (0 < top <= TOKEN_MAX_TOP):
+        _need(False, "token log probabilities: top must be in 0..%d" % TOKEN_MAX_TOP)
     return (torch.empty(shape + (top,), dtype=torch.int32, device=device), torch.empty(shape + (top,), dtype=torch.float32, device=device))
 
 
@@ -1087,7 +1124,7 @@ def token_logprob(logits, targets=None, *, scale: float = 1.0, entropy: bool = F
     d = _token_desc(torch, logits, targets, None, 0, scale, top)
     device, shape = logits.device, tuple(logits.shape[:-1])
     handle, other = _stream_of(torch, stream, device)
-    with torch.cuda.stream(other):
+    with _pool(torch, other):
         lse = torch.empty(shape, dtype=torch.float32, device=device)
         logp = None if targets is None else torch.empty_like(lse)
         ent = torch.empty_like(lse) if entropy else None
@@ -1109,7 +1146,7 @@ def token_part(logits, targets, *, vocab_begin: int, scale: float = 1.0, top: in
     d = _token_desc(torch, logits, targets, None, vocab_begin, scale, top)
     device, shape = logits.device, tuple(logits.shape[:-1])
     handle, other = _stream_of(torch, stream, device)
-    with torch.cuda.stream(other):
+    with _pool(torch, other):
         if stats is None:
             stats = torch.empty(shape + (4,), dtype=torch.float32, device=device)
         ids, z = _top_space(torch, shape, top, device)
@@ -1127,12 +1164,14 @@ def token_join(stats, targets=None, *, entropy: bool = False, top_ids=None, top_
     torch = _torch()
     L = _lib or load()
     what = "token log probabilities"
-    _need(stats.dim() in (3, 4) and stats.shape[-1] == 4, "%s: stats must be [ranks, seq, 4] or [ranks, batch, seq, 4]" % what)
+    if not (stats.dim() in (3, 4) and stats.shape[-1] == 4):
+        _need(False, "%s: stats must be [ranks, seq, 4] or [ranks, batch, seq, 4]" % what)
     _here(what, stats, targets, top_ids, top_z)
     ranks, shape, device = stats.shape[0], tuple(stats.shape[1:-1]), stats.device
     _packed(what, stats, stats.shape, torch.float32, "stats")
     top = 0
-    _need((top_ids is None) == (top_z is None), "%s: top_ids and top_z come together" % what)
+    if not ((top_ids is None) == (top_z is None)):
+        _need(False, "%s: top_ids and top_z come together" % what)
     if top_ids is not None:
         top = top_ids.shape[-1]
         _packed(what, top_ids, (ranks,) + shape + (top,), torch.int32, "top_ids")
@@ -1140,14 +1179,16 @@ def token_join(stats, targets=None, *, entropy: bool = False, top_ids=None, top_
     ist, id_bytes = 0, 8
     if targets is not None:
         id_bytes = targets.element_size()
-        _need(id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed,
-              "%s: targets must be int32 or int64" % what)
-        _need(tuple(targets.shape) == shape, "%s: targets must have the tokens' shape" % what)
-        _need(shape[-1] <= 1 or targets.stride(-1) == 1, "%s: the targets of a sequence must be contiguous" % what)
+        if not (id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed):
+            _need(False, "%s: targets must be int32 or int64" % what)
+        if not (tuple(targets.shape) == shape):
+            _need(False, "%s: targets must have the tokens' shape" % what)
+        if not (shape[-1] <= 1 or targets.stride(-1) == 1):
+            _need(False, "%s: the targets of a sequence must be contiguous" % what)
         ist = targets.stride(0) if len(shape) == 2 else 0
     d = TokenDesc(shape[0] if len(shape) == 2 else 1, shape[-1], 1, 0, ist, 0, 0, 0, 0, id_bytes, 0, top, 1.0)
     handle, other = _stream_of(torch, stream, device)
-    with torch.cuda.stream(other):
+    with _pool(torch, other):
         lse = torch.empty(shape, dtype=torch.float32, device=device)
         logp = None if targets is None else torch.empty_like(lse)
         ent = torch.empty_like(lse) if entropy else None
@@ -1167,13 +1208,16 @@ def token_grad(logits, targets, lse, *, dlogp=None, entropy=None, dentropy=None,
     L = _lib or load()
     what = "token log probabilities' gradient"
     _here(what, logits, lse, dlogp, entropy, dentropy, targets, dlogits)
-    _need(logits.dim() in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    if not (logits.dim() in (2, 3)):
+        _need(False, "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
     handle, other = _stream_of(torch, stream, logits.device)
     if dlogits is None:
-        with torch.cuda.stream(other):
+        with _pool(torch, other):
             dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _need(dlogp is None or targets is not None, "%s: dlogp without targets" % what)
-    _need(dentropy is None or entropy is not None, "%s: dentropy without entropy" % what)
+    if not (dlogp is None or targets is not None):
+        _need(False, "%s: dlogp without targets" % what)
+    if not (dentropy is None or entropy is not None):
+        _need(False, "%s: dentropy without entropy" % what)
     d = _token_desc(torch, logits, targets, dlogits, vocab_begin, scale, 0)
     for t, name in ((lse, "lse"), (dlogp, "dlogp"), (entropy, "entropy"), (dentropy, "dentropy")):
         if t is not None:
@@ -1193,14 +1237,15 @@ def token_loss(logits, targets, weights=1.0, *, scale: float = 1.0, dlogits=None
     what = "token loss"
     _no_graph(torch, what, logits)
     _here(what, logits, targets, dlogits)
-    _need(logits.dim() in (2, 3), "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
+    if not (logits.dim() in (2, 3)):
+        _need(False, "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
     device, shape = logits.device, logits.shape[:-1]
     w, factor = (weights, 1.0) if isinstance(weights, torch.Tensor) else (None, float(weights))
     if w is not None:
         _here(what, logits, w)
         _packed(what, w, shape, torch.float32, "weights")
     handle, other = _stream_of(torch, stream, device)
-    with torch.cuda.stream(other):
+    with _pool(torch, other):
         if dlogits is None:
             dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=device)
         logp = torch.empty(shape, dtype=torch.float32, device=device)
@@ -1212,40 +1257,52 @@ def token_loss(logits, targets, weights=1.0, *, scale: float = 1.0, dlogits=None
     return logp, dlogits
 
 
-def _block_weights(what, hidden, dtype, weight, bias, post_weight, post_bias) -> None:
-    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"), (post_bias, "post_bias")):
-        if t is not None:
-            _packed(what, t, (hidden,), dtype, name)
+def _block_weights(what, hidden, dtype, *weights) -> None:
+    for t in weights:
+        if t is not None and not (t.dtype is dtype and t.dim() == 1 and t.shape[0] == hidden and t.is_contiguous()):
+            _need(False, "%s: weights and biases must be [%d] of one type, contiguous" % (what, hidden))
 
 
 def _block_gate(what, x, gate, dtype) -> int:
     """The stride between sequences' gates."""
-    if gate is None:
-        return 0
     hidden = x.shape[-1]
-    _need(gate.dtype == dtype and (tuple(gate.shape) == (hidden,) or (x.dim() == 3 and tuple(gate.shape) == (x.shape[0], hidden))),
-          "%s: the gate must be [hidden], or [batch, hidden] for [batch, seq, hidden], of the weights' type" % what)
-    _need(hidden <= 1 or gate.stride(-1) == 1, "%s: the last dimension must be contiguous" % what)
+    if not (gate.dtype == dtype and (tuple(gate.shape) == (hidden,) or (x.dim() == 3 and tuple(gate.shape) == (x.shape[0], hidden)))):
+        _need(False, "%s: the gate must be [hidden], or [batch, hidden] for [batch, seq, hidden], of the weights' type" % what)
+    if not (hidden <= 1 or gate.stride(-1) == 1):
+        _need(False, "%s: the last dimension must be contiguous" % what)
     return gate.stride(0) if gate.dim() == 2 else 0
 
 
-def _block_desc(what, x, block, y, h, weights, gate, kind, eps, res_scale, block_scale):
-    _need(x.dim() in (2, 3), "%s: must be [tokens, hidden] or [batch, seq, hidden]" % what)
-    _need(kind in _BLOCK_KINDS, "%s: kind must be 'rms' or 'layer'" % what)
-    like = block if block is not None else h
-    some = [t for t in (*weights, gate) if t is not None]
-    wtype = some[0].dtype if some else x.dtype
-    _block_weights(what, x.shape[-1], wtype, *weights)
-    strides = []
-    for t in (x, block, y, h):
-        if t is not None:
-            _need(t.shape == x.shape, "%s: the tensors must have one shape" % what)
-        strides.append(0 if t is None else _flat(what, t)[1])
-    _need(y is None or y.dtype == x.dtype, "%s: y must have x's type" % what)
-    _need(block is None or h is None or h.dtype == block.dtype, "%s: h must have the block's type" % what)
-    batch, seq = (x.shape[0], x.shape[1]) if x.dim() == 3 else (1, x.shape[0])
-    return BlockDesc(batch, seq, x.shape[-1], *strides, _block_gate(what, x, gate, wtype), _BLOCK_KINDS[kind],
-                     _type(x if like is None else like, what), _type(x, what), _TYPES.get(wtype, -1), float(eps), float(res_scale), float(block_scale))
+def _block_stride(what, x, t) -> int:
+    """The stride between rows of a tensor of x's shape."""
+    if t is None:
+        return 0
+    if t.shape != x.shape:
+        _need(False, "%s: the tensors must have one shape" % what)
+    return x.shape[-1] if t.is_contiguous() else _flat(what, t)[1]
+
+
+def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale):
+    shape = x.shape
+    dims = len(shape)
+    if dims != 3 and dims != 2:
+        _need(False, "%s: must be [tokens, hidden] or [batch, seq, hidden]" % what)
+    code = _BLOCK_KINDS.get(kind)
+    if code is None:
+        _need(False, "%s: kind must be 'rms' or 'layer'" % what)
+    like = block if block is not None else h if h is not None else x
+    first = weight if weight is not None else post_weight if post_weight is not None else bias if bias is not None else post_bias
+    first = first if first is not None else gate
+    wtype = x.dtype if first is None else first.dtype
+    if weight is not None or post_weight is not None or bias is not None or post_bias is not None:
+        _block_weights(what, shape[-1], wtype, weight, bias, post_weight, post_bias)
+    if y is not None and y.dtype != x.dtype:
+        _need(False, "%s: y must have x's type" % what)
+    if h is not None and h.dtype != like.dtype:
+        _need(False, "%s: h must have the block's type" % what)
+    return BlockDesc(shape[0] if dims == 3 else 1, shape[-2], shape[-1], _block_stride(what, x, x), _block_stride(what, x, block),
+                     _block_stride(what, x, y), _block_stride(what, x, h), 0 if gate is None else _block_gate(what, x, gate, wtype), code,
+                     _type(like, what), _type(x, what), _TYPES.get(wtype, -1), eps, res_scale, block_scale)
 
 
 def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, kind: str = "rms", eps: float = 1e-6,
@@ -1260,16 +1317,19 @@ def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_
     _no_graph(torch, what, x, block, weight, bias, post_weight, post_bias, gate)
     _here(what, x, block, weight, bias, post_weight, post_bias, gate, y, h)
     handle, other = _stream_of(torch, stream, x.device)
-    _need(block is None or dtype is None or dtype == block.dtype, "block norm: dtype is the block's")
-    _need(block is not None or y is None, "block norm: without a block y is x")
-    _need(weight is not None or h is None, "block norm: h without its weight")
-    with torch.cuda.stream(other):
+    if not (block is None or dtype is None or dtype == block.dtype):
+        _need(False, "block norm: dtype is the block's")
+    if not (block is not None or y is None):
+        _need(False, "block norm: without a block y is x")
+    if not (weight is not None or h is None):
+        _need(False, "block norm: h without its weight")
+    with _pool(torch, other):
         if block is not None and y is None:
             y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if weight is not None and h is None:
             h = torch.empty(x.shape, dtype=block.dtype if block is not None else dtype or x.dtype, device=x.device)
         stats = torch.empty(tuple(x.shape[:-1]) + (4,), dtype=torch.float32, device=x.device)
-    d = _block_desc(what, x, block, y, h, (weight, bias, post_weight, post_bias), gate, kind, eps, res_scale, block_scale)
+    d = _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale)
     _on_device(torch, x.device, L.mist_block_forward, ctypes.byref(d), x.data_ptr(), _ptr(block), _ptr(weight), _ptr(bias), _ptr(post_weight),
                _ptr(post_bias), _ptr(gate), _ptr(y), _ptr(h), stats.data_ptr(), handle)
     if other is not None:
@@ -1289,32 +1349,37 @@ def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post
     grads = (dweight, dbias, dpost_weight, dpost_bias)
     _here(what, y, stats, dh, block, dy, weight, post_weight, post_bias, gate, *grads, dgate, dx, dblock)
     handle, other = _stream_of(torch, stream, y.device)
-    _need(dh is not None or dy is not None, "%s: neither dh nor dy" % what)
-    _need((dh is None) == (weight is None), "%s: dh comes with weight" % what)
-    _need(block is not None or dblock is None, "%s: of a block that is not there" % what)
-    with torch.cuda.stream(other):
+    if not (dh is not None or dy is not None):
+        _need(False, "%s: neither dh nor dy" % what)
+    if not ((dh is None) == (weight is None)):
+        _need(False, "%s: dh comes with weight" % what)
+    if not (block is not None or dblock is None):
+        _need(False, "%s: of a block that is not there" % what)
+    with _pool(torch, other):
         if dx is None:
             dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
         if block is not None and dblock is None:
             dblock = torch.empty(block.shape, dtype=block.dtype, device=y.device)
-    d = _block_desc(what, y, block, y, dh, (weight, None, post_weight, post_bias), gate, kind, 0.0, res_scale, block_scale)
+    d = _block_desc(what, y, block, y, dh, weight, None, post_weight, post_bias, gate, kind, 0.0, res_scale, block_scale)
     wtype = next((t.dtype for t in (weight, post_weight, post_bias, gate) if t is not None), y.dtype)
     _block_weights(what, y.shape[-1], wtype, *grads)
     dgate_stride = 0
     if dgate is not None:
-        _need(gate is not None and dgate.shape == gate.shape, "%s: dgate must have the gate's shape" % what)
+        if not (gate is not None and dgate.shape == gate.shape):
+            _need(False, "%s: dgate must have the gate's shape" % what)
         dgate_stride = _block_gate(what, y, dgate, wtype)
     _packed(what, stats, tuple(y.shape[:-1]) + (4,), torch.float32, "stats")
     strides = []
     for t, dtype in ((dh, None if block is None else block.dtype), (dy, y.dtype), (dx, y.dtype), (dblock, None if block is None else block.dtype)):
-        _need(t is None or (t.shape == y.shape and (dtype is None or t.dtype == dtype)), "%s: a gradient must have its tensor's shape and type" % what)
+        if not (t is None or (t.shape == y.shape and (dtype is None or t.dtype == dtype))):
+            _need(False, "%s: a gradient must have its tensor's shape and type" % what)
         strides.append(0 if t is None else _flat(what, t)[1])
     g = BlockGrads(_ptr(dh), _ptr(dy), _ptr(dx), _ptr(dblock), *(_ptr(t) for t in grads), _ptr(dgate), *strides, dgate_stride, 1 if accumulate else 0)
     need = ctypes.c_size_t()
     _check(L, L.mist_block_workspace(ctypes.byref(d), ctypes.byref(g), ctypes.byref(need)))
     ws = None
     if need.value:
-        with torch.cuda.stream(other):  # of that stream's pool
+        with _pool(torch, other):  # of that stream's pool
             ws = torch.empty(need.value, dtype=torch.uint8, device=y.device)
     _on_device(torch, y.device, L.mist_block_backward, ctypes.byref(d), y.data_ptr(), _ptr(block), stats.data_ptr(), _ptr(weight), _ptr(post_weight),
                _ptr(post_bias), _ptr(gate), ctypes.byref(g), _ptr(ws), need.value, handle)
@@ -1330,20 +1395,24 @@ class Checkpoint:
     def __init__(self, shape, dtype, device="cuda", stream=None):
         torch = _torch()
         device = torch.device(device)
-        _need(device.type == "cuda", "checkpoint: must be on a GPU")
-        _need(dtype in _TYPES, "checkpoint: %s is not float32, bfloat16 or float16" % dtype)
+        if not (device.type == "cuda"):
+            _need(False, "checkpoint: must be on a GPU")
+        if not (dtype in _TYPES):
+            _need(False, "checkpoint: %s is not float32, bfloat16 or float16" % dtype)
         self.shape, self.dtype = tuple(int(n) for n in shape), dtype
-        _need(len(self.shape) >= 1 and self.shape[-1] >= 1 and min(self.shape) >= 0, "checkpoint: the last dimension must be at least 1")
+        if not (len(self.shape) >= 1 and self.shape[-1] >= 1 and min(self.shape) >= 0):
+            _need(False, "checkpoint: the last dimension must be at least 1")
         self.rows, self.width = math.prod(self.shape[:-1]), self.shape[-1]
         groups = -(-self.width // KEPT_GROUP)
-        with torch.cuda.stream(stream):
+        with _pool(torch, stream):
             self.values = torch.empty(self.rows, groups * KEPT_GROUP, dtype=torch.int8, device=device)
             self.exponents = torch.empty(self.rows, groups, dtype=torch.uint8, device=device)
 
     def kept(self, what, device) -> Kept:
         torch = _torch()
         groups = -(-self.width // KEPT_GROUP)
-        _need(self.values.device == device and self.exponents.device == device, "%s: the tensors must be on one GPU" % what)
+        if not (self.values.device == device and self.exponents.device == device):
+            _need(False, "%s: the tensors must be on one GPU" % what)
         _packed(what, self.values, (self.rows, groups * KEPT_GROUP), torch.int8, "a checkpoint's values")
         _packed(what, self.exponents, (self.rows, groups), torch.uint8, "a checkpoint's exponents")
         return Kept(self.values.data_ptr(), self.exponents.data_ptr())
@@ -1352,7 +1421,8 @@ class Checkpoint:
 def _checkpoint_for(what, t, given, other) -> Checkpoint:
     if given is None:
         return Checkpoint(t.shape, t.dtype, t.device, other)
-    _need(isinstance(given, Checkpoint) and given.shape == tuple(t.shape) and given.dtype == t.dtype, "%s: a checkpoint of another shape or type" % what)
+    if not (isinstance(given, Checkpoint) and given.shape == tuple(t.shape) and given.dtype == t.dtype):
+        _need(False, "%s: a checkpoint of another shape or type" % what)
     return given
 
 
@@ -1381,13 +1451,16 @@ def checkpoint_load(checkpoint: Checkpoint, *, out=None, dtype=None, stream=None
     L = _lib or load()
     what = "checkpoint"
     device = checkpoint.values.device
-    _need(device.type == "cuda", "checkpoint: the tensors must be on one GPU")
+    if not (device.type == "cuda"):
+        _need(False, "checkpoint: the tensors must be on one GPU")
     handle, other = _stream_of(torch, stream, device)
     if out is None:
-        with torch.cuda.stream(other):
+        with _pool(torch, other):
             out = torch.empty(checkpoint.shape, dtype=dtype or checkpoint.dtype, device=device)
-    _need(tuple(out.shape) == checkpoint.shape and (dtype is None or out.dtype == dtype), "%s: out must have the checkpoint's shape" % what)
-    _need(out.device == device, "%s: the tensors must be on one GPU" % what)
+    if not (tuple(out.shape) == checkpoint.shape and (dtype is None or out.dtype == dtype)):
+        _need(False, "%s: out must have the checkpoint's shape" % what)
+    if not (out.device == device):
+        _need(False, "%s: the tensors must be on one GPU" % what)
     k = checkpoint.kept(what, device)
     rows, stride = _flat(what, out)
     d = KeptDesc(rows, checkpoint.width, stride, _type(out, what))
@@ -1405,18 +1478,23 @@ def mlp_act(up, gate=None, *, kind: str = "silu", save=False, out=None, stream=N
     what = "activation"
     _no_graph(torch, what, up, gate)
     _here(what, up, gate, out)
-    _need(kind in _ACTS, "activation: kind must be 'silu' or 'gelu'")
+    if not (kind in _ACTS):
+        _need(False, "activation: kind must be 'silu' or 'gelu'")
     handle, other = _stream_of(torch, stream, up.device)
-    _need(up.dim() >= 1 and up.shape[-1] >= 1, "activation: the last dimension must be at least 1")
-    _need(gate is None or (gate.shape == up.shape and gate.dtype == up.dtype), "activation: gate must have up's shape and type")
+    if not (up.dim() >= 1 and up.shape[-1] >= 1):
+        _need(False, "activation: the last dimension must be at least 1")
+    if not (gate is None or (gate.shape == up.shape and gate.dtype == up.dtype)):
+        _need(False, "activation: gate must have up's shape and type")
     if out is None:
-        with torch.cuda.stream(other):
+        with _pool(torch, other):
             out = torch.empty(up.shape, dtype=up.dtype, device=up.device)
-    _need(out.shape == up.shape and out.dtype == up.dtype, "activation: out must have up's shape and type")
+    if not (out.shape == up.shape and out.dtype == up.dtype):
+        _need(False, "activation: out must have up's shape and type")
     keep = (None, None)
     if save:
         pair = (None, None) if save is True else save
-        _need(len(pair) == 2, "activation: save must be a bool or (up's checkpoint, gate's or None)")
+        if not (len(pair) == 2):
+            _need(False, "activation: save must be a bool or (up's checkpoint, gate's or None)")
         keep = (_checkpoint_for(what, up, pair[0], other), None if gate is None else _checkpoint_for(what, gate, pair[1], other))
     rows, stride = _flat(what, up)
     d = ActDesc(rows, up.shape[-1], stride, 0 if gate is None else _flat(what, gate)[1], _flat(what, out)[1], 0, _type(up, what), _ACTS[kind])
@@ -1434,18 +1512,23 @@ def mlp_act_grad(dout, up: Checkpoint, gate: Checkpoint | None = None, *, kind: 
     L = _lib or load()
     what = "activation's gradient"
     _here(what, dout, dup, dgate, out)
-    _need(kind in _ACTS, "activation: kind must be 'silu' or 'gelu'")
-    _need(isinstance(up, Checkpoint) and (gate is None or isinstance(gate, Checkpoint)), "%s: up and gate must be checkpoints" % what)
-    _need(up.shape == tuple(dout.shape) and (gate is None or gate.shape == up.shape), "%s: a checkpoint of another shape" % what)
-    _need(gate is not None or dgate is None, "%s: of a gate that is not there" % what)
+    if not (kind in _ACTS):
+        _need(False, "activation: kind must be 'silu' or 'gelu'")
+    if not (isinstance(up, Checkpoint) and (gate is None or isinstance(gate, Checkpoint))):
+        _need(False, "%s: up and gate must be checkpoints" % what)
+    if not (up.shape == tuple(dout.shape) and (gate is None or gate.shape == up.shape)):
+        _need(False, "%s: a checkpoint of another shape" % what)
+    if not (gate is not None or dgate is None):
+        _need(False, "%s: of a gate that is not there" % what)
     handle, other = _stream_of(torch, stream, dout.device)
-    with torch.cuda.stream(other):
+    with _pool(torch, other):
         if dup is None:
             dup = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
         if gate is not None and dgate is None:
             dgate = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
     for t in (dup, dgate, out):
-        _need(t is None or (t.shape == dout.shape and t.dtype == dout.dtype), "%s: an output must have dout's shape and type" % what)
+        if not (t is None or (t.shape == dout.shape and t.dtype == dout.dtype)):
+            _need(False, "%s: an output must have dout's shape and type" % what)
     rows, stride = _flat(what, dout)
     d = ActDesc(rows, up.width, _flat(what, dup)[1], 0 if gate is None else _flat(what, dgate)[1], stride, 0 if out is None else _flat(what, out)[1],
                 _type(dout, what), _ACTS[kind])
