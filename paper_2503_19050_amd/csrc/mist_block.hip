@@ -177,14 +177,15 @@ struct Input {
   mist::Raw8<A> b[U];
 };
 
-// Waves of the largest block of a kernel: rows beside each other in one, and what more than eight need, 128 registers at most, is not
-// asked of smaller ones.
-constexpr int most_waves(int u, int l, bool wide) { return l < 64 ? 1 : u == 1 && !wide ? kMostWaves / 2 : kMostWaves; }
+// Waves of a kernel's largest block.  Kernels for rows of up to ten waves (eight with a norm before or a gate) are built apart from those
+// for wider ones, which have 128 registers at most; rows beside each other are one wave's.
+constexpr int narrow_waves(bool more) { return more ? 8 : 10; }
+constexpr int most_waves(int u, int l, bool wide, bool more) { return l < 64 ? 1 : u == 1 && !wide ? narrow_waves(more) : kMostWaves; }
 
 // The next row is read before the sums of this one are waited for, where the registers are there.
 // MORE: a norm before, or a gate.
 template <class A, class R, int U, int L, bool WIDE, bool MORE>
-__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
+__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
   constexpr int kRows = 64 / L;  // of a block at a time
   __shared__ float2 part[3 * kMostWaves];
   Join<L> join{part, part + 2 * kMostWaves, (int)blockDim.x / 64, 0};
@@ -273,7 +274,7 @@ struct BackInput {
 // With e the gradient of gate v (v = n post_weight + post_bias) over a sequence's tokens, the sums of e and of e n are all
 // that the gradients of gate, post_weight and post_bias need: two sums a column for three.
 template <class A, class R, int U, int L, bool WIDE, bool MORE>
-__global__ __launch_bounds__(most_waves(U, L, WIDE) * 64, MORE && !WIDE ? 2 : back_waves(U, L, WIDE, sizeof(R))) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
+__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 2 : back_waves(U, L, WIDE, sizeof(R))) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
                                                                           A* dblock) {
   constexpr bool kAhead = U == 1 && !(MORE && WIDE);
   constexpr int kRows = 64 / L;
@@ -498,9 +499,9 @@ int lanes(int64_t hidden) { return hidden <= 128 ? 16 : hidden <= 256 ? 32 : 64;
 int units(int64_t hidden) { return hidden > kMostWaves * 512 ? 2 : 1; }
 unsigned threads(int64_t hidden) { return (unsigned)((hidden + units(hidden) * 512 - 1) / (units(hidden) * 512) * 64); }
 
-// f(activation type, residual type, columns a thread / 8, lanes a row, more than eight waves)
+// f(activation type, residual type, columns a thread / 8, lanes a row, a wide row)
 template <class F>
-void with_kernel(const mist_block_desc* d, F&& f) {
+void with_kernel(const mist_block_desc* d, bool more, F&& f) {
   mist::with_type(d->type, [&](auto x) {
     using A = typename decltype(x)::type;
     auto run = [&](auto r) {
@@ -510,7 +511,7 @@ void with_kernel(const mist_block_desc* d, F&& f) {
       if (units(d->hidden) == 2) f(A{}, R{}, std::integral_constant<int, 2>{}, Wave{}, std::true_type{});
       else if (lanes(d->hidden) == 32) f(A{}, R{}, One{}, std::integral_constant<int, 32>{}, std::false_type{});
       else if (lanes(d->hidden) == 16) f(A{}, R{}, One{}, std::integral_constant<int, 16>{}, std::false_type{});
-      else if (threads(d->hidden) > kMostWaves / 2 * 64) f(A{}, R{}, One{}, Wave{}, std::true_type{});
+      else if (threads(d->hidden) > (unsigned)narrow_waves(more) * 64) f(A{}, R{}, One{}, Wave{}, std::true_type{});
       else f(A{}, R{}, One{}, Wave{}, std::false_type{});
     };
     if (d->res_type == d->type) run(x);
@@ -525,7 +526,8 @@ mist_status launched(const char* what) {
 
 // Waves of the backward pass that a CU holds: one round of blocks of the same work (two to four rounds took 0-5 % more).
 int64_t resident_waves(const mist_block_desc* d, int64_t waves, bool more) {
-  return more && waves <= kMostWaves / 2 ? 12 : 4 * back_waves(units(d->hidden), lanes(d->hidden), waves == 1 || waves > kMostWaves / 2, (size_t)mist::type_bytes(d->res_type));
+  const bool wide = waves == 1 || waves > narrow_waves(more);
+  return more && !wide ? 12 : more ? 16 : 4 * back_waves(units(d->hidden), lanes(d->hidden), wide, (size_t)mist::type_bytes(d->res_type));
 }
 
 Parts parts_of(const mist_block_desc* d, bool by_sequence, bool more) {
@@ -589,7 +591,7 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   if (const mist_status st = check_tensors(d, {{x, d->x_stride, d->res_type, false, {}}, {block, d->block_stride, d->type, false, {}},
                                                {y, d->y_stride, d->res_type, true, {x, block}}, {h, d->h_stride, d->type, true, {}}}))
     return st;
-  with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
+  with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide) {
     using A = decltype(e);
     using R = decltype(f);
     const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, wide.value, true> : k_forward<A, R, u.value, l.value, wide.value, false>;
@@ -653,7 +655,7 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
   }
   const hipStream_t st = (hipStream_t)stream;
   if (any) {
-    with_kernel(d, [&](auto e, auto f, auto u, auto l, auto wide) {
+    with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide) {
       using A = decltype(e);
       using R = decltype(f);
       const auto kernel = post_weight || gate          ? k_backward<A, R, u.value, l.value, wide.value, true>

@@ -192,7 +192,8 @@ mist_status check_tensors(const Shape& s, int32_t type, std::initializer_list<Te
         return lib_fail(MIST_E_INVALID, "kept activations: an output overlaps another tensor");
     }
   }
-  for (const mist_kept* k : ks) {
+  for (auto it = ks.begin(); it != ks.end(); ++it) {
+    const mist_kept* k = *it;
     if (!k) continue;
     if (s.rows && (!k->values || !k->exponents)) return lib_fail(MIST_E_INVALID, "kept activations: null buffer");
     if (!mist::is_aligned(k->values, 16)) return lib_fail(MIST_E_INVALID, "kept activations: values are not aligned to 16");
@@ -201,9 +202,8 @@ mist_status check_tensors(const Shape& s, int32_t type, std::initializer_list<Te
         return lib_fail(MIST_E_INVALID, "kept activations: values or exponents overlap a tensor");
     if (!ks_out) continue;
     if (mist::overlap(values_of(s, k), exponents_of(s, k))) return lib_fail(MIST_E_INVALID, "kept activations: values and exponents overlap");
-    for (const mist_kept* o : ks)
-      if (o && o != k &&
-          (mist::overlap(values_of(s, k), values_of(s, o)) || mist::overlap(values_of(s, k), exponents_of(s, o)) || mist::overlap(exponents_of(s, k), exponents_of(s, o))))
+    for (auto o = ks.begin(); o != it; ++o)
+      if (*o && (mist::overlap(values_of(s, k), values_of(s, *o)) || mist::overlap(values_of(s, k), exponents_of(s, *o)) || mist::overlap(exponents_of(s, k), exponents_of(s, *o))))
         return lib_fail(MIST_E_INVALID, "kept activations: two of them overlap");
   }
   return MIST_OK;
