@@ -11,6 +11,7 @@
 
 #include "mist_ops.h"
 
+using mist::Eight;
 using mist::Float8;
 using mist::hip_failed;
 using mist::lib_fail;
@@ -34,10 +35,11 @@ struct BlockArgs {
   const void *weight, *bias, *post_weight, *post_bias, *gate;
 };
 
-__device__ __forceinline__ Float8 load_weight(const void* p, int32_t type, int64_t col, int64_t left) {
-  if (type == MIST_F32) return load8((const float*)p + col, left);
-  if (type == MIST_BF16) return load8((const __bf16*)p + col, left);
-  return load8((const _Float16*)p + col, left);
+template <bool WHOLE>
+__device__ __forceinline__ Float8 load_weight(const void* p, int32_t type, int64_t row, const Eight<WHOLE>& c) {
+  if (type == MIST_F32) return load8((const float*)p + row, c);
+  if (type == MIST_BF16) return load8((const __bf16*)p + row, c);
+  return load8((const _Float16*)p + row, c);
 }
 __device__ __forceinline__ void store_weight(void* p, int32_t type, int64_t at, float x, int32_t accumulate) {
   if (type == MIST_F32) ((float*)p)[at] = accumulate ? ((float*)p)[at] + x : x;
@@ -46,10 +48,11 @@ __device__ __forceinline__ void store_weight(void* p, int32_t type, int64_t at, 
 }
 
 __device__ __forceinline__ float sum8(Float8 x) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
-__device__ __forceinline__ Float8 masked(Float8 x, int64_t left) {
+template <bool WHOLE>
+__device__ __forceinline__ Float8 masked(Float8 x, const Eight<WHOLE>& c) {
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    if (k >= left) x[k] = 0.0f;
+    if (!WHOLE && k >= c.left) x[k] = 0.0f;
   return x;
 }
 
@@ -105,15 +108,14 @@ struct Join {
 };
 
 // A thread's columns.
-template <int U, int L>
+template <int U, int L, bool WHOLE>
 struct Columns {
-  int col[U], left[U];
+  Eight<WHOLE> e[U];
   __device__ __forceinline__ explicit Columns(const BlockArgs& a) {
     const int lane = L < 64 ? (int)threadIdx.x % L : (int)threadIdx.x, all = L < 64 ? L : (int)blockDim.x;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      col[u] = (u * all + lane) * 8;
-      left[u] = (int)a.hidden - col[u];  // none where <= 0
+      e[u] = Eight<WHOLE>((u * all + lane) * 8, (int)a.hidden);
     }
   }
 };
@@ -124,18 +126,18 @@ __device__ __forceinline__ void each(F&& f) {
 }
 
 // A thread's values of a weight, `none` without one: in registers, or read where they are used by rows of more than 8192 columns.
-template <int U, int L>
+template <int U, int L, bool WHOLE>
 struct Weights {
   const void* p;
-  const Columns<U, L>& c;
+  const Columns<U, L, WHOLE>& c;
   int32_t type;
   float none;
   Float8 held;
-  __device__ __forceinline__ Weights(const BlockArgs& a, const void* weight, const Columns<U, L>& columns, float without)
+  __device__ __forceinline__ Weights(const BlockArgs& a, const void* weight, const Columns<U, L, WHOLE>& columns, float without)
       : p(weight), c(columns), type(a.weight_type), none(without) {
     if (U == 1) held = read(0);
   }
-  __device__ __forceinline__ Float8 read(int u) const { return p ? load_weight(p, type, c.col[u], c.left[u]) : Float8(none); }
+  __device__ __forceinline__ Float8 read(int u) const { return p ? load_weight(p, type, 0, c.e[u]) : Float8(none); }
   __device__ __forceinline__ Float8 operator()(int u) const { return U == 1 ? held : read(u); }
 };
 
@@ -144,8 +146,8 @@ struct Moments {
 };
 // The variance is of the distances from the mean, not a difference of squares: of each wave's values from that wave's mean, and of
 // the waves' means, so that the waves meet once.
-template <int U, int L>
-__device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, const Columns<U, L>& c, const Float8* x) {
+template <int U, int L, bool WHOLE>
+__device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, const Columns<U, L, WHOLE>& c, const Float8* x) {
   float s = 0.0f, q = 0.0f;
   if (!a.layer) {
     each<U>([&](int u) { s += sum8(x[u] * x[u]); });
@@ -156,7 +158,7 @@ __device__ __forceinline__ Moments moments(const BlockArgs& a, Join<L>& join, co
   const bool alone = L < 64 || join.waves == 1;
   const float near = s * (alone ? a.inv_hidden : join.count[threadIdx.x / 64].y);
   each<U>([&](int u) {
-    const Float8 d = masked(x[u] - near, c.left[u]);
+    const Float8 d = masked(x[u] - near, c.e[u]);
     q += sum8(d * d);
   });
   q = wave_sum<L>(q);
@@ -184,22 +186,22 @@ constexpr int most_waves(int u, int l, bool wide, bool more) { return l < 64 ? 1
 
 // The next row is read before the sums of this one are waited for, where the registers are there.
 // MORE: a norm before, or a gate.
-template <class A, class R, int U, int L, bool WIDE, bool MORE>
+template <class A, class R, int U, int L, bool WIDE, bool WHOLE, bool MORE>
 __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
   constexpr int kRows = 64 / L;  // of a block at a time
   __shared__ float2 part[3 * kMostWaves];
   Join<L> join{part, part + 2 * kMostWaves, (int)blockDim.x / 64, 0};
   join.template count_columns<U>(a);
-  const Columns<U, L> c(a);
-  const Weights<U, L> w(a, a.weight, c, 1.0f), wb(a, a.bias, c, 0.0f), pw(a, MORE ? a.post_weight : nullptr, c, 1.0f), pb(a, MORE ? a.post_bias : nullptr, c, 0.0f);
-  const Weights<U, L> shared_gate(a, !MORE || a.gate_stride ? nullptr : a.gate, c, 1.0f);
+  const Columns<U, L, WHOLE> c(a);
+  const Weights<U, L, WHOLE> w(a, a.weight, c, 1.0f), wb(a, a.bias, c, 0.0f), pw(a, MORE ? a.post_weight : nullptr, c, 1.0f), pb(a, MORE ? a.post_bias : nullptr, c, 0.0f);
+  const Weights<U, L, WHOLE> shared_gate(a, !MORE || a.gate_stride ? nullptr : a.gate, c, 1.0f);
   const int sub = L < 64 ? (int)threadIdx.x / L : 0;
   auto read = [&](int64_t t0) {
     const int64_t t = min(t0 + sub, a.n - 1);
     Input<A, R, U> in;
     each<U>([&](int u) {
-      in.x[u] = mist::load_raw8(x + t * a.x_stride + c.col[u], c.left[u]);
-      if (block) in.b[u] = mist::load_raw8(block + t * a.block_stride + c.col[u], c.left[u]);
+      in.x[u] = mist::load_raw8(x + t * a.x_stride, c.e[u]);
+      if (block) in.b[u] = mist::load_raw8(block + t * a.block_stride, c.e[u]);
     });
     return in;
   };
@@ -217,31 +219,31 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(B
       now = read(t0);
     }
     Float8 v[U];
-    each<U>([&](int u) { v[u] = mist::wide8<R>(now.x[u]); });
+    each<U>([&](int u) { v[u] = mist::wide8<R>(now.x[u], c.e[u]); });
     Moments before{0.0f, 1.0f}, after{0.0f, 1.0f};
     if (block) {
       Float8 b[U];
       each<U>([&](int u) {
-        b[u] = mist::wide8<A>(now.b[u]);
+        b[u] = mist::wide8<A>(now.b[u], c.e[u]);
       });
       const int64_t gate_row = MORE && a.gate_stride ? min(t, a.n - 1) / a.seq * a.gate_stride : 0;
       if (MORE && a.post_weight) {
-        before = moments<U, L>(a, join, c, b);
+        before = moments<U, L, WHOLE>(a, join, c, b);
         each<U>([&](int u) { b[u] = (b[u] - before.mean) * before.r * pw(u) + pb(u); });
       }
       each<U>([&](int u) {
-        if (MORE) b[u] *= a.gate_stride ? load_weight(a.gate, a.weight_type, gate_row + c.col[u], c.left[u]) : shared_gate(u);
+        if (MORE) b[u] *= a.gate_stride ? load_weight(a.gate, a.weight_type, gate_row, c.e[u]) : shared_gate(u);
         v[u] = a.res_scale * v[u] + a.block_scale * b[u];
-        if (there) store8(y + t * a.y_stride + c.col[u], c.left[u], v[u]);
+        if (there) store8(y + t * a.y_stride, c.e[u], v[u]);
         // the norm is of y as it is stored: formed again from it, h has the same bits
-        v[u] = masked(mist::wide8<R>(__builtin_convertvector(v[u], mist::Raw8<R>)), c.left[u]);
+        v[u] = masked(__builtin_convertvector(__builtin_convertvector(v[u], mist::Raw8<R>), Float8), c.e[u]);
       });
     }
     if (h) {
-      after = moments<U, L>(a, join, c, v);
-      if (there) each<U>([&](int u) { store8(h + t * a.h_stride + c.col[u], c.left[u], (v[u] - after.mean) * after.r * w(u) + wb(u)); });
+      after = moments<U, L, WHOLE>(a, join, c, v);
+      if (there) each<U>([&](int u) { store8(h + t * a.h_stride, c.e[u], (v[u] - after.mean) * after.r * w(u) + wb(u)); });
     }
-    if (there && c.col[0] == 0) *(float4*)(stats + t * 4) = float4{before.mean, before.r, after.mean, after.r};
+    if (there && c.e[0].col == 0) *(float4*)(stats + t * 4) = float4{before.mean, before.r, after.mean, after.r};
   }
 }
 
@@ -273,20 +275,20 @@ struct BackInput {
 
 // With e the gradient of gate v (v = n post_weight + post_bias) over a sequence's tokens, the sums of e and of e n are all
 // that the gradients of gate, post_weight and post_bias need: two sums a column for three.
-template <class A, class R, int U, int L, bool WIDE, bool MORE>
-__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 2 : back_waves(U, L, WIDE, sizeof(R))) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
+template <class A, class R, int U, int L, bool WIDE, bool WHOLE, bool MORE>
+__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? L == 64 ? 3 : 2 : back_waves(U, L, WIDE, sizeof(R))) void k_backward(BackArgs k, const R* y, const A* block, const float* stats, const A* dh, const R* dy, R* dx,
                                                                           A* dblock) {
   constexpr bool kAhead = U == 1 && !(MORE && WIDE);
   constexpr int kRows = 64 / L;
   __shared__ float2 shared[2 * kMostWaves];
   const BlockArgs& a = k.a;
   Join<L> join{shared, nullptr, (int)blockDim.x / 64, 0};
-  const Columns<U, L> c(a);
-  const Weights<U, L> w(a, a.weight, c, 1.0f);
+  const Columns<U, L, WHOLE> c(a);
+  const Weights<U, L, WHOLE> w(a, a.weight, c, 1.0f);
   Float8 gp[U];  // gate post_weight
   Float8 sw[U] = {}, sb[U] = {}, sen[U], se[U];
-  auto post_weight = [&](int u) { return a.post_weight ? load_weight(a.post_weight, a.weight_type, c.col[u], c.left[u]) : Float8(1.0f); };
-  auto gate = [&](int u, int64_t s) { return a.gate ? load_weight(a.gate, a.weight_type, s * a.gate_stride + c.col[u], c.left[u]) : Float8(1.0f); };
+  auto post_weight = [&](int u) { return a.post_weight ? load_weight(a.post_weight, a.weight_type, 0, c.e[u]) : Float8(1.0f); };
+  auto gate = [&](int u, int64_t s) { return a.gate ? load_weight(a.gate, a.weight_type, s * a.gate_stride, c.e[u]) : Float8(1.0f); };
   const int sub = L < 64 ? (int)threadIdx.x / L : 0;
   const int64_t part = blockIdx.x, first = part / k.parts.pieces * k.parts.seqs, row0 = part % k.parts.pieces * k.parts.rows;
   const int64_t last = min(first + k.parts.seqs, k.parts.batch), row1 = min(row0 + k.parts.rows, k.parts.seq);
@@ -294,10 +296,10 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
     const int64_t t = s * k.parts.seq + min(r0 + sub, row1 - 1);
     BackInput<A, R, U> in;
     each<U>([&](int u) {
-      if (dh) in.dh[u] = mist::load_raw8(dh + t * k.dh_stride + c.col[u], c.left[u]);
-      if (dh) in.y[u] = mist::load_raw8(y + t * a.y_stride + c.col[u], c.left[u]);
-      if (dy) in.dy[u] = mist::load_raw8(dy + t * k.dy_stride + c.col[u], c.left[u]);
-      if (MORE && block) in.b[u] = mist::load_raw8(block + t * a.block_stride + c.col[u], c.left[u]);
+      if (dh) in.dh[u] = mist::load_raw8(dh + t * k.dh_stride, c.e[u]);
+      if (dh) in.y[u] = mist::load_raw8(y + t * a.y_stride, c.e[u]);
+      if (dy) in.dy[u] = mist::load_raw8(dy + t * k.dy_stride, c.e[u]);
+      if (MORE && block) in.b[u] = mist::load_raw8(block + t * a.block_stride, c.e[u]);
     });
     in.st = *(const float4*)(stats + t * 4);
     return in;
@@ -316,10 +318,10 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
       const float4 st = in.st;
       Float8 d[U], g[U], n[U], b[U];
       each<U>([&](int u) {
-        d[u] = dy ? mist::wide8<R>(in.dy[u]) : Float8(0.0f);
-        if (dh) g[u] = mist::wide8<A>(in.dh[u]);
-        if (dh) n[u] = (mist::wide8<R>(in.y[u]) - st.z) * st.w;
-        if (MORE && block) b[u] = masked((mist::wide8<A>(in.b[u]) - st.x) * st.y, c.left[u]);
+        d[u] = dy ? mist::wide8<R>(in.dy[u], c.e[u]) : Float8(0.0f);
+        if (dh) g[u] = mist::wide8<A>(in.dh[u], c.e[u]);
+        if (dh) n[u] = (mist::wide8<R>(in.y[u], c.e[u]) - st.z) * st.w;
+        if (MORE && block) b[u] = masked((mist::wide8<A>(in.b[u], c.e[u]) - st.x) * st.y, c.e[u]);
       });
       if (kAhead) {  // in the registers that have just been read
         if (r0 + kRows < row1) in = read(s, r0 + kRows);
@@ -334,13 +336,13 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
           }
           g[u] *= w(u);
           p += sum8(g[u]);
-          q += sum8(masked(g[u] * n[u], c.left[u]));
+          q += sum8(masked(g[u] * n[u], c.e[u]));
         });
         const float2 m = join.sum(p, q);
         const float mean = a.layer ? m.x * a.inv_hidden : 0.0f, along = m.y * a.inv_hidden;
         each<U>([&](int u) { d[u] += st.w * (g[u] - mean - n[u] * along); });
       }
-      if (dx && there) each<U>([&](int u) { store8(dx + t * k.dx_stride + c.col[u], c.left[u], a.res_scale * d[u]); });
+      if (dx && there) each<U>([&](int u) { store8(dx + t * k.dx_stride, c.e[u], a.res_scale * d[u]); });
       if (block) {
         each<U>([&](int u) { d[u] *= a.block_scale; });
         if (MORE) {
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
               se[u] += d[u];
               sen[u] += d[u] * b[u];
             }
-            d[u] = masked(d[u] * gp[u], c.left[u]);
+            d[u] = masked(d[u] * gp[u], c.e[u]);
           });
           if (a.post_weight) {
             float p = 0.0f, q = 0.0f;
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
             each<U>([&](int u) { d[u] = st.y * (d[u] - mean - b[u] * along); });
           }
         }
-        if (dblock && there) each<U>([&](int u) { store8(dblock + t * k.dblock_stride + c.col[u], c.left[u], d[u]); });
+        if (dblock && there) each<U>([&](int u) { store8(dblock + t * k.dblock_stride, c.e[u], d[u]); });
       }
     }
     if (MORE) {
@@ -371,31 +373,31 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
         sen[u] = over_rows<L>(sen[u]);
         if (sub) return;
         const Float8 g = gate(u, s);
-        const int64_t at = part * a.hidden + c.col[u];
+        const int64_t at = part * a.hidden;
         auto add = [&](float* p, Float8 x) {  // the part's sum over its sequences
-          if (s > first) x += load8(p + at, c.left[u]);
-          store8(p + at, c.left[u], x);
+          if (s > first) x += load8(p + at, c.e[u]);
+          store8(p + at, c.e[u], x);
         };
         if (k.slot[2]) add(k.slot[2], g * sen[u]);
         if (k.slot[3]) add(k.slot[3], g * se[u]);
         if (!k.slot[4] && !k.dgate) return;
         Float8 x = sen[u];
         if (a.post_weight) x *= post_weight(u);
-        if (a.post_bias) x += load_weight(a.post_bias, a.weight_type, c.col[u], c.left[u]) * se[u];
+        if (a.post_bias) x += load_weight(a.post_bias, a.weight_type, 0, c.e[u]) * se[u];
         if (k.slot[4]) add(k.slot[4], x);
         if (!k.dgate) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (i < c.left[u]) store_weight(k.dgate, a.weight_type, s * k.dgate_stride + c.col[u] + i, x[i], k.accumulate);
+          if (i < c.e[u].left) store_weight(k.dgate, a.weight_type, s * k.dgate_stride + c.e[u].col + i, x[i], k.accumulate);
       });
     }
   }
   each<U>([&](int u) {
-    const int64_t at = part * a.hidden + c.col[u];
+    const int64_t at = part * a.hidden;
     sw[u] = over_rows<L>(sw[u]);
     sb[u] = over_rows<L>(sb[u]);
-    if (k.slot[0] && !sub) store8(k.slot[0] + at, c.left[u], sw[u]);
-    if (k.slot[1] && !sub) store8(k.slot[1] + at, c.left[u], sb[u]);
+    if (k.slot[0] && !sub) store8(k.slot[0] + at, c.e[u], sw[u]);
+    if (k.slot[1] && !sub) store8(k.slot[1] + at, c.e[u], sb[u]);
   });
 }
 
@@ -499,7 +501,7 @@ int lanes(int64_t hidden) { return hidden <= 128 ? 16 : hidden <= 256 ? 32 : 64;
 int units(int64_t hidden) { return hidden > kMostWaves * 512 ? 2 : 1; }
 unsigned threads(int64_t hidden) { return (unsigned)((hidden + units(hidden) * 512 - 1) / (units(hidden) * 512) * 64); }
 
-// f(activation type, residual type, columns a thread / 8, lanes a row, a wide row)
+// f(activation type, residual type, columns a thread / 8, lanes a row, a wide row, whole waves)
 template <class F>
 void with_kernel(const mist_block_desc* d, bool more, F&& f) {
   mist::with_type(d->type, [&](auto x) {
@@ -508,11 +510,16 @@ void with_kernel(const mist_block_desc* d, bool more, F&& f) {
       using R = typename decltype(r)::type;
       using One = std::integral_constant<int, 1>;
       using Wave = std::integral_constant<int, 64>;
-      if (units(d->hidden) == 2) f(A{}, R{}, std::integral_constant<int, 2>{}, Wave{}, std::true_type{});
-      else if (lanes(d->hidden) == 32) f(A{}, R{}, One{}, std::integral_constant<int, 32>{}, std::false_type{});
-      else if (lanes(d->hidden) == 16) f(A{}, R{}, One{}, std::integral_constant<int, 16>{}, std::false_type{});
-      else if (threads(d->hidden) > (unsigned)narrow_waves(more) * 64) f(A{}, R{}, One{}, Wave{}, std::true_type{});
-      else f(A{}, R{}, One{}, Wave{}, std::false_type{});
+      using No = std::false_type;
+      const auto wave = [&](auto whole) {  // rows of whole waves are the common ones; the others' code has their ends to hold and to mask
+        if (threads(d->hidden) > (unsigned)narrow_waves(more) * 64) f(A{}, R{}, One{}, Wave{}, std::true_type{}, whole);
+        else f(A{}, R{}, One{}, Wave{}, No{}, whole);
+      };
+      if (units(d->hidden) == 2) f(A{}, R{}, std::integral_constant<int, 2>{}, Wave{}, std::true_type{}, No{});
+      else if (lanes(d->hidden) == 32) f(A{}, R{}, One{}, std::integral_constant<int, 32>{}, No{}, No{});
+      else if (lanes(d->hidden) == 16) f(A{}, R{}, One{}, std::integral_constant<int, 16>{}, No{}, No{});
+      else if (d->hidden % 512 == 0) wave(std::true_type{});
+      else wave(No{});
     };
     if (d->res_type == d->type) run(x);
     else run(mist::Elem<MIST_F32>{});
@@ -591,10 +598,10 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   if (const mist_status st = check_tensors(d, {{x, d->x_stride, d->res_type, false, {}}, {block, d->block_stride, d->type, false, {}},
                                                {y, d->y_stride, d->res_type, true, {x, block}}, {h, d->h_stride, d->type, true, {}}}))
     return st;
-  with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide) {
+  with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide, auto whole) {
     using A = decltype(e);
     using R = decltype(f);
-    const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, wide.value, true> : k_forward<A, R, u.value, l.value, wide.value, false>;
+    const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, wide.value, whole.value, true> : k_forward<A, R, u.value, l.value, wide.value, whole.value, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
                        (const R*)x, (const A*)block, (R*)y, (A*)h, stats);
   });
@@ -655,12 +662,12 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
   }
   const hipStream_t st = (hipStream_t)stream;
   if (any) {
-    with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide) {
+    with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide, auto whole) {
       using A = decltype(e);
       using R = decltype(f);
-      const auto kernel = post_weight || gate          ? k_backward<A, R, u.value, l.value, wide.value, true>
-                          : threads(d->hidden) == 64 && l.value == 64 ? k_backward<A, R, u.value, l.value, true, false>
-                                                                      : k_backward<A, R, u.value, l.value, wide.value, false>;
+      const auto kernel = post_weight || gate          ? k_backward<A, R, u.value, l.value, wide.value, whole.value, true>
+                          : threads(d->hidden) == 64 && l.value == 64 ? k_backward<A, R, u.value, l.value, true, whole.value, false>
+                                                                      : k_backward<A, R, u.value, l.value, wide.value, whole.value, false>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)p.parts.n), dim3(threads(d->hidden)), 0, st, k, (const R*)y, (const A*)block, stats, (const A*)g->dh,
                          (const R*)g->dy, (R*)g->dx, (A*)g->dblock);
     });

@@ -27,7 +27,8 @@ typedef int8_t Byte8 __attribute__((ext_vector_type(8)));
 // Eight columns of a row: work of one lane.
 struct Place {
   int64_t row;
-  int32_t group, col, left;  // left: columns there are from col on, none where <= 0
+  int32_t group;
+  mist::Eight<> c;
 };
 
 struct Shape {
@@ -47,7 +48,7 @@ __device__ __forceinline__ void each_place(const Shape& s, F&& f) {
     row += more;
     at -= more * per_row;
     if (row >= s.rows) continue;  // whole groups of lanes
-    f(Place{row, (int32_t)(at / kLanes), (int32_t)(at * 8), s.width - (int32_t)(at * 8)});
+    f(Place{row, (int32_t)(at / kLanes), mist::Eight<>((int)(at * 8), s.width)});
   }
 }
 
@@ -71,14 +72,14 @@ __device__ __forceinline__ void store_group(const Shape& s, const Place& p, Floa
   Byte8 q;
 #pragma unroll
   for (int i = 0; i < 8; ++i) q[i] = byte == 255 ? 0 : (int8_t)(int)fminf(fmaxf(rintf(x[i] * inverse), -127.0f), 127.0f);
-  *(Byte8*)(k.values + (p.row * s.groups + p.group) * MIST_KEPT_GROUP + p.col % MIST_KEPT_GROUP) = q;
-  if (p.col % MIST_KEPT_GROUP == 0) k.exponents[p.row * s.groups + p.group] = (uint8_t)byte;
+  *(Byte8*)(k.values + (p.row * s.groups + p.group) * MIST_KEPT_GROUP + p.c.col % MIST_KEPT_GROUP) = q;
+  if (p.c.col % MIST_KEPT_GROUP == 0) k.exponents[p.row * s.groups + p.group] = (uint8_t)byte;
 }
 
 // The byte 255 gives an infinite factor of zeros: NaN.
 __device__ __forceinline__ Float8 load_group(const Shape& s, const Place& p, const mist_kept& k) {
   const float step = __uint_as_float((uint32_t)k.exponents[p.row * s.groups + p.group] << 23);
-  const Byte8 q = *(const Byte8*)(k.values + (p.row * s.groups + p.group) * MIST_KEPT_GROUP + p.col % MIST_KEPT_GROUP);
+  const Byte8 q = *(const Byte8*)(k.values + (p.row * s.groups + p.group) * MIST_KEPT_GROUP + p.c.col % MIST_KEPT_GROUP);
   return __builtin_convertvector(q, Float8) * step;
 }
 
@@ -93,12 +94,12 @@ __device__ __forceinline__ Float8 in_range(Float8 x) {
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_store(Shape s, const T* x, int64_t stride, mist_kept k) {
-  each_place(s, [&](const Place& p) { store_group(s, p, load8(x + p.row * stride + p.col, p.left), k); });
+  each_place(s, [&](const Place& p) { store_group(s, p, load8(x + p.row * stride, p.c), k); });
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_load(Shape s, mist_kept k, T* x, int64_t stride) {
-  each_place(s, [&](const Place& p) { store8(x + p.row * stride + p.col, p.left, in_range<T>(load_group(s, p, k))); });
+  each_place(s, [&](const Place& p) { store8(x + p.row * stride, p.c, in_range<T>(load_group(s, p, k))); });
 }
 
 // The activation and its derivative.  With e = exp(-z) and p = 1 / (1 + e), 1 - p is e p, without the difference's loss; where e is
@@ -127,21 +128,21 @@ struct Strides {
 template <class T, int KIND, bool GATE>
 __global__ __launch_bounds__(kThreads) void k_act(Shape s, Strides st, const T* up, const T* gate, T* out, mist_kept up8, mist_kept gate8) {
   each_place(s, [&](const Place& p) {
-    const Float8 u = load8(up + p.row * st.up + p.col, p.left);
+    const Float8 u = load8(up + p.row * st.up, p.c);
     Float8 g, y;
-    if (GATE) g = load8(gate + p.row * st.gate + p.col, p.left);
+    if (GATE) g = load8(gate + p.row * st.gate, p.c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = GATE ? act<KIND>(g[i]).a * u[i] : act<KIND>(u[i]).a;
     if (up8.values) store_group(s, p, u, up8);
     if (GATE && gate8.values) store_group(s, p, g, gate8);
-    store8(out + p.row * st.out + p.col, p.left, y);
+    store8(out + p.row * st.out, p.c, y);
   });
 }
 
 template <class T, int KIND, bool GATE>
 __global__ __launch_bounds__(kThreads) void k_act_back(Shape s, Strides st, mist_kept up8, mist_kept gate8, const T* dout, T* dup, T* dgate, T* again) {
   each_place(s, [&](const Place& p) {
-    const Float8 d = load8(dout + p.row * st.out + p.col, p.left), u = load_group(s, p, up8);
+    const Float8 d = load8(dout + p.row * st.out, p.c), u = load_group(s, p, up8);
     Float8 g, y, du, dg;
     if (GATE) g = load_group(s, p, gate8);
 #pragma unroll
@@ -151,9 +152,9 @@ __global__ __launch_bounds__(kThreads) void k_act_back(Shape s, Strides st, mist
       du[i] = d[i] * (GATE ? f.a : f.slope);
       if (GATE) dg[i] = d[i] * u[i] * f.slope;
     }
-    store8(dup + p.row * st.up + p.col, p.left, du);
-    if (GATE) store8(dgate + p.row * st.gate + p.col, p.left, dg);
-    if (again) store8(again + p.row * st.again + p.col, p.left, y);
+    store8(dup + p.row * st.up, p.c, du);
+    if (GATE) store8(dgate + p.row * st.gate, p.c, dg);
+    if (again) store8(again + p.row * st.again, p.c, y);
   });
 }
 

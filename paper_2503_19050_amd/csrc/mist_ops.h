@@ -43,41 +43,73 @@ struct Vec {
 
 typedef float Float8 __attribute__((ext_vector_type(8)));
 
-// Eight consecutive values as fp32, of which `left` are there (the others are `fill`).
-template <class T>
-__device__ __forceinline__ Float8 load8(const T* p, int64_t left, float fill = 0.0f) {
-  if (left >= 8) return __builtin_convertvector(*(const typename Vec<T, 8>::type*)p, Float8);
-  Float8 x = fill;
-#pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (k < left) x[k] = (float)p[k];
-  return x;
-}
-// The same as they are stored, zeros for those that are not there: 4 registers of 16-bit values.
+// Eight columns of a row.  The columns at its end, and lanes past it, are read from the row's last eight values, in bounds and without
+// a branch, and moved down when they are used: read value by value they would be waited for eight times (residual and norm of
+// 65536 x 2559 bf16: 513 us so, 330 by one access).
+// WHOLE: every lane has all eight.
+template <bool WHOLE = false>
+struct Eight {
+  int col, left;  // left: columns there are from col on, none where <= 0
+  int at, shift;  // the columns read, and how far they are to be moved down (8: nothing is left)
+  bool narrow;    // the row has less than eight
+  __device__ __forceinline__ Eight() {}
+  __device__ __forceinline__ Eight(int column, int width) : col(column), left(width - column), narrow(width < 8) {
+    at = narrow ? 0 : min(col, width - 8);
+    shift = narrow ? 0 : min(col - at, 8);
+  }
+};
+
+// As they are stored: 4 registers of 16-bit values.
 template <class T>
 using Raw8 = T __attribute__((ext_vector_type(8)));
-template <class T>
-__device__ __forceinline__ Raw8<T> load_raw8(const T* p, int64_t left) {
-  if (left >= 8) return *(const typename Vec<T, 8>::type*)p;
+template <class T, bool WHOLE>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* row, const Eight<WHOLE>& c) {
+  if (WHOLE) return *(const typename Vec<T, 8>::type*)(row + c.col);
+  if (!c.narrow) return *(const typename Vec<T, 8>::type*)(row + c.at);
   Raw8<T> x = (T)0.0f;
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    if (k < left) x[k] = p[k];
+    if (k < c.left) x[k] = row[c.col + k];
   return x;
 }
-template <class T>
-__device__ __forceinline__ Float8 wide8(Raw8<T> x) {
-  return __builtin_convertvector(x, Float8);
+// Moved down, with zeros for what is not there.
+template <class T, bool WHOLE>
+__device__ __forceinline__ Raw8<T> settled(Raw8<T> x, const Eight<WHOLE>& c) {
+  if (WHOLE) return x;
+  typedef uint32_t Words __attribute__((ext_vector_type(sizeof(Raw8<T>) / 4)));
+  constexpr int kWords = sizeof(Raw8<T>) / 4, kPer = 4 / sizeof(T);
+  if (c.shift) {
+    Words w = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (int step = 8; step >= kPer; step /= 2) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) w[k] = !(c.shift & step) ? w[k] : k + step / kPer < kWords ? w[k + step / kPer] : 0u;
+    }
+    if (kPer == 2) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) w[k] = !(c.shift & 1) ? w[k] : k + 1 < kWords ? w[k] >> 16 | w[k + 1] << 16 : w[k] >> 16;
+    }
+    x = __builtin_bit_cast(Raw8<T>, w);
+  }
+  return x;
 }
-template <class T>
-__device__ __forceinline__ void store8(T* p, int64_t left, Float8 x) {
-  if (left >= 8) {
-    *(typename Vec<T, 8>::type*)p = __builtin_convertvector(x, typename Vec<T, 8>::type);
+template <class T, bool WHOLE>
+__device__ __forceinline__ Float8 wide8(Raw8<T> x, const Eight<WHOLE>& c) {
+  return __builtin_convertvector(settled<T>(x, c), Float8);
+}
+template <class T, bool WHOLE>
+__device__ __forceinline__ Float8 load8(const T* row, const Eight<WHOLE>& c) {
+  return wide8<T>(load_raw8(row, c), c);
+}
+template <class T, bool WHOLE>
+__device__ __forceinline__ void store8(T* row, const Eight<WHOLE>& c, Float8 x) {
+  if (WHOLE || c.left >= 8) {
+    *(typename Vec<T, 8>::type*)(row + c.col) = __builtin_convertvector(x, typename Vec<T, 8>::type);
     return;
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    if (k < left) p[k] = (T)x[k];
+    if (k < c.left) row[c.col + k] = (T)x[k];
 }
 
 // Sum, or largest, over a wave; every lane has the result.  Exchanges within 16 lanes are operands of the additions
