@@ -65,8 +65,8 @@ __device__ __forceinline__ void store_group(const Shape& s, const Place& p, Floa
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-#pragma unroll
-  for (int d = 1; d < kLanes; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d, kLanes));
+  static_assert(kLanes == 16, "a group is a row of lanes");
+  most = mist::most_of_16(most);
   const uint32_t byte = byte_of(most);
   const float inverse = byte == 255 ? 0.0f : __uint_as_float((254 - byte) << 23);
   Byte8 q;

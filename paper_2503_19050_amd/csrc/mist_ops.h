@@ -115,8 +115,19 @@ __device__ __forceinline__ void store8(T* row, const Eight<WHOLE>& c, Float8 x) 
 // Sum, or largest, over a wave; every lane has the result.  Exchanges within 16 lanes are operands of the additions
 // themselves, those of halves and quarters of the wave two instructions: no trip through shared memory.
 template <int CTRL>
+__device__ __forceinline__ uint32_t lanes(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL>
 __device__ __forceinline__ float lanes(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+  return __uint_as_float(lanes<CTRL>(__float_as_uint(x)));
+}
+// The largest of 16 neighbouring lanes, as unsigned numbers.
+__device__ __forceinline__ uint32_t most_of_16(uint32_t x) {
+  x = max(x, lanes<0xB1>(x));   // pairs
+  x = max(x, lanes<0x4E>(x));   // fours
+  x = max(x, lanes<0x141>(x));  // eights: mirrored
+  return max(x, lanes<0x140>(x));
 }
 template <class J>
 __device__ __forceinline__ float join_pairs_of_16(float x, J join) {

@@ -57,9 +57,10 @@ __device__ __forceinline__ float of_rank(uint32_t r) {
 // Distinct keys of alternatives: larger logits first, the lower id first among equals.
 __device__ __forceinline__ uint64_t key_of(uint32_t rank, uint32_t id) { return (uint64_t)rank << 32 | (uint32_t)~id; }
 
+template <int L = 64>
 __device__ __forceinline__ uint64_t wave_max_key(uint64_t x) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
+  for (int d = L / 2; d; d >>= 1) {
     const uint64_t y = (uint64_t)__shfl_xor((int)(x >> 32), d) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)x, d);
     x = y > x ? y : x;
   }
@@ -446,29 +447,31 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
   }
 }
 
-// One wave a token.
+// L lanes a token: 16 where that many ranks are all (8 ranks of 32768 tokens: 15 us with 64 lanes a token, 6 with 16).
+template <int L>
 __global__ __launch_bounds__(kThreads) void k_join(TokenArgs a, int32_t ranks, const float* stats, const int32_t* ids, const float* zs,
                                                    const void* targets, float* logp, float* lse, float* entropy, int32_t* out_ids,
                                                    float* out_logp) {
-  const int lane = threadIdx.x % 64;
-  for (int64_t t = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64; t < a.n; t += (int64_t)gridDim.x * (kThreads / 64)) {
+  const int lane = threadIdx.x % L;
+  const auto most = [](float x) { return mist::wave_join<L>(x, [](float p, float q) { return fmaxf(p, q); }); };
+  for (int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L; t < a.n; t += (int64_t)gridDim.x * (kThreads / L)) {
     Stats r{-HUGE_VALF, 0.0f, 0.0f, -HUGE_VALF};
-    for (int32_t k = lane; k < ranks; k += 64) {
+    for (int32_t k = lane; k < ranks; k += L) {
       const float4 x = *(const float4*)(stats + ((int64_t)k * a.n + t) * 4);
       r.m = fmaxf(r.m, x.x);
       r.z = fmaxf(r.z, x.w);
     }
-    r.m = wave_max(r.m);
-    r.z = wave_max(r.z);
+    r.m = most(r.m);
+    r.z = most(r.z);
     const float from = r.m == -HUGE_VALF ? 0.0f : r.m;
-    for (int32_t k = lane; k < ranks; k += 64) {
+    for (int32_t k = lane; k < ranks; k += L) {
       const float4 x = *(const float4*)(stats + ((int64_t)k * a.n + t) * 4);
       const float d = x.x - from, f = expf(d);
       r.s = fmaf(f, x.y, r.s);
       r.u += f * fmaf(fmaxf(d, kLow), x.y, x.z);
     }
-    r.s = wave_sum(r.s);
-    r.u = wave_sum(r.u);
+    r.s = wave_sum<L>(r.s);
+    r.u = wave_sum<L>(r.u);
     const float l = lse_of(r);
     const int64_t target = targets ? target_of(a, targets, (int32_t)t) : -1;
     if (lane == 0) {
@@ -479,14 +482,14 @@ __global__ __launch_bounds__(kThreads) void k_join(TokenArgs a, int32_t ranks, c
     uint64_t last = ~0ull;
     for (int k = 0; k < a.top; ++k) {
       uint64_t best = 0;
-      for (int64_t j = lane; j < (int64_t)ranks * a.top; j += 64) {
+      for (int64_t j = lane; j < (int64_t)ranks * a.top; j += L) {
         const int64_t at = (j / a.top * a.n + t) * a.top + j % a.top;
         const int32_t id = ids[at];
         const uint32_t rank = rank_of(zs[at]);
         const uint64_t key = id >= 0 && rank ? key_of(rank, (uint32_t)id) : 0;
         if (key > best && key < last) best = key;
       }
-      last = best = wave_max_key(best);
+      last = best = wave_max_key<L>(best);
       if (lane == 0) {
         out_ids[t * a.top + k] = best ? (int32_t)~(uint32_t)best : -1;
         out_logp[t * a.top + k] = best ? of_rank((uint32_t)(best >> 32)) - l : -HUGE_VALF;
@@ -639,8 +642,9 @@ mist_status mist_token_join(const mist_token_desc* d, int32_t ranks, const float
   if (!mist::is_aligned(stats, 16) || !mist::is_aligned(targets, d->ids_bytes) || !mist::is_aligned(top_ids, 4) || !mist::is_aligned(out_ids, 4) ||
       !floats_ok({top_z, logp, lse, entropy, out_logp}))
     return lib_fail(MIST_E_INVALID, "token log probabilities: a buffer is not aligned to its elements, or stats to 16");
-  const int64_t blocks = std::min<int64_t>((a.n + kThreads / 64 - 1) / (kThreads / 64), kMostBlocks);
-  hipLaunchKernelGGL(k_join, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, ranks, stats, top_ids, top_z, targets, logp, lse,
+  const int lanes = (int64_t)ranks * std::max(1, a.top) <= 16 ? 16 : 64, tokens = kThreads / lanes;
+  const int64_t blocks = std::min<int64_t>((a.n + tokens - 1) / tokens, kMostBlocks);
+  hipLaunchKernelGGL(lanes == 16 ? k_join<16> : k_join<64>, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, ranks, stats, top_ids, top_z, targets, logp, lse,
                      entropy, out_ids, out_logp);
   return launched("token log probabilities");
 }
