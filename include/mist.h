@@ -637,9 +637,9 @@ mist_status mist_adam_step(const mist_tensors* p, const mist_tensors* m, const m
 #define MIST_TOKEN_MAX_TOP 64
 
 /* Logits of batch sequences of seq tokens: columns [vocab_begin, vocab_begin + rows) of the vocabulary, this rank's
- * shard.  With z = scale * logits, m = max z, s = sum exp(z - m) and u = sum exp(z - m) (z - m):
+ * shard.  With z = scale * logits (in fp32: past it z is +inf, or masked out), m = max z, s = sum exp(z - m) and u = sum exp(z - m) (z - m):
  * lse = m + log s, the target's log probability is z[target] - lse, the entropy log s - u / s.
- * A logit of -inf is masked out.  A target below 0 is padding: its log probability is 0 and has no gradient.  One
+ * A z of -inf is masked out.  A target below 0 is padding: its log probability is 0 and has no gradient.  One
  * of 0 or more that no rank holds, or that is masked out, has -inf.  A token whose logits are all -inf has lse = -inf,
  * entropy 0 and no gradient; one with NaN or +inf among them has NaN.  Strides are in elements; columns are contiguous. */
 typedef struct mist_token_desc {

@@ -447,7 +447,7 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       take_top<THREADS>(x + base, (int)(a.rows - base), (uint32_t)base, a.top, top, [&](int at, uint64_t key) {
         const float z = of_rank((uint32_t)(key >> 32)) * a.scale;
         o.top_ids[(int64_t)t * a.top + at] = (int32_t)(~(uint32_t)key + (uint32_t)a.vocab_begin);
-        o.top_logp[(int64_t)t * a.top + at] = o.stats ? z : z - l;
+        o.top_logp[(int64_t)t * a.top + at] = o.stats || z == -HUGE_VALF ? z : z - l;  // a finite logit whose z is past fp32
       });
       if (t + (int32_t)gridDim.x < a.n) __syncthreads();
     }

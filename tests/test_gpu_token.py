@@ -269,6 +269,26 @@ def test_all_nan(torch):
     assert r.lse.isnan().all() and r.logp.isnan().all() and r.entropy.isnan().all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [9, 5000, 70000])
+def test_logits_whose_scaled_value_passes_fp32(torch, rows, kind):
+    """z is in fp32: below its range it is masked out, above it counts as +inf; the logits themselves still have an order."""
+    from paper_2503_19050_amd import mist
+    low, high = torch.finfo(types(torch)[kind]).min, torch.finfo(types(torch)[kind]).max
+    x = torch.full((1, 3, rows), low, device="cuda", dtype=types(torch)[kind])
+    x[0, 1, 4] = 1.0
+    x[0, 2, 5] = high
+    t = torch.full((1, 3), 4, device="cuda")
+    r = mist.token_logprob(x, t, scale=1.5, entropy=True, top=2)
+    assert r.lse[0, :2].tolist() == [-math.inf, 1.5] and r.logp[0, :2].tolist() == [-math.inf, 0.0] and r.entropy[0, :2].tolist() == [0.0, 0.0]
+    assert r.top_ids.tolist() == [[[0, 1], [4, 0], [5, 0]]] and r.top_logp[0, :2].tolist() == [[-math.inf, -math.inf], [0.0, -math.inf]]
+    assert r.lse[0, 2].isnan() and r.logp[0, 2].isnan()
+    logp, d = mist.token_loss(x, t, 1.0, scale=1.5)
+    assert (d[0, 0] == 0).all() and (d[0, 1] == 0).all() and d[0, 2].isnan().any()
+    even = mist.token_logprob(x[:, :1], t[:, :1], entropy=True)   # unscaled they are equal
+    assert abs(float(even.entropy) - math.log(rows)) < 1e-5 and abs(float(even.lse) / low - 1) < 1e-6
+
+
 def test_targets_of_no_one(torch):
     """An id past the vocabulary has no probability: -inf, and a gradient of the others alone."""
     from paper_2503_19050_amd import mist
