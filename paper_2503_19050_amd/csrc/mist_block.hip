@@ -406,7 +406,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64, MORE && !WIDE ? 
 }
 
 // The parts' sums, in an order that goes by their number: parts [i * count, (i + 1) * count) give row i of out.  A block
-// takes 64 columns in 16 shares of the parts, or, of many parts, 16 columns in 64 shares.
+// takes 64 columns in 16 shares of the parts, or, of many parts, 32 columns (a cache line) in 32 shares.
 struct JoinJob {
   const float* part;
   void* out;
@@ -417,7 +417,7 @@ struct JoinArgs {
   int64_t hidden;
   int32_t type, accumulate;
 };
-__host__ __device__ __forceinline__ int join_columns(const JoinJob& j) { return j.count >= 256 ? 16 : 64; }
+__host__ __device__ __forceinline__ int join_columns(const JoinJob& j) { return j.count >= 256 ? 32 : 64; }
 
 __global__ __launch_bounds__(kJoinThreads) void k_join_parts(JoinArgs k) {
   constexpr int kWaves = kJoinThreads / 64;
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_parts(JoinArgs k) {
       for (int64_t r = mine; r < j.count; r += shares) s += p[r * k.hidden];
     }
     auto sum = [](float a, float b) { return a + b; };
-    if (width == 16) s = mist::join_pairs_of_32(mist::join_pairs_of_16(s, sum), sum);  // the shares of a wave
+    if (width == 32) s = mist::join_pairs_of_32(s, sum);  // the shares of a wave
     __syncthreads();
     share[threadIdx.x / 64][threadIdx.x % 64] = s;
     __syncthreads();
@@ -605,7 +605,8 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide, auto whole) {
     using A = decltype(e);
     using R = decltype(f);
-    const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, wide.value, whole.value, true> : k_forward<A, R, u.value, l.value, wide.value, whole.value, false>;
+    constexpr bool kWide = l.value == 64;  // its registers are the same for all
+    const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, kWide, whole.value, true> : k_forward<A, R, u.value, l.value, kWide, whole.value, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
                        (const R*)x, (const A*)block, (R*)y, (A*)h, stats);
   });
