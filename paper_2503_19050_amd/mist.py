@@ -1038,8 +1038,13 @@ def _pool(torch, other):
     return _IDLE if other is None else torch.cuda.stream(other)
 
 
+def _like(torch, t, dtype=None):
+    """A new contiguous tensor of t's shape."""
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 def _shaped(what, t, shape, dtype, name) -> None:
-    if not (t.dtype == dtype and tuple(t.shape) == tuple(shape)):
+    if not (t.dtype == dtype and t.shape == shape):
         _need(False, "%s: %s must be %s of %s" % (what, name, dtype, tuple(shape)))
 
 
@@ -1111,7 +1116,8 @@ def _top_space(torch, shape, top, device):
         return None, None
     if not (0 < top <= TOKEN_MAX_TOP):
         _need(False, "token log probabilities: top must be in 0..%d" % TOKEN_MAX_TOP)
-    return (torch.empty(shape + (top,), dtype=torch.int32, device=device), torch.empty(shape + (top,), dtype=torch.float32, device=device))
+    ids = torch.empty(shape + (top,), dtype=torch.int32, device=device)
+    return ids, torch.empty_like(ids, dtype=torch.float32)
 
 
 def token_logprob(logits, targets=None, *, scale: float = 1.0, entropy: bool = False, top: int = 0, stream=None) -> TokenLogprob:
@@ -1213,7 +1219,7 @@ def token_grad(logits, targets, lse, *, dlogp=None, entropy=None, dentropy=None,
     handle, other = _stream_of(torch, stream, logits.device)
     if dlogits is None:
         with _pool(torch, other):
-            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            dlogits = _like(torch, logits)
     if not (dlogp is None or targets is not None):
         _need(False, "%s: dlogp without targets" % what)
     if not (dentropy is None or entropy is not None):
@@ -1247,7 +1253,7 @@ def token_loss(logits, targets, weights=1.0, *, scale: float = 1.0, dlogits=None
     handle, other = _stream_of(torch, stream, device)
     with _pool(torch, other):
         if dlogits is None:
-            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=device)
+            dlogits = _like(torch, logits)
         logp = torch.empty(shape, dtype=torch.float32, device=device)
     d = _token_desc(torch, logits, targets, dlogits, 0, scale, 0)
     _on_device(torch, device, L.mist_token_loss, ctypes.byref(d), logits.data_ptr(), targets.data_ptr(), _ptr(w), factor, logp.data_ptr(),
@@ -1273,18 +1279,9 @@ def _block_gate(what, x, gate, dtype) -> int:
     return gate.stride(0) if gate.dim() == 2 else 0
 
 
-def _block_stride(what, x, t) -> int:
-    """The stride between rows of a tensor of x's shape."""
-    if t is None:
-        return 0
-    if t.shape != x.shape:
-        _need(False, "%s: the tensors must have one shape" % what)
-    return x.shape[-1] if t.is_contiguous() else _flat(what, t)[1]
-
-
 def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale):
     shape = x.shape
-    dims = len(shape)
+    dims, hidden = len(shape), shape[-1] if len(shape) else 0
     if dims != 3 and dims != 2:
         _need(False, "%s: must be [tokens, hidden] or [batch, seq, hidden]" % what)
     code = _BLOCK_KINDS.get(kind)
@@ -1293,16 +1290,25 @@ def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate
     like = block if block is not None else h if h is not None else x
     first = weight if weight is not None else post_weight if post_weight is not None else bias if bias is not None else post_bias
     first = first if first is not None else gate
-    wtype = x.dtype if first is None else first.dtype
+    rtype = x.dtype
+    wtype = rtype if first is None else first.dtype
     if weight is not None or post_weight is not None or bias is not None or post_bias is not None:
-        _block_weights(what, shape[-1], wtype, weight, bias, post_weight, post_bias)
-    if y is not None and y.dtype != x.dtype:
+        _block_weights(what, hidden, wtype, weight, bias, post_weight, post_bias)
+    strides = [hidden if x.is_contiguous() else _flat(what, x)[1], 0, 0, 0]
+    for k, t in ((1, block), (2, y), (3, h)):
+        if t is not None and t is not x:
+            if t.shape != shape:
+                _need(False, "%s: the tensors must have one shape" % what)
+            strides[k] = hidden if t.is_contiguous() else _flat(what, t)[1]
+        elif t is x:
+            strides[k] = strides[0]
+    if y is not None and y.dtype != rtype:
         _need(False, "%s: y must have x's type" % what)
     if h is not None and h.dtype != like.dtype:
         _need(False, "%s: h must have the block's type" % what)
-    return BlockDesc(shape[0] if dims == 3 else 1, shape[-2], shape[-1], _block_stride(what, x, x), _block_stride(what, x, block),
-                     _block_stride(what, x, y), _block_stride(what, x, h), 0 if gate is None else _block_gate(what, x, gate, wtype), code,
-                     _type(like, what), _type(x, what), _TYPES.get(wtype, -1), eps, res_scale, block_scale)
+    return BlockDesc(shape[0] if dims == 3 else 1, shape[-2], hidden, strides[0], strides[1], strides[2], strides[3],
+                     0 if gate is None else _block_gate(what, x, gate, wtype), code, _type(like, what), _type(x, what), _TYPES.get(wtype, -1),
+                     eps, res_scale, block_scale)
 
 
 def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, kind: str = "rms", eps: float = 1e-6,
@@ -1325,10 +1331,10 @@ def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_
         _need(False, "block norm: h without its weight")
     with _pool(torch, other):
         if block is not None and y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            y = _like(torch, x)
         if weight is not None and h is None:
-            h = torch.empty(x.shape, dtype=block.dtype if block is not None else dtype or x.dtype, device=x.device)
-        stats = torch.empty(tuple(x.shape[:-1]) + (4,), dtype=torch.float32, device=x.device)
+            h = _like(torch, x, dtype if block is None else block.dtype)
+        stats = torch.empty((*x.shape[:-1], 4), dtype=torch.float32, device=x.device)
     d = _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale)
     _on_device(torch, x.device, L.mist_block_forward, ctypes.byref(d), x.data_ptr(), _ptr(block), _ptr(weight), _ptr(bias), _ptr(post_weight),
                _ptr(post_bias), _ptr(gate), _ptr(y), _ptr(h), stats.data_ptr(), handle)
@@ -1357,23 +1363,28 @@ def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post
         _need(False, "%s: of a block that is not there" % what)
     with _pool(torch, other):
         if dx is None:
-            dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+            dx = _like(torch, y)
         if block is not None and dblock is None:
-            dblock = torch.empty(block.shape, dtype=block.dtype, device=y.device)
+            dblock = _like(torch, block)
     d = _block_desc(what, y, block, y, dh, weight, None, post_weight, post_bias, gate, kind, 0.0, res_scale, block_scale)
-    wtype = next((t.dtype for t in (weight, post_weight, post_bias, gate) if t is not None), y.dtype)
+    first = weight if weight is not None else post_weight if post_weight is not None else gate
+    wtype = y.dtype if first is None else first.dtype
     _block_weights(what, y.shape[-1], wtype, *grads)
     dgate_stride = 0
     if dgate is not None:
         if not (gate is not None and dgate.shape == gate.shape):
             _need(False, "%s: dgate must have the gate's shape" % what)
         dgate_stride = _block_gate(what, y, dgate, wtype)
-    _packed(what, stats, tuple(y.shape[:-1]) + (4,), torch.float32, "stats")
-    strides = []
-    for t, dtype in ((dh, None if block is None else block.dtype), (dy, y.dtype), (dx, y.dtype), (dblock, None if block is None else block.dtype)):
-        if not (t is None or (t.shape == y.shape and (dtype is None or t.dtype == dtype))):
+    shape, rtype = y.shape, y.dtype
+    _packed(what, stats, (*shape[:-1], 4), torch.float32, "stats")
+    strides, btype = [], None if block is None else block.dtype
+    for t, dtype in ((dh, btype), (dy, rtype), (dx, rtype), (dblock, btype)):
+        if t is None:
+            strides.append(0)
+            continue
+        if t.shape != shape or (dtype is not None and t.dtype != dtype):
             _need(False, "%s: a gradient must have its tensor's shape and type" % what)
-        strides.append(0 if t is None else _flat(what, t)[1])
+        strides.append(shape[-1] if t.is_contiguous() else _flat(what, t)[1])
     g = BlockGrads(_ptr(dh), _ptr(dy), _ptr(dx), _ptr(dblock), *(_ptr(t) for t in grads), _ptr(dgate), *strides, dgate_stride, 1 if accumulate else 0)
     need = ctypes.c_size_t()
     _check(L, L.mist_block_workspace(ctypes.byref(d), ctypes.byref(g), ctypes.byref(need)))
@@ -1403,19 +1414,19 @@ class Checkpoint:
         if not (len(self.shape) >= 1 and self.shape[-1] >= 1 and min(self.shape) >= 0):
             _need(False, "checkpoint: the last dimension must be at least 1")
         self.rows, self.width = math.prod(self.shape[:-1]), self.shape[-1]
-        groups = -(-self.width // KEPT_GROUP)
+        groups = self.groups = -(-self.width // KEPT_GROUP)
         with _pool(torch, stream):
             self.values = torch.empty(self.rows, groups * KEPT_GROUP, dtype=torch.int8, device=device)
             self.exponents = torch.empty(self.rows, groups, dtype=torch.uint8, device=device)
 
     def kept(self, what, device) -> Kept:
         torch = _torch()
-        groups = -(-self.width // KEPT_GROUP)
-        if not (self.values.device == device and self.exponents.device == device):
+        values, exponents = self.values, self.exponents
+        if not (values.device == device and exponents.device == device):
             _need(False, "%s: the tensors must be on one GPU" % what)
-        _packed(what, self.values, (self.rows, groups * KEPT_GROUP), torch.int8, "a checkpoint's values")
-        _packed(what, self.exponents, (self.rows, groups), torch.uint8, "a checkpoint's exponents")
-        return Kept(self.values.data_ptr(), self.exponents.data_ptr())
+        _packed(what, values, (self.rows, self.groups * KEPT_GROUP), torch.int8, "a checkpoint's values")
+        _packed(what, exponents, (self.rows, self.groups), torch.uint8, "a checkpoint's exponents")
+        return Kept(values.data_ptr(), exponents.data_ptr())
 
 
 def _checkpoint_for(what, t, given, other) -> Checkpoint:
@@ -1487,7 +1498,7 @@ def mlp_act(up, gate=None, *, kind: str = "silu", save=False, out=None, stream=N
         _need(False, "activation: gate must have up's shape and type")
     if out is None:
         with _pool(torch, other):
-            out = torch.empty(up.shape, dtype=up.dtype, device=up.device)
+            out = _like(torch, up)
     if not (out.shape == up.shape and out.dtype == up.dtype):
         _need(False, "activation: out must have up's shape and type")
     keep = (None, None)
@@ -1523,9 +1534,9 @@ def mlp_act_grad(dout, up: Checkpoint, gate: Checkpoint | None = None, *, kind: 
     handle, other = _stream_of(torch, stream, dout.device)
     with _pool(torch, other):
         if dup is None:
-            dup = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+            dup = _like(torch, dout)
         if gate is not None and dgate is None:
-            dgate = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+            dgate = _like(torch, dout)
     for t in (dup, dgate, out):
         if not (t is None or (t.shape == dout.shape and t.dtype == dout.dtype)):
             _need(False, "%s: an output must have dout's shape and type" % what)
