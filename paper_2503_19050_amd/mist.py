@@ -1079,36 +1079,42 @@ def _packed(what, t, shape, dtype, name):
     return t
 
 
+def _targets(what, targets, shape) -> tuple[int, int]:
+    """(stride between sequences, bytes of an id) of targets for tokens of this shape."""
+    if targets is None:
+        return 0, 8
+    id_bytes, dtype = targets.element_size(), targets.dtype
+    if not (id_bytes in (4, 8) and not dtype.is_floating_point and not dtype.is_complex and dtype.is_signed):
+        _need(False, "%s: targets must be int32 or int64" % what)
+    if targets.shape != shape:
+        _need(False, "%s: targets must have the logits' shape but for the last dimension" % what)
+    strides = targets.stride()
+    if not (shape[-1] <= 1 or strides[-1] == 1):
+        _need(False, "%s: the targets of a sequence must be contiguous" % what)
+    return strides[0] if len(shape) == 2 else 0, id_bytes
+
+
 def _token_desc(torch, logits, targets, grad, vocab_begin, scale, top) -> TokenDesc:
     what = "token log probabilities"
     _here(what, logits, targets, grad)
-    lshape = logits.shape
-    shape = lshape[:-1]
-    if not (len(lshape) in (2, 3)):
+    shape, lst = logits.shape, logits.stride()
+    dims, rows = len(shape), shape[-1] if len(shape) else 0
+    if dims != 3 and dims != 2:
         _need(False, "%s: the logits must be [seq, rows] or [batch, seq, rows]" % what)
-    two = len(lshape) == 3
-    ist, id_bytes = 0, 8
-    if targets is not None:
-        id_bytes = targets.element_size()
-        if not (id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed):
-            _need(False, "%s: targets must be int32 or int64" % what)
-        if not (targets.shape == shape):
-            _need(False, "%s: targets must have the logits' shape but for the last dimension" % what)
-        if not (shape[-1] <= 1 or targets.stride(-1) == 1):
-            _need(False, "%s: the targets of a sequence must be contiguous" % what)
-        ist = targets.stride(0) if two else 0
-    lst = logits.stride()
-    if not (lshape[-1] <= 1 or lst[-1] == 1 or logits.numel() == 0):
+    ist, id_bytes = _targets(what, targets, shape[:-1])
+    if not (rows <= 1 or lst[-1] == 1 or logits.numel() == 0):
         _need(False, "%s: the last dimension must be contiguous" % what)
     gst = lst
     if grad is not None:
-        if not (grad.shape == lshape and grad.dtype == logits.dtype):
+        if not (grad.shape == shape and grad.dtype == logits.dtype):
             _need(False, "%s: the gradient must have the logits' shape and type" % what)
         gst = grad.stride()
-        if not (lshape[-1] <= 1 or gst[-1] == 1 or logits.numel() == 0):
+        if not (rows <= 1 or gst[-1] == 1 or logits.numel() == 0):
             _need(False, "%s: the last dimension must be contiguous" % what)
-    return TokenDesc(lshape[0] if two else 1, lshape[-2], lshape[-1], int(vocab_begin), ist, lst[0] if two else 0, lst[-2], gst[0] if two else 0,
-                     gst[-2], id_bytes, _type(logits, what), int(top), float(scale))
+    code = _type(logits, what)
+    if dims == 3:
+        return TokenDesc(shape[0], shape[1], rows, vocab_begin, ist, lst[0], lst[1], gst[0], gst[1], id_bytes, code, top, scale)
+    return TokenDesc(1, shape[0], rows, vocab_begin, ist, 0, lst[0], 0, gst[0], id_bytes, code, top, scale)
 
 
 def _top_space(torch, shape, top, device):
@@ -1182,16 +1188,7 @@ def token_join(stats, targets=None, *, entropy: bool = False, top_ids=None, top_
         top = top_ids.shape[-1]
         _packed(what, top_ids, (ranks,) + shape + (top,), torch.int32, "top_ids")
         _packed(what, top_z, (ranks,) + shape + (top,), torch.float32, "top_z")
-    ist, id_bytes = 0, 8
-    if targets is not None:
-        id_bytes = targets.element_size()
-        if not (id_bytes in (4, 8) and not targets.dtype.is_floating_point and not targets.dtype.is_complex and targets.dtype.is_signed):
-            _need(False, "%s: targets must be int32 or int64" % what)
-        if not (tuple(targets.shape) == shape):
-            _need(False, "%s: targets must have the tokens' shape" % what)
-        if not (shape[-1] <= 1 or targets.stride(-1) == 1):
-            _need(False, "%s: the targets of a sequence must be contiguous" % what)
-        ist = targets.stride(0) if len(shape) == 2 else 0
+    ist, id_bytes = _targets(what, targets, shape)
     d = TokenDesc(shape[0] if len(shape) == 2 else 1, shape[-1], 1, 0, ist, 0, 0, 0, 0, id_bytes, 0, top, 1.0)
     handle, other = _stream_of(torch, stream, device)
     with _pool(torch, other):
@@ -1429,12 +1426,21 @@ class Checkpoint:
         return Kept(values.data_ptr(), exponents.data_ptr())
 
 
-def _checkpoint_for(what, t, given, other) -> Checkpoint:
-    if given is None:
-        return Checkpoint(t.shape, t.dtype, t.device, other)
-    if not (isinstance(given, Checkpoint) and given.shape == tuple(t.shape) and given.dtype == t.dtype):
-        _need(False, "%s: a checkpoint of another shape or type" % what)
-    return given
+def _checkpoint_for(torch, what, t, given, other) -> Checkpoint:
+    if given is not None:
+        if not (isinstance(given, Checkpoint) and given.shape == t.shape and given.dtype == t.dtype):
+            _need(False, "%s: a checkpoint of another shape or type" % what)
+        return given
+    if t.dtype not in _TYPES or not t.dim() or not t.shape[-1]:
+        return Checkpoint(t.shape, t.dtype, t.device, other)  # says what is wrong
+    c = Checkpoint.__new__(Checkpoint)
+    c.shape, c.dtype, device = tuple(t.shape), t.dtype, t.device
+    c.width = c.shape[-1]
+    c.rows, c.groups = t.numel() // c.width, -(-c.width // KEPT_GROUP)
+    with _pool(torch, other):
+        c.values = torch.empty((c.rows, c.groups * KEPT_GROUP), dtype=torch.int8, device=device)
+        c.exponents = torch.empty((c.rows, c.groups), dtype=torch.uint8, device=device)
+    return c
 
 
 def checkpoint_store(x, checkpoint: Checkpoint | None = None, *, stream=None) -> Checkpoint:
@@ -1447,7 +1453,7 @@ def checkpoint_store(x, checkpoint: Checkpoint | None = None, *, stream=None) ->
     _here(what, x)
     handle, other = _stream_of(torch, stream, x.device)
     rows, stride = _flat(what, x)
-    c = _checkpoint_for(what, x, checkpoint, other)
+    c = _checkpoint_for(torch, what, x, checkpoint, other)
     k = c.kept(what, x.device)
     d = KeptDesc(rows, c.width, stride, _type(x, what))
     _on_device(torch, x.device, L.mist_kept_store, ctypes.byref(d), x.data_ptr(), k.values, k.exponents, handle)
@@ -1506,7 +1512,7 @@ def mlp_act(up, gate=None, *, kind: str = "silu", save=False, out=None, stream=N
         pair = (None, None) if save is True else save
         if not (len(pair) == 2):
             _need(False, "activation: save must be a bool or (up's checkpoint, gate's or None)")
-        keep = (_checkpoint_for(what, up, pair[0], other), None if gate is None else _checkpoint_for(what, gate, pair[1], other))
+        keep = (_checkpoint_for(torch, what, up, pair[0], other), None if gate is None else _checkpoint_for(torch, what, gate, pair[1], other))
     rows, stride = _flat(what, up)
     d = ActDesc(rows, up.shape[-1], stride, 0 if gate is None else _flat(what, gate)[1], _flat(what, out)[1], 0, _type(up, what), _ACTS[kind])
     k = [None if c is None else ctypes.byref(c.kept(what, up.device)) for c in keep]

@@ -55,7 +55,7 @@ def reference(torch, model, p, x, targets, weight, kept):
     logp = torch.log_softmax(z, -1).gather(-1, targets.clamp(min=0)[..., None])[..., 0]
     logp = torch.where(targets >= 0, logp, 0.0)
     (-weight * logp.sum()).backward()
-    return logp, dict({k: v.grad for k, v in q.items()}, x=x.grad)
+    return logp.detach(), dict({k: v.grad for k, v in q.items()}, x=x.grad)
 
 
 @pytest.mark.parametrize("name", ["tiny", "tiny_llama"])
