@@ -358,8 +358,8 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
   Join<THREADS / 64> join{part, 0};
   for (int32_t t = blockIdx.x; t < a.n; t += gridDim.x) {
     const T* x = logits + logits_offset(a, t);
-    const int64_t target = targets ? target_of(a, targets, t) : -1, at = target - a.vocab_begin;
-    const bool here = target >= 0 && at >= 0 && at < a.rows;
+    const int64_t target = targets ? target_of(a, targets, t) : -1, at = target < 0 ? -1 : target - a.vocab_begin;
+    const bool here = at >= 0 && at < a.rows;
     const float xt = here ? (float)x[at] : -HUGE_VALF;
     Stats r{-HUGE_VALF, 0.0f, 0.0f, here ? xt * a.scale : -HUGE_VALF};
     if constexpr (MODE == kTop) {
@@ -516,9 +516,9 @@ __global__ __launch_bounds__(kThreads) void k_grad(TokenArgs a, int32_t slabs, c
     const int32_t t = (int32_t)(i / slabs);
     const int64_t base = i % slabs * C::kAll;
     const int n = (int)min((int64_t)C::kAll, a.rows - base);
-    const int64_t target = dlogp ? target_of(a, targets, t) : -1, at = target - a.vocab_begin - base;
+    const int64_t target = dlogp ? target_of(a, targets, t) : -1, at = target < 0 ? -1 : target - a.vocab_begin - base;
     const Slope g = slope_of(lse[t], a.scale, target >= 0 ? dlogp[t] : 0.0f, dentropy ? dentropy[t] : 0.0f, dentropy ? entropy[t] : 0.0f);
-    const bool zero = flat(g), here = target >= 0 && at >= 0 && at < n;
+    const bool zero = flat(g), here = at >= 0 && at < n;
     const T* x = logits + logits_offset(a, t) + base;
     T* y = dlogits + grad_offset(a, t) + base;
     C c;

@@ -295,6 +295,9 @@ def test_targets_of_no_one(torch):
     logits, t = inputs(torch, 1, 3, 50, "f32", "text")
     t[0, 1] = 50
     t[0, 2] = 2 ** 40
+    far = torch.tensor([[-2 ** 63, 2 ** 63 - 1, 2 ** 32]], device="cuda")   # padding, and of no one
+    assert mist.token_logprob(logits, far).logp.tolist() == [[0.0, -math.inf, -math.inf]]
+    assert not mist.token_grad(logits, far, mist.token_logprob(logits).lse, dlogp=torch.ones(1, 3, device="cuda"))[0, 0].any()
     logp, d = mist.token_loss(logits, t, 1.0)
     assert logp[0, 0].isfinite() and (logp[0, 1:] == -math.inf).all()
     assert abs(float(d[0, 0].sum())) < 1e-5 and abs(float(d[0, 1].sum()) - 1) < 1e-5
