@@ -374,6 +374,32 @@ def test_large_offsets(torch):
     assert torch.equal(logp[:, at], logp2) and torch.equal(d[:, at], d2)
 
 
+def test_more_tokens_than_blocks(torch):
+    """Blocks that take a second row (from 2^20 tokens on), and waves that join a second token: the same bits as in small calls."""
+    from paper_2503_19050_amd import mist
+    n, rows = (1 << 20) + 77, 104   # rows of whole vectors: every row is aligned alike
+    x, t = inputs(torch, 1, n, rows, "bf16", "masked")
+    w = torch.rand(1, n, device="cuda")
+    at = [slice(0, 100), slice((1 << 20) - 60, n)]
+    r = mist.token_logprob(x, t, entropy=True, top=5)
+    logp, d = mist.token_loss(x, t, w)
+    g = mist.token_grad(x, t, r.lse, dlogp=w, entropy=r.entropy, dentropy=w)
+    for k in at:
+        xs, ts, ws = x[:, k].contiguous(), t[:, k].contiguous(), w[:, k].contiguous()
+        want = mist.token_logprob(xs, ts, entropy=True, top=5)
+        assert all(torch.equal(a[:, k], b) for a, b in zip(r, want))
+        logps, ds = mist.token_loss(xs, ts, ws)
+        assert torch.equal(logp[:, k], logps) and torch.equal(d[:, k], ds)
+        assert torch.equal(g[:, k], mist.token_grad(xs, ts, want.lse, dlogp=ws, entropy=want.entropy, dentropy=ws))
+    n = (1 << 24) + 55
+    stats = torch.rand(1, n, 4, device="cuda") + 0.5
+    t = torch.zeros(n, device="cuda", dtype=torch.int32)
+    r = mist.token_join(stats, t, entropy=True)
+    for k in (slice(0, 100), slice((1 << 24) - 40, n)):
+        want = mist.token_join(stats[:, k].contiguous(), t[k], entropy=True)
+        assert torch.equal(r.lse[k], want.lse) and torch.equal(r.logp[k], want.logp) and torch.equal(r.entropy[k], want.entropy)
+
+
 def test_streams_and_graphs(torch):
     """A run of the operators on another stream, and captured: replays with new inputs and eager work between give the eager results."""
     from paper_2503_19050_amd import mist
