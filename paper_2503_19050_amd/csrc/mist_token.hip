@@ -140,11 +140,10 @@ struct Chunk {
     asm("" : "+v"(at));  // formed anew where it is used, rather than N of them held
     return head + (j * THREADS + at) * kV;
   }
+  __device__ __forceinline__ int tail() const { return n - (n - head) % kV; }  // past the last vector
   // of the odd value; n or more: none
   __device__ __forceinline__ int odd_place() const { return odd_place((int)threadIdx.x); }
-  __device__ __forceinline__ int odd_place(int t) const {
-    return t < head ? t : n - (n - head) % kV + t - head;
-  }
+  __device__ __forceinline__ int odd_place(int t) const { return t < head ? t : tail() + t - head; }
   __device__ __forceinline__ bool any(int j) const { return head + (j * THREADS + 1) * kV <= n; }  // the j-th vector of some thread
   __device__ __forceinline__ void load(const T* x, int count, bool read = true) {
     n = count;
@@ -207,8 +206,8 @@ struct Chunk {
   }
   // whether this thread holds a place
   __device__ __forceinline__ bool mine(int at) const {
-    const int tail = n - (n - head) % kV, t = threadIdx.x;
-    return at < head ? at == t : at >= tail ? at - tail + head == t : (at - head) / kV % THREADS == t;
+    const int t = threadIdx.x;
+    return at < head ? at == t : at >= tail() ? at - tail() + head == t : (at - head) / kV % THREADS == t;
   }
 };
 
@@ -257,14 +256,15 @@ __device__ __forceinline__ void list_groups(const C& c, const float (&group)[8],
     if (nan || group[i] >= bound) add_group(t, i);
   if (!(c.odd < bound)) add_group(t, 8);
 }
-// The listed groups' values from bound on with keys above least join the candidates.  Between two barriers.
+// The listed groups' values from bound on with keys above least join the candidates, each once: a group's places past the last
+// vector are others' odd values.  Between two barriers.
 template <int THREADS, class C, class T>
 __device__ __forceinline__ void list_candidates(const C& c, const T* x, uint32_t base, float bound, uint64_t least, Top& t) {
   for (int i = threadIdx.x; i < min(t.groups, kCandidates) * C::kGroup; i += THREADS) {
     const uint32_t g = t.group[i / C::kGroup];
     const int k = i % C::kGroup, thread = (int)(g & 0xFFFF), which = (int)(g >> 16);
     const int at = which < 8 ? c.group_place(which, thread, k) : c.odd_place(thread) + (k ? c.n : 0);
-    const float v = at < c.n ? (float)x[at] : -HUGE_VALF;
+    const float v = at < (which < 8 ? c.tail() : c.n) ? (float)x[at] : -HUGE_VALF;
     if (v < bound) continue;
     const uint64_t key = key_of(rank_of(v), base + (uint32_t)at);
     if (key <= least) continue;

@@ -1,0 +1,53 @@
+"""Cases of the token operators beyond the grids of test_gpu_token.py, against the same definition and with its tolerances."""
+import math
+import sys
+
+import pytest
+
+from test_gpu_token import Truth, alternatives, types, within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "a GPU is required"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+@pytest.mark.parametrize("kind, rows", [("bf16", 37001), ("bf16", 57349), ("f16", 45071), ("bf16", 70013), ("f16", 131079), ("f32", 18501), ("f32", 28675),
+                                        ("f32", 33003), ("bf16", 4003), ("bf16", 20013), ("f32", 1001), ("f32", 9999)])
+def test_alternatives_at_the_end_of_a_row(torch, kind, rows):
+    """The last values of a row, or of its first chunk, that fill no whole vector, and values that the thread behind them looks through,
+    are alternatives together, each once; also where that thread has a NaN."""
+    from paper_2503_19050_amd import mist
+    per = 4 if kind == "f32" else 8   # of a vector
+    chunk = 512 * 16 * per
+    for off in (0, 1, per - 1):   # of the row from a multiple of 16 bytes
+        for nan in (0, 64, 256, 512):
+            say("end of a row", kind, rows, off, nan)
+            g = torch.Generator("cuda").manual_seed(rows + off)
+            room = torch.empty(1, 3, rows + (-rows) % per + per, device="cuda").normal_(0.0, 1.0, generator=g).to(types(torch)[kind])
+            x = room[..., off:off + rows]
+            head = (-off) % per
+            for n in {rows, min(rows, chunk)}:
+                tail = n - (n - head) % per
+                x[..., tail:n] = torch.arange(40, 40 - (n - tail), -1, device="cuda", dtype=x.dtype)
+                back = tail - 512 * per
+                if back >= 0:
+                    x[..., back:back + per] = torch.arange(20, 20 - per, -1, device="cuda", dtype=x.dtype)
+                if nan and tail - nan * per >= 0:
+                    x[:, 1, tail - nan * per + 1] = math.nan
+            x[..., 5] = 9
+            for top in (1, 2, 3, 12, 40):
+                r = mist.token_logprob(x, top=top)
+                ids = alternatives(torch, x, top)
+                assert torch.equal(r.top_ids.reshape(ids.shape), ids), (off, nan, top)
+                p = mist.token_part(x, torch.zeros(1, 3, device="cuda", dtype=torch.int64), vocab_begin=7, top=top)
+                assert torch.equal(p.top_ids.reshape(ids.shape), ids + 7), (off, nan, top)
