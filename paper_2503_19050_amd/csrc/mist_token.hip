@@ -385,7 +385,7 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
       if (base) {
         const float d = r.m == -HUGE_VALF ? 0.0f : r.m - from, f = fast_exp(d);  // where nothing was visible s and u are 0
-        u = f * fmaf(d, s, u);
+        u = f * fmaf(fmaxf(d, kLow), s, u);  // d may be near fp32's end, and f 0
         s *= f;
       }
       r.m = m;

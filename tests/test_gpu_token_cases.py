@@ -51,3 +51,34 @@ def test_alternatives_at_the_end_of_a_row(torch, kind, rows):
                 assert torch.equal(r.top_ids.reshape(ids.shape), ids), (off, nan, top)
                 p = mist.token_part(x, torch.zeros(1, 3, device="cuda", dtype=torch.int64), vocab_begin=7, top=top)
                 assert torch.equal(p.top_ids.reshape(ids.shape), ids + 7), (off, nan, top)
+
+
+@pytest.mark.parametrize("kind, chunk", [("bf16", 65536), ("f16", 65536), ("f32", 32768)])
+@pytest.mark.parametrize("more", [1, 4000, 70003])
+def test_chunks_of_the_lowest_value(torch, kind, chunk, more):
+    """Every value of a first chunk at the type's lowest, as masks have it, ordinary ones after it."""
+    from paper_2503_19050_amd import mist
+    say("lowest chunk", kind, chunk, more)
+    rows = chunk + more
+    g = torch.Generator("cuda").manual_seed(rows)
+    x = torch.empty(1, 4, rows, device="cuda").normal_(0.0, 2.0, generator=g).to(types(torch)[kind])
+    x[..., :chunk] = torch.finfo(x.dtype).min
+    x[0, 1, 3] = 1.0
+    x[0, 2, chunk:-1] = torch.finfo(x.dtype).min
+    t = torch.tensor([[rows - 1, 3, rows - 1, -1]], device="cuda")
+    for scale in (1.0, 0.5):   # products of the lowest value that are exact
+        w = Truth(torch, x, t, scale)
+        r = mist.token_logprob(x, t, scale=scale, entropy=True, top=3)
+        part = mist.token_part(x, t, vocab_begin=0, scale=scale)
+        for got in (r, mist.token_join(part.stats[None], t, entropy=True)):
+            within(got.lse, w.lse, w.e_lse, "lse")
+            within(got.logp, w.logp, w.e_logp, "logp")
+            within(got.entropy, w.entropy, w.e_entropy, "entropy")
+        d = torch.tensor([[1.0, -1.0, 0.5, 2.0]], device="cuda")
+        got = mist.token_grad(x, t, r.lse, dlogp=d, entropy=r.entropy, dentropy=-d, scale=scale)
+        want, slack = w.grad(torch, d, -d, scale, kind)
+        within(got, want, slack, "gradient")
+        logp, got = mist.token_loss(x, t, -d, scale=scale)
+        want, slack = w.grad(torch, d, torch.zeros_like(d), scale, kind)
+        within(logp, w.logp, w.e_logp, "logp")
+        within(got, want, slack, "loss")
