@@ -676,7 +676,8 @@ mist_status mist_token_join(const mist_token_desc* d, int32_t ranks, const float
 
 /* The logits' gradient from the log probabilities' (dlogp, NULL: zero) and the entropies' (dentropy, NULL: zero; then
  * entropy may be NULL too), with lse and entropy of the whole vocabulary: dlogits[j] = scale * (dlogp ([j = target] -
- * p[j]) - dentropy p[j] (log p[j] + entropy)).  dlogits may be the logits (with their strides).
+ * p[j]) - dentropy p[j] (log p[j] + entropy)), p[j] = exp(z[j] - lse): the rounding of the given lse, up to 2^-24 |lse|, is a relative error
+ * of every p (mist_token_loss has none of it).  dlogits may be the logits (with their strides).
  * Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_token_grad(const mist_token_desc* d, const void* logits, const void* targets, const float* lse, const float* dlogp,
                             const float* entropy, const float* dentropy, void* dlogits, void* hip_stream);

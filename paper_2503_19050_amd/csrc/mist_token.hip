@@ -1,7 +1,8 @@
 // Token log probabilities, entropies and alternatives, their gradient, and the loss of a training microbatch.
 //
-// z = scale * logits is never stored: z - m is one fused multiply-add.  A row's largest logit comes first, so that every
-// exponential is at most 1 and a row needs no rescaling.  A row stays in the registers of its block from its one reading to the
+// z = scale * logits is never stored.  A row's largest logit comes first, and exponentials are of the scaled distance from it, not of a
+// difference of scaled values: the distance is exact for 16-bit logits and never above 0, so that every exponential is at most 1, however large
+// the logits are (a fused product less a rounded largest one is off by up to half a step of that: past any exponential from 2^31 on).  A row stays in the registers of its block from its one reading to the
 // last pass over it (of 16-bit values up to 65536, of fp32 32768; longer ones by chunks, whose sums are rescaled); the loss writes the
 // gradient from there.  Measured on one MI355X, where a large copy reads and writes 4.9 TB/s:
 //   loss        32768 x 50257 bf16  1310 us, 5.0 TB/s: memory
@@ -35,7 +36,7 @@ struct TokenArgs {
   int64_t rows, vocab_begin, ids_stride, logits_batch_stride, logits_stride, grad_batch_stride, grad_stride;
   uint32_t seq;  // at least 1
   int32_t n, ids_bytes, top;  // n: tokens
-  float scale;
+  float scale, pre, rest;  // log2(e) scale = pre * rest, with pre a power of two: 1 unless a scale is past 2^64 either way
 };
 
 __device__ __forceinline__ int64_t offset_of(const TokenArgs& a, int32_t t, int64_t batch_stride, int64_t stride) {
@@ -324,8 +325,16 @@ __device__ __forceinline__ void take_top(const T* x, int n, uint32_t base, int t
   }
 }
 
+// The exponent of 2 of exp(z - max z): the distance from the largest logit, times log2(e) scale.  from: pre times that logit; 0 where
+// nothing is visible (the exponentials are 0, of -inf, not NaN), +inf where the largest z is: all of the row becomes NaN.
+__device__ __forceinline__ float start_of(const TokenArgs& a, float most) {
+  const float m = most * a.scale;
+  return m == -HUGE_VALF ? 0.0f : m == HUGE_VALF ? m : most * a.pre;
+}
+__device__ __forceinline__ float below(const TokenArgs& a, float x, float from) { return fmaf(x, a.pre, -from) * a.rest; }
+
 // A row's gradient, p (c0 + c1 log p) + [j = target] up with scale in the factors.  One without factors is zeros, whatever the
-// logits are: they are not looked at.
+// logits are: they are not looked at.  z is rounded before lse, which is none below it, is subtracted: p is at most 1.
 struct Slope {
   float lse, c0, c1, up;
 };
@@ -335,7 +344,7 @@ __device__ __forceinline__ Slope slope_of(float lse, float scale, float dlogp, f
   return Slope{lse, scale * (dentropy != 0.0f ? -dlogp - dentropy * entropy : -dlogp), scale * -dentropy, scale * dlogp};
 }
 __device__ __forceinline__ float slope_at(const Slope& g, float x, float scale) {
-  const float l = fmaf(x, scale, -g.lse), p = fast_exp(l);
+  const float z = x * scale, l = z - g.lse, p = fast_exp(l);
   return p * fmaf(g.c1, fmaxf(l, kLow), g.c0);
 }
 
@@ -372,7 +381,8 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       if (THREADS == 64) __syncthreads();  // larger blocks meet in their joins
     }
     C c;
-    float s = 0.0f, u = 0.0f, bound = 0.0f;
+    float s = 0.0f, u = 0.0f, bound = 0.0f;  // u: in units of log(2)
+    float most = -HUGE_VALF, from = 0.0f;
     for (int64_t base = 0; base < a.rows; base += C::kAll) {
       const int n = (int)min((int64_t)C::kAll, a.rows - base);
       c.load(x + base, n);
@@ -381,16 +391,17 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       float2 w = {wave_max(low), 0.0f};
       if (MODE == kTop) w.y = wave_bound(low, (a.top + THREADS / 64 - 1) / (THREADS / 64));
       w = join.most_and_least(w);
-      const float m = fmaxf(r.m, w.x * a.scale);
-      const float from = m == -HUGE_VALF ? 0.0f : m;  // nothing is visible: exponentials of -inf, not of NaN
+      const float start = start_of(a, fmaxf(most, w.x));
       if (base) {
-        const float d = r.m == -HUGE_VALF ? 0.0f : r.m - from, f = fast_exp(d);  // where nothing was visible s and u are 0
+        // where nothing was visible s and u are 0
+        const float d = most * a.scale == -HUGE_VALF ? 0.0f : (from - start) * a.rest, f = __builtin_amdgcn_exp2f(d);
         u = f * fmaf(fmaxf(d, kLow), s, u);  // d may be near fp32's end, and f 0
         s *= f;
       }
-      r.m = m;
+      most = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(fmaxf(most, w.x))));  // the block's, in a scalar register
+      from = start;
       c.each([&](float v) {
-        const float d = fmaf(v, a.scale, -from), e = fast_exp(d);
+        const float d = below(a, v, from), e = __builtin_amdgcn_exp2f(d);
         s += e;
         if (MODE != kLoss) u = fmaf(e, fmaxf(d, kLow), u);  // a NaN comes with e
       });
@@ -413,7 +424,7 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       }
     }
     const float2 su = join.sum(s, u);
-    r.s = su.x, r.u = su.y;
+    r.m = most * a.scale, r.s = su.x, r.u = su.y * 0.693147180559945309f;
     const float l = lse_of(r);
     if (threadIdx.x == 0) {
       if (MODE == kLoss) {
@@ -427,17 +438,19 @@ __global__ __launch_bounds__(THREADS, N == 8 ? MODE == kTop ? 5 : 8 : 4) void k_
       }
     }
     if constexpr (MODE == kLoss) {
+      // the exponentials over their sum: no rounding of lse comes into p
       const Slope g = slope_of(l, a.scale, target < 0 ? 0.0f : -(o.weights ? o.weight * o.weights[t] : o.weight), 0.0f, 0.0f);
       const bool zero = flat(g);
+      const float share = g.c0 / r.s;
       T* y = dlogits + grad_offset(a, t);
       // the last chunk is still here; the others are read again
       const int64_t final = (a.rows - 1) / C::kAll * C::kAll;
       for (int64_t base = final; base >= 0; base -= C::kAll) {
         const int n = (int)min((int64_t)C::kAll, a.rows - base);
         if (base != final) c.load(x + base, n);
-        c.store(y + base, [&](float v) { return zero ? 0.0f : slope_at(g, v, a.scale); });
+        c.store(y + base, [&](float v) { return zero ? 0.0f : __builtin_amdgcn_exp2f(below(a, v, from)) * share; });
         const int64_t k = at - base;
-        if (here && k >= 0 && k < n && c.mine((int)k)) y[at] = (T)(zero ? 0.0f : slope_at(g, xt, a.scale) + g.up);
+        if (here && k >= 0 && k < n && c.mine((int)k)) y[at] = (T)(zero ? 0.0f : fmaf(__builtin_amdgcn_exp2f(below(a, xt, from)), share, g.up));
       }
     } else if constexpr (MODE == kTop) {
       if (THREADS == 64) __syncthreads();  // else the sums' join was the barrier after the last group
@@ -583,8 +596,10 @@ mist_status check_grad(const mist_token_desc* d, const void* logits, const void*
 }
 
 TokenArgs args(const mist_token_desc* d) {
+  const float pre = d->scale > 0x1p64f ? 0x1p64f : d->scale < 0x1p-64f ? 0x1p-64f : 1.0f;
   return TokenArgs{d->rows, d->vocab_begin, d->ids_stride, d->logits_batch_stride, d->logits_stride,
-                   d->grad_batch_stride, d->grad_stride, (uint32_t)std::max<int64_t>(d->seq, 1), (int32_t)(d->batch * d->seq), d->ids_bytes, d->top, d->scale};
+                   d->grad_batch_stride, d->grad_stride, (uint32_t)std::max<int64_t>(d->seq, 1), (int32_t)(d->batch * d->seq), d->ids_bytes, d->top, d->scale,
+                   pre, (float)(1.44269504088896341 * d->scale / pre)};
 }
 
 bool floats_ok(std::initializer_list<const float*> ps) {

@@ -66,7 +66,7 @@ def test_chunks_of_the_lowest_value(torch, kind, chunk, more):
     x[0, 1, 3] = 1.0
     x[0, 2, chunk:-1] = torch.finfo(x.dtype).min
     t = torch.tensor([[rows - 1, 3, rows - 1, -1]], device="cuda")
-    for scale in (1.0, 0.5):   # products of the lowest value that are exact
+    for scale in (1.0, 0.75):
         w = Truth(torch, x, t, scale)
         r = mist.token_logprob(x, t, scale=scale, entropy=True, top=3)
         part = mist.token_part(x, t, vocab_begin=0, scale=scale)
@@ -82,3 +82,49 @@ def test_chunks_of_the_lowest_value(torch, kind, chunk, more):
         want, slack = w.grad(torch, d, torch.zeros_like(d), scale, kind)
         within(logp, w.logp, w.e_logp, "logp")
         within(got, want, slack, "loss")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows", [9, 5000, 50257, 70000])
+@pytest.mark.parametrize("scale", [0.75, 0.9, 1.0 / 3.0, 1.25, 2.0 ** -70, 3e-39, 1e30])
+def test_scaled_values_of_any_size(torch, kind, rows, scale):
+    """Rows of one value, whatever its size and the scale, are uniform: entropy log n, a gradient of weight / n, and log
+    probabilities that are none above 0.  Beside the largest value others have none."""
+    from paper_2503_19050_amd import mist
+    say("sizes", kind, rows, scale)
+    T = types(torch)[kind]
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    top, tiny = float(torch.finfo(torch.float32).max), 2.0 ** -100
+    values = [v for v in (float(torch.finfo(T).min), -1.23e10, -7e8, -3.3, 0.0, 1.7, 1e5, 3.1e37) if abs(v) <= float(torch.finfo(T).max)]
+    x = torch.tensor(values, device="cuda", dtype=T)[None, :, None].expand(1, len(values), rows).contiguous()
+    z = x[0, :, 0].double() * scale
+    t = torch.full((1, len(values)), rows - 1, device="cuda")
+    r = mist.token_logprob(x, t, scale=scale, entropy=True, top=2)
+    logp, d = mist.token_loss(x, t, 0.5, scale=scale)
+    grad = mist.token_grad(x, t, r.lse, dlogp=torch.ones(1, len(values), device="cuda"), entropy=r.entropy, dentropy=torch.ones(1, len(values), device="cuda"), scale=scale)
+    for k, v in enumerate(z.tolist()):
+        if v < -top:      # masked out
+            assert r.lse[0, k] == -math.inf and r.entropy[0, k] == 0 and r.logp[0, k] == -math.inf and not d[0, k].any() and not grad[0, k].any(), v
+            continue
+        if v > top:
+            assert r.lse[0, k].isnan() and r.logp[0, k].isnan() and r.entropy[0, k].isnan() and d[0, k].isnan().all(), v
+            continue
+        # a sum of ones is exact below 2^24; the logarithm, at most 11.2, is off by two of its ulps of 2^-20
+        assert abs(float(r.entropy[0, k]) - math.log(rows)) <= 2.0 ** -19, v
+        assert abs(float(r.lse[0, k]) - v) <= math.log(rows) + 2.0 ** -22 * (abs(v) + 20), v
+        assert -math.log(rows) - 2.0 ** -22 * (abs(v) + 20) <= float(r.logp[0, k]) <= 0.0 and r.logp[0, k] == logp[0, k], v
+        assert r.top_ids[0, k].tolist() == [0, 1] and bool((r.top_logp[0, k] == r.logp[0, k]).all()), v
+        if 4 * scale * (1 + math.log(rows)) > float(torch.finfo(T).max):   # the gradient's own factors pass the type
+            continue
+        p = d[0, k].double() / (0.5 * scale)
+        # of p c0: roundings of p (2^-22 of it), of the factor and of the output
+        unit = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}[kind] + 2.0 ** -21
+        small = {"bf16": 2.0 ** -133, "f16": 2.0 ** -24, "f32": 2.0 ** -148}[kind] / (0.5 * scale)
+        assert bool(((p[:-1] - 1 / rows).abs() <= unit / rows + small).all()) and abs(float(p[-1]) - 1 / rows + 1) <= unit + small, v
+        assert bool(grad[0, k].isfinite().all()), v
+    y = x.clone()
+    y[..., 0] = torch.where(x[..., 0] < 0, x[..., 0] / 2, x[..., 0] * 2 + 1)
+    far = (y[0, :, 0].double() - x[0, :, 0].double()) * scale > 200
+    r = mist.token_logprob(y, torch.zeros_like(t), scale=scale, entropy=True)
+    one = far & (y[0, :, 0].double() * scale <= top) & (y[0, :, 0].double() * scale >= -top)
+    assert bool((r.logp[0][one] == 0).all()) and bool((r.entropy[0][one].abs() < tiny).all())
