@@ -1363,6 +1363,10 @@ def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post
             dx = _like(torch, y)
         if block is not None and dblock is None:
             dblock = _like(torch, block)
+    shared = gate
+    if gate is not None and dgate is not None and gate.dim() == 2 and gate.shape[0] > 1 and gate.stride(0) == 0:
+        with _pool(torch, other):  # rows of one place: their gradients are still a row for each sequence
+            gate = gate.contiguous()
     d = _block_desc(what, y, block, y, dh, weight, None, post_weight, post_bias, gate, kind, 0.0, res_scale, block_scale)
     first = weight if weight is not None else post_weight if post_weight is not None else gate
     wtype = y.dtype if first is None else first.dtype
@@ -1392,7 +1396,7 @@ def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post
     _on_device(torch, y.device, L.mist_block_backward, ctypes.byref(d), y.data_ptr(), _ptr(block), stats.data_ptr(), _ptr(weight), _ptr(post_weight),
                _ptr(post_bias), _ptr(gate), ctypes.byref(g), _ptr(ws), need.value, handle)
     if other is not None:
-        _used_on(other, y, stats, dh, block, dy, weight, post_weight, post_bias, gate, *grads, dgate, dx, dblock)
+        _used_on(other, y, stats, dh, block, dy, weight, post_weight, post_bias, shared, *grads, dgate, dx, dblock)
     return dx, dblock
 
 

@@ -1,0 +1,46 @@
+"""Cases of the norms around a block beyond the grids of test_gpu_block.py, against the same definition and with its tolerances."""
+import sys
+
+import pytest
+
+from test_gpu_block import EPS, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "a GPU is required"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+@pytest.mark.parametrize("batch, seq, hidden", [(3, 5, 64), (4, 300, 1025), (300, 2, 24), (2, 3, 9000), (1, 7, 200)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_an_expanded_gate(torch, batch, seq, hidden, accumulate):
+    """A row of gates for each sequence that is one row in memory: the results, and a row of gradients for each sequence, as for rows of their own."""
+    from paper_2503_19050_amd import mist
+    say("expanded gate", batch, seq, hidden)
+    s, w, gr = make(torch, batch, seq, hidden, "bf16", "f32", "f32", True, True, "sequence")
+    shared = w["gate"][:1].expand(batch, hidden)
+    results = []
+    for gate in (shared, shared.contiguous()):
+        how = dict(w, gate=gate)
+        r = mist.block_norm(s["x"], s["block"], kind="layer", eps=EPS, **how)
+        outs = {"d" + k: torch.full(t.shape, 3.0, device="cuda") for k, t in w.items()}
+        how.pop("bias")
+        d = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], kind="layer", accumulate=accumulate, **how, **outs)
+        results.append([*r, *d, *outs.values()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = {"d" + k: torch.full(t.shape, 3.0, device="cuda") for k, t in w.items()}
+    torch.cuda.synchronize()
+    d = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], kind="layer", accumulate=accumulate, stream=side, **dict(how, gate=shared), **outs)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip([*d, *outs.values()], results[1][3:]))
