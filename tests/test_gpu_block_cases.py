@@ -44,3 +44,15 @@ def test_an_expanded_gate(torch, batch, seq, hidden, accumulate):
     d = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], kind="layer", accumulate=accumulate, stream=side, **dict(how, gate=shared), **outs)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip([*d, *outs.values()], results[1][3:]))
+
+
+def test_gradients_in_the_places_given(torch):
+    """What is returned is what was given, with the bits of a call with places of its own."""
+    from paper_2503_19050_amd import mist
+    s, w, gr = make(torch, 3, 11, 333, "bf16", "bf16", "bf16", True, True, "sequence")
+    r = mist.block_norm(s["x"], s["block"], kind="layer", **w)
+    how = {k: v for k, v in w.items() if k != "bias"}
+    dx, db = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], kind="layer", **how)
+    dy, dh = gr["dy"].clone(), gr["dh"].clone()
+    p, q = mist.block_norm_grad(r.y, r.stats, dh, block=s["block"], dy=dy, dx=dy, dblock=dh, kind="layer", **how)
+    assert p is dy and q is dh and torch.equal(p, dx) and torch.equal(q, db)
