@@ -782,7 +782,7 @@ typedef struct mist_kept {
 mist_status mist_act_forward(const mist_act_desc* d, const void* up, const void* gate, void* out, const mist_kept* up8,
                              const mist_kept* gate8, void* hip_stream);
 
-/* Gradients at the kept values: dgate = dout * up * act'(gate) and dup = dout * act(gate), or dup = dout * act'(up)
+/* Gradients at the kept values (as mist_kept_load gives them in the type): dgate = dout * up * act'(gate) and dup = dout * act(gate), or dup = dout * act'(up)
  * where gate8 is NULL (then dgate is too).  again (NULL: not wanted) receives the activation at the kept values.
  * dup or dgate may be dout (with its stride).  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_act_backward(const mist_act_desc* d, const mist_kept* up8, const mist_kept* gate8, const void* dout, void* dup,

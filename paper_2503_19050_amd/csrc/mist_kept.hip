@@ -85,6 +85,7 @@ __device__ __forceinline__ Float8 load_group(const Shape& s, const Place& p, con
   return __builtin_convertvector(q, Float8) * step;
 }
 
+// f16's largest value is kept as one past it.
 template <class T>
 __device__ __forceinline__ Float8 in_range(Float8 x) {
   if (sizeof(T) == 2 && !__is_same(T, __bf16)) {
@@ -144,9 +145,9 @@ __global__ __launch_bounds__(kThreads) void k_act(Shape s, Strides st, const T* 
 template <class T, int KIND, bool GATE>
 __global__ __launch_bounds__(kThreads) void k_act_back(Shape s, Strides st, mist_kept up8, mist_kept gate8, const T* dout, T* dup, T* dgate, T* again) {
   each_place(s, [&](const Place& p) {
-    const Float8 d = load8(dout + p.row * st.out, p.c), u = load_group(s, p, up8);
+    const Float8 d = load8(dout + p.row * st.out, p.c), u = in_range<T>(load_group(s, p, up8));
     Float8 g, y, du, dg;
-    if (GATE) g = load_group(s, p, gate8);
+    if (GATE) g = in_range<T>(load_group(s, p, gate8));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const Act f = act<KIND>(GATE ? g[i] : u[i]);
