@@ -660,11 +660,13 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
   for (int i = 0; i < kSlots; ++i) {
     if (!p.wanted[i]) continue;
     k.slot[i] = (float*)ws;
-    const bool gates = i == 4 && a.gate_stride;
+    const bool gates = i == 4 && d->gate_stride && d->batch != 1;  // a row for each sequence
+    if (gates && !d->batch) continue;
     j.job[jobs++] = JoinJob{k.slot[i], out[i], gates ? p.parts.pieces : p.parts.n, gates ? d->batch : 1, gates ? g->dgate_stride : 0};
     most = std::max(most, (d->hidden + join_columns(j.job[jobs - 1]) - 1) / join_columns(j.job[jobs - 1]) * j.job[jobs - 1].rows);
     ws += ((size_t)p.parts.n * d->hidden * 4 + 255) / 256 * 256;
   }
+  if (!any && !jobs) return MIST_OK;
   const hipStream_t st = (hipStream_t)stream;
   if (any) {
     with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide, auto whole) {

@@ -1,4 +1,5 @@
 """Cases of the norms around a block beyond the grids of test_gpu_block.py, against the same definition and with its tolerances."""
+import ctypes
 import sys
 
 import pytest
@@ -56,3 +57,20 @@ def test_gradients_in_the_places_given(torch):
     dy, dh = gr["dy"].clone(), gr["dh"].clone()
     p, q = mist.block_norm_grad(r.y, r.stats, dh, block=s["block"], dy=dy, dx=dy, dblock=dh, kind="layer", **how)
     assert p is dy and q is dh and torch.equal(p, dx) and torch.equal(q, db)
+
+
+def test_gates_of_sequences_without_tokens(torch):
+    """The C call: a row of zeros for each sequence's gate, whether the gate itself is given or not, and nothing beside them."""
+    from paper_2503_19050_amd import mist
+    L = mist.load()
+    for gate in (None, torch.ones(3, 40, device="cuda")):
+        out = torch.full((5, 48), 7.0, device="cuda")
+        d = mist.BlockDesc(3, 0, 40, 40, 40, 40, 40, 48, 0, 0, 0, 0, 1e-5, 1.0, 1.0)
+        g = mist.BlockGrads(None, None, None, None, None, None, None, None, out.data_ptr(), 40, 40, 40, 40, 48, 0)
+        need = ctypes.c_size_t()
+        assert L.mist_block_workspace(ctypes.byref(d), ctypes.byref(g), ctypes.byref(need)) == 0
+        ws = torch.empty(max(1, need.value), device="cuda", dtype=torch.uint8)
+        ptr = None if gate is None else gate.data_ptr()
+        assert L.mist_block_backward(ctypes.byref(d), None, None, None, None, None, None, ptr, ctypes.byref(g), ws.data_ptr(), need.value,
+                                     torch.cuda.current_stream().cuda_stream) == 0
+        assert bool((out[:3, :40] == 0).all()) and bool((out[3:] == 7).all()) and bool((out[:, 40:] == 7).all())
