@@ -489,6 +489,18 @@ mist_status check_tensors(const mist_block_desc* d, std::initializer_list<Tensor
   return MIST_OK;
 }
 
+// A vector of n values, and rows of the residual's or the block's type, for the checks of the call's other tensors.
+mist::Use<mist::Rows> vector(const void* p, int64_t n, int64_t bytes, bool out) { return {mist::Rows{p, 1, 0, n, bytes}, out}; }
+mist::Use<mist::Rows> rows(const mist_block_desc* d, const void* p, int64_t stride, int32_t type, bool out) {
+  return {mist::Rows{p, d->batch * d->seq, stride, d->hidden, mist::type_bytes(type)}, out};
+}
+// gates by sequence, or one for all
+mist::Use<mist::Rows> gates(const mist_block_desc* d, const void* p, int64_t stride, bool out) {
+  const bool by_sequence = d->gate_stride && d->batch != 1;
+  return {mist::Rows{p, by_sequence ? d->batch : 1, by_sequence ? stride : 0, d->hidden, mist::type_bytes(d->weight_type)}, out};
+}
+mist_status not_shared(bool shared) { return shared ? lib_fail(MIST_E_INVALID, "block norm: an output or the workspace overlaps another tensor") : MIST_OK; }
+
 BlockArgs args(const mist_block_desc* d, const void* weight, const void* bias, const void* post_weight, const void* post_bias, const void* gate) {
   return BlockArgs{d->batch * d->seq, std::max<int64_t>(d->seq, 1), d->hidden, d->x_stride, d->block_stride, d->y_stride, d->h_stride,
                    gate && d->batch > 1 ? d->gate_stride : 0, d->kind == MIST_BLOCK_LAYER, d->weight_type, d->eps, d->res_scale, d->block_scale,
@@ -602,6 +614,13 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
   if (const mist_status st = check_tensors(d, {{x, d->x_stride, d->res_type, false, {}}, {block, d->block_stride, d->type, false, {}},
                                                {y, d->y_stride, d->res_type, true, {x, block}}, {h, d->h_stride, d->type, true, {}}}))
     return st;
+  const int64_t wide = mist::type_bytes(d->weight_type);
+  if (const mist_status st = not_shared(mist::shared<mist::Rows>(
+          {vector(stats, a.n * 4, 4, true), vector(weight, d->hidden, wide, false), vector(bias, d->hidden, wide, false), vector(post_weight, d->hidden, wide, false),
+           vector(post_bias, d->hidden, wide, false), gates(d, gate, d->gate_stride, false)},
+          {rows(d, x, d->x_stride, d->res_type, false), rows(d, block, d->block_stride, d->type, false), rows(d, y, d->y_stride, d->res_type, true),
+           rows(d, h, d->h_stride, d->type, true)})))
+    return st;
   with_kernel(d, post_weight || gate, [&](auto e, auto f, auto u, auto l, auto wide, auto whole) {
     using A = decltype(e);
     using R = decltype(f);
@@ -643,6 +662,15 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
                                                {g->dh, g->dh_stride, d->type, false, {}}, {g->dy, g->dy_stride, d->res_type, false, {}},
                                                {g->dx, g->dx_stride, d->res_type, true, {g->dy, nullptr}},
                                                {g->dblock, g->dblock_stride, d->type, true, {g->dh, block}}}))
+    return st;
+  const int64_t wide = mist::type_bytes(d->weight_type);
+  if (const mist_status st = not_shared(mist::shared<mist::Rows>(
+          {vector(stats, a.n * 4, 4, false), vector(weight, d->hidden, wide, false), vector(post_weight, d->hidden, wide, false), vector(post_bias, d->hidden, wide, false),
+           gates(d, gate, d->gate_stride, false), vector(g->dweight, d->hidden, wide, true), vector(g->dbias, d->hidden, wide, true),
+           vector(g->dpost_weight, d->hidden, wide, true), vector(g->dpost_bias, d->hidden, wide, true), gates(d, g->dgate, g->dgate_stride, true),
+           vector(workspace, (int64_t)p.bytes, 1, true)},
+          {rows(d, y, d->y_stride, d->res_type, false), rows(d, block, d->block_stride, d->type, false), rows(d, g->dh, g->dh_stride, d->type, false),
+           rows(d, g->dy, g->dy_stride, d->res_type, false), rows(d, g->dx, g->dx_stride, d->res_type, true), rows(d, g->dblock, g->dblock_stride, d->type, true)})))
     return st;
   BackArgs k{};
   k.a = a;

@@ -5,6 +5,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "mist.h"
 
 namespace mist {
@@ -186,6 +188,28 @@ inline bool overlap(const Rows& a, const Rows& b) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p), m = (uintptr_t)step;
   const int64_t off = (int64_t)(y >= x ? (y - x) % m : (m - (x - y) % m) % m);
   return off < wa || off + wb > step;
+}
+
+// A tensor of a call, by its addresses (Range or Rows).
+template <class R>
+struct Use {
+  R at;
+  bool out;
+};
+inline bool empty(const Range& x) { return x.lo == x.hi; }
+inline bool empty(const Rows& x) { return !x.p || x.rows <= 0 || x.width <= 0; }
+// Whether an output of the first list shares memory with another tensor of it, or one of the first list with one of the second where
+// either is an output.
+template <class R>
+bool shared(std::initializer_list<Use<R>> all, std::initializer_list<Use<R>> others = {}) {
+  for (auto a = all.begin(); a != all.end(); ++a) {
+    if (empty(a->at)) continue;
+    for (auto b = all.begin(); b != a; ++b)
+      if ((a->out || b->out) && !empty(b->at) && overlap(a->at, b->at)) return true;
+    for (const Use<R>& b : others)
+      if ((a->out || b.out) && !empty(b.at) && overlap(a->at, b.at)) return true;
+  }
+  return false;
 }
 
 inline bool is_aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

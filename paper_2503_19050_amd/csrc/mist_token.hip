@@ -602,6 +602,13 @@ TokenArgs args(const mist_token_desc* d) {
                    pre, (float)(1.44269504088896341 * d->scale / pre)};
 }
 
+// The addresses of n values of 4 bytes (2^50 bytes at most: more than there are on any device), and of the targets.
+mist::Range values(const void* p, int64_t n) { return mist::range_of(p, 1, 0, std::min<int64_t>(n, (int64_t)1 << 48), 4); }
+mist::Range targets_range(const mist_token_desc* d, const void* p) { return mist::range_of(p, d->batch, d->ids_stride, d->seq, d->ids_bytes); }
+mist::Range logits_range(const mist_token_desc* d, const void* p) { return rows_range(d, p, d->logits_batch_stride, d->logits_stride); }
+mist::Range grad_range(const mist_token_desc* d, const void* p) { return rows_range(d, p, d->grad_batch_stride, d->grad_stride); }
+mist_status not_shared(bool shared) { return shared ? lib_fail(MIST_E_INVALID, "token log probabilities: an output overlaps another tensor") : MIST_OK; }
+
 bool floats_ok(std::initializer_list<const float*> ps) {
   for (const float* p : ps)
     if (!mist::is_aligned(p, 4)) return false;
@@ -622,6 +629,11 @@ mist_status forward(const mist_token_desc* d, const void* logits, const void* ta
   if (!mist::is_aligned(logits, mist::type_bytes(d->type)) || !mist::is_aligned(targets, d->ids_bytes) || !mist::is_aligned(stats, 16) ||
       !mist::is_aligned(top_ids, 4) || !floats_ok({logp, lse, entropy, top_logp}))
     return lib_fail(MIST_E_INVALID, "token log probabilities: a buffer is not aligned to its elements, or stats to 16");
+  const int64_t n = a.n;
+  if (const mist_status st = not_shared(mist::shared<mist::Range>({{logits_range(d, logits), false}, {targets_range(d, targets), false}, {values(stats, n * 4), true},
+                                                                   {values(logp, n), true}, {values(lse, n), true}, {values(entropy, n), true},
+                                                                   {values(top_ids, n * a.top), true}, {values(top_logp, n * a.top), true}})))
+    return st;
   const unsigned blocks = (unsigned)std::min<int64_t>(a.n, kMostBlocks);
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
@@ -664,6 +676,11 @@ mist_status mist_token_join(const mist_token_desc* d, int32_t ranks, const float
   if (!mist::is_aligned(stats, 16) || !mist::is_aligned(targets, d->ids_bytes) || !mist::is_aligned(top_ids, 4) || !mist::is_aligned(out_ids, 4) ||
       !floats_ok({top_z, logp, lse, entropy, out_logp}))
     return lib_fail(MIST_E_INVALID, "token log probabilities: a buffer is not aligned to its elements, or stats to 16");
+  const int64_t n = a.n, most = n * a.top;
+  if (const mist_status st = not_shared(mist::shared<mist::Range>({{values(stats, ranks * n * 4), false}, {values(top_ids, ranks * most), false}, {values(top_z, ranks * most), false},
+                                                                   {targets_range(d, targets), false}, {values(logp, n), true}, {values(lse, n), true},
+                                                                   {values(entropy, n), true}, {values(out_ids, most), true}, {values(out_logp, most), true}})))
+    return st;
   const int lanes = (int64_t)ranks * std::max(1, a.top) <= 16 ? 16 : 64, tokens = kThreads / lanes;
   const int64_t blocks = std::min<int64_t>((a.n + tokens - 1) / tokens, kMostBlocks);
   hipLaunchKernelGGL(lanes == 16 ? k_join<16> : k_join<64>, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, a, ranks, stats, top_ids, top_z, targets, logp, lse,
@@ -683,6 +700,10 @@ mist_status mist_token_grad(const mist_token_desc* d, const void* logits, const 
       !floats_ok({lse, dlogp, entropy, dentropy}))
     return lib_fail(MIST_E_INVALID, "token log probabilities: a buffer is not aligned to its elements");
   if (const mist_status st = check_grad(d, logits, dlogits)) return st;
+  const int64_t n = a.n;
+  if (const mist_status st = not_shared(mist::shared<mist::Range>({{grad_range(d, dlogits), true}, {targets_range(d, targets), false}, {values(lse, n), false},
+                                                                   {values(dlogp, n), false}, {values(entropy, n), false}, {values(dentropy, n), false}})))
+    return st;
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;
     constexpr int kSlab = Chunk<T, kThreads, kGradVectors, false>::kAll;
@@ -706,6 +727,10 @@ mist_status mist_token_loss(const mist_token_desc* d, const void* logits, const 
   if (!mist::is_aligned(logits, bytes) || !mist::is_aligned(dlogits, bytes) || !mist::is_aligned(targets, d->ids_bytes) || !floats_ok({weights, logp}))
     return lib_fail(MIST_E_INVALID, "token loss: a buffer is not aligned to its elements");
   if (const mist_status st = check_grad(d, logits, dlogits)) return st;
+  const int64_t n = a.n;
+  if (const mist_status st = not_shared(mist::shared<mist::Range>({{grad_range(d, dlogits), true}, {targets_range(d, targets), false}, {values(weights, n), false}, {values(logp, n), true}}) ||
+                                        mist::shared<mist::Range>({{values(logp, n), true}, {logits_range(d, logits), false}})))
+    return st;
   const unsigned blocks = (unsigned)std::min<int64_t>(a.n, kMostBlocks);
   mist::with_type(d->type, [&](auto x) {
     using T = typename decltype(x)::type;

@@ -63,7 +63,7 @@ def test_gates_of_sequences_without_tokens(torch):
     """The C call: a row of zeros for each sequence's gate, whether the gate itself is given or not, and nothing beside them."""
     from paper_2503_19050_amd import mist
     L = mist.load()
-    for gate in (None, torch.ones(3, 40, device="cuda")):
+    for gate in (None, torch.ones(3, 48, device="cuda")):   # rows of 40 at a stride of 48
         out = torch.full((5, 48), 7.0, device="cuda")
         d = mist.BlockDesc(3, 0, 40, 40, 40, 40, 40, 48, 0, 0, 0, 0, 1e-5, 1.0, 1.0)
         g = mist.BlockGrads(None, None, None, None, None, None, None, None, out.data_ptr(), 40, 40, 40, 40, 48, 0)
@@ -74,3 +74,17 @@ def test_gates_of_sequences_without_tokens(torch):
         assert L.mist_block_backward(ctypes.byref(d), None, None, None, None, None, None, ptr, ctypes.byref(g), ws.data_ptr(), need.value,
                                      torch.cuda.current_stream().cuda_stream) == 0
         assert bool((out[:3, :40] == 0).all()) and bool((out[3:] == 7).all()) and bool((out[:, 40:] == 7).all())
+
+
+def test_gates_beside_their_gradients(torch):
+    """Columns of one buffer at one stride: gates and their gradients may lie in it."""
+    from paper_2503_19050_amd import mist
+    s, w, gr = make(torch, 3, 11, 64, "bf16", "f32", "f32", True, True, "sequence")
+    both = torch.full((3, 130), 7.0, device="cuda")
+    both[:, 1:65] = w["gate"]
+    r = mist.block_norm(s["x"], s["block"], **w)
+    how = {k: v for k, v in w.items() if k not in ("bias", "gate")}
+    want = torch.empty_like(w["gate"])
+    for gate, dgate in ((w["gate"], want), (both[:, 1:65], both[:, 65:129])):
+        mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], gate=gate, dgate=dgate, **how)
+    assert torch.equal(both[:, 65:129], want) and torch.equal(both[:, 1:65], w["gate"]) and bool((both[:, [0, 129]] == 7).all())
