@@ -572,10 +572,11 @@ struct Plan {
   size_t bytes;
   bool wanted[kSlots], direct;  // direct: gates' gradients need no parts
 };
-Plan plan_of(const mist_block_desc* d, const mist_block_grads* g) {
+// more: a norm before or a gate, as the kernel has it, whether or not their gradients are wanted.
+Plan plan_of(const mist_block_desc* d, const mist_block_grads* g, bool more) {
   Plan p{};
   const bool by_sequence = d->gate_stride && d->batch > 1;
-  p.parts = parts_of(d, by_sequence, g->dpost_weight || g->dpost_bias || g->dgate);
+  p.parts = parts_of(d, by_sequence, more);
   const void* out[kSlots] = {g->dweight, g->dbias, g->dpost_weight, g->dpost_bias, g->dgate};
   p.direct = by_sequence && p.parts.pieces == 1;
   for (int i = 0; i < kSlots; ++i) {
@@ -583,6 +584,12 @@ Plan plan_of(const mist_block_desc* d, const mist_block_grads* g) {
     if (p.wanted[i]) p.bytes += (size_t)p.parts.n * d->hidden * 4 + 256;
   }
   return p;
+}
+
+// The query does not see whether there is a norm before or a gate, unless their gradients are wanted: enough for both.
+size_t scratch_of(const mist_block_desc* d, const mist_block_grads* g) {
+  const size_t more = plan_of(d, g, true).bytes;
+  return g->dpost_weight || g->dpost_bias || g->dgate ? more : std::max(more, plan_of(d, g, false).bytes);
 }
 
 mist_status check_grads(const mist_block_desc* d, const mist_block_grads* g) {
@@ -635,7 +642,7 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
 mist_status mist_block_workspace(const mist_block_desc* d, const mist_block_grads* g, size_t* bytes) {
   if (!bytes) return lib_fail(MIST_E_INVALID, "block norm's gradient: null argument");
   if (const mist_status st = check_grads(d, g)) return st;
-  *bytes = plan_of(d, g).bytes;
+  *bytes = scratch_of(d, g);
   return MIST_OK;
 }
 
@@ -649,15 +656,16 @@ mist_status mist_block_backward(const mist_block_desc* d, const void* y, const v
   if (any && ((!weight && (g->dweight || g->dbias)) || (!post_weight && (g->dpost_weight || g->dpost_bias)) || (!gate && g->dgate)))
     return lib_fail(MIST_E_INVALID, "block norm's gradient: of a weight, bias or gate that is not there");
   BlockArgs a = args(d, weight, nullptr, post_weight, post_bias, gate);
-  Plan p = plan_of(d, g);
+  const Plan p = plan_of(d, g, post_weight || gate);
+  const size_t need = scratch_of(d, g);
   if (!any && g->accumulate) return MIST_OK;
   if (any && (!stats || (weight && (!y || !g->dh)) || (!weight && g->dh) || (!g->dh && !g->dy)))
     return lib_fail(MIST_E_INVALID, "block norm's gradient: null buffer, or dh without its weight");
   if (!mist::is_aligned(stats, 16) || !mist::is_aligned(workspace, 256) ||
       !weights_ok(d, {weight, post_weight, post_bias, gate, g->dweight, g->dbias, g->dpost_weight, g->dpost_bias, g->dgate}))
     return lib_fail(MIST_E_INVALID, "block norm's gradient: a buffer is not aligned to its elements, stats to 16 or the workspace to 256");
-  if (p.bytes && !workspace) return lib_fail(MIST_E_INVALID, "block norm's gradient: null workspace");
-  if (workspace_bytes < p.bytes) return lib_fail(MIST_E_RANGE, "block norm's gradient: workspace too small");
+  if (need && !workspace) return lib_fail(MIST_E_INVALID, "block norm's gradient: null workspace");
+  if (workspace_bytes < need) return lib_fail(MIST_E_RANGE, "block norm's gradient: workspace too small");
   if (const mist_status st = check_tensors(d, {{y, d->y_stride, d->res_type, false, {}}, {block, d->block_stride, d->type, false, {}},
                                                {g->dh, g->dh_stride, d->type, false, {}}, {g->dy, g->dy_stride, d->res_type, false, {}},
                                                {g->dx, g->dx_stride, d->res_type, true, {g->dy, nullptr}},

@@ -47,6 +47,27 @@ def test_an_expanded_gate(torch, batch, seq, hidden, accumulate):
     assert all(torch.equal(a, b) for a, b in zip([*d, *outs.values()], results[1][3:]))
 
 
+@pytest.mark.parametrize("shape", [(2, 700, 512), (1, 5000, 2560), (1, 9000, 1024), (3, 500, 96), (1, 90, 9000)], ids=str)
+@pytest.mark.parametrize("gate", ["", "all", "sequence"])
+def test_sums_do_not_go_by_what_is_wanted(torch, shape, gate):
+    """With a norm before or a gate: each gradient has the same bits whichever others are asked for."""
+    from paper_2503_19050_amd import mist
+    say("wanted", shape, gate)
+    s, w, gr = make(torch, *shape, "bf16", "bf16", "f32", True, True, gate)
+    r = mist.block_norm(s["x"], s["block"], eps=EPS, **w)
+    how = {k: t for k, t in w.items() if k != "bias"}
+
+    def grads(*names):
+        outs = {"d" + k: torch.zeros_like(w[k]) for k in names}
+        dx, db = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], **how, **outs)
+        return dict(outs, dx=dx, db=db)
+
+    want = grads(*w)
+    for names in [("weight", "bias"), ("weight",), ("post_weight",), ("bias", "post_bias"), ()] + ([("gate",)] if gate else []):
+        for k, t in grads(*names).items():
+            assert torch.equal(t, want[k]), (names, k)
+
+
 def test_gradients_in_the_places_given(torch):
     """What is returned is what was given, with the bits of a call with places of its own."""
     from paper_2503_19050_amd import mist
