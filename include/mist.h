@@ -657,18 +657,19 @@ typedef struct mist_token_desc {
 
 /* Over the whole vocabulary (vocab_begin = 0): per token fp32 logp, lse and entropy (logp and entropy may be NULL; without
  * logp, targets may be), and int32 top_ids[tokens * top] with fp32 top_logp[tokens * top], the most probable tokens by logit, the
- * lower id first among equals (a NaN above everything); where fewer than top are not masked out the rest has
- * id -1 and -inf.  Per-token arrays are contiguous, sequence by sequence.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+ * lower id first among equals (a NaN above everything); a logit of -inf is none, a finite one whose z is past fp32 is one of -inf; where
+ * there are fewer than top the rest has id -1 and -inf.  Per-token arrays are contiguous, sequence by sequence.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_token_logprob(const mist_token_desc* d, const void* logits, const void* targets, float* logp, float* lse,
                                float* entropy, int32_t* top_ids, float* top_logp, void* hip_stream);
 
 /* One rank's part: stats[tokens * 4] = (m, s, u, the target's z or -inf where another rank holds it) and its
- * alternatives as ids of the whole vocabulary with z.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
+ * alternatives, by logit, as ids of the whole vocabulary with z.  Errors: MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_token_part(const mist_token_desc* d, const void* logits, const void* targets, float* stats, int32_t* top_ids,
                             float* top_z, void* hip_stream);
 
 /* The ranks' parts joined: stats[ranks][tokens * 4], top_ids and top_z [ranks][tokens * top] as gathered; outputs as
- * of mist_token_logprob.  Of *d it uses batch, seq, ids_stride, ids_bytes and top.  ranks in 1..65536.  Errors:
+ * of mist_token_logprob, but alternatives go by z, which the parts have, the lower id first among equals: fp32 logits that differ may
+ * have one z.  Of *d it uses batch, seq, ids_stride, ids_bytes and top.  ranks in 1..65536.  Errors:
  * MIST_E_INVALID, MIST_E_DEVICE. */
 mist_status mist_token_join(const mist_token_desc* d, int32_t ranks, const float* stats, const int32_t* top_ids, const float* top_z,
                             const void* targets, float* logp, float* lse, float* entropy, int32_t* out_ids, float* out_logp,

@@ -506,13 +506,14 @@ __global__ __launch_bounds__(kThreads) void k_join(TokenArgs a, int32_t ranks, c
         const int64_t at = (j / a.top * a.n + t) * a.top + j % a.top;
         const int32_t id = ids[at];
         const uint32_t rank = rank_of(zs[at]);
-        const uint64_t key = id >= 0 && rank ? key_of(rank, (uint32_t)id) : 0;
+        const uint64_t key = id >= 0 ? key_of(rank, (uint32_t)id) : 0;  // a finite logit whose z is past fp32 is one too: rank 0
         if (key > best && key < last) best = key;
       }
       last = best = wave_max_key<L>(best);
       if (lane == 0) {
+        const uint32_t rank = (uint32_t)(best >> 32);
         out_ids[t * a.top + k] = best ? (int32_t)~(uint32_t)best : -1;
-        out_logp[t * a.top + k] = best ? of_rank((uint32_t)(best >> 32)) - l : -HUGE_VALF;
+        out_logp[t * a.top + k] = rank ? of_rank(rank) - l : -HUGE_VALF;
       }
     }
   }

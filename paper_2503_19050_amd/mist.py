@@ -1172,7 +1172,7 @@ def token_part(logits, targets, *, vocab_begin: int, scale: float = 1.0, top: in
 
 def token_join(stats, targets=None, *, entropy: bool = False, top_ids=None, top_z=None, stream=None) -> TokenLogprob:
     """mist_token_join: token_logprob's results from the parts of all ranks, stats [ranks, ..., 4], and top_ids and top_z
-    [ranks, ..., top] where alternatives are wanted."""
+    [ranks, ..., top] where alternatives are wanted (in the order of z, the lower id first among equals)."""
     torch = _torch()
     L = _lib or load()
     what = "token log probabilities"

@@ -128,3 +128,39 @@ def test_scaled_values_of_any_size(torch, kind, rows, scale):
     r = mist.token_logprob(y, torch.zeros_like(t), scale=scale, entropy=True)
     one = far & (y[0, :, 0].double() * scale <= top) & (y[0, :, 0].double() * scale >= -top)
     assert bool((r.logp[0][one] == 0).all()) and bool((r.entropy[0][one].abs() < tiny).all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("ranks", [1, 2, 4, 30])
+def test_joined_alternatives_past_fp32(torch, kind, ranks):
+    """Finite logits whose scaled value is below fp32's range are alternatives of -inf, from parts as from the whole vocabulary; a masked one is none."""
+    from paper_2503_19050_amd import mist
+    low = torch.finfo(types(torch)[kind]).min
+    x = torch.full((1, 3, 60), low, device="cuda", dtype=types(torch)[kind])
+    x[0, 1, 44] = 1.0
+    x[0, 2] = -math.inf
+    x[0, 2, 31] = low
+    t = torch.full((1, 3), 44, device="cuda")
+    whole = mist.token_logprob(x, t, scale=1.5, top=3)
+    assert whole.top_ids.tolist() == [[[0, 1, 2], [44, 0, 1], [31, -1, -1]]]
+    per = 60 // ranks
+    parts = [mist.token_part(x[..., k * per:(k + 1) * per], t, vocab_begin=k * per, scale=1.5, top=3) for k in range(ranks)]
+    r = mist.token_join(torch.stack([p.stats for p in parts]), t, top_ids=torch.stack([p.top_ids for p in parts]), top_z=torch.stack([p.top_z for p in parts]))
+    assert torch.equal(r.top_ids, whole.top_ids) and torch.equal(r.top_logp, whole.top_logp) and torch.equal(r.logp, whole.logp)
+
+
+def test_joined_alternatives_of_one_scaled_value(torch):
+    """fp32 logits that differ and have one z: by logit in a part and in the whole vocabulary, by id where parts are joined."""
+    from paper_2503_19050_amd import mist
+    scale = float(torch.tensor(0.6))
+    high = torch.tensor([2.0 - k * 2.0 ** -23 for k in range(1, 9)], device="cuda")
+    z = high * torch.tensor(scale, device="cuda")
+    k = int((z[:-1] == z[1:]).nonzero()[0])
+    x = torch.zeros(1, 1, 20, device="cuda")
+    x[0, 0, 3], x[0, 0, 17] = high[k + 1], high[k]
+    t = torch.zeros(1, 1, device="cuda", dtype=torch.int64)
+    assert mist.token_logprob(x, t, scale=scale, top=3).top_ids.tolist() == [[[17, 3, 0]]]
+    part = mist.token_part(x, t, vocab_begin=0, scale=scale, top=3)
+    assert part.top_ids.tolist() == [[[17, 3, 0]]] and part.top_z[0, 0, 0] == part.top_z[0, 0, 1] == z[k]
+    r = mist.token_join(part.stats[None], t, top_ids=part.top_ids[None], top_z=part.top_z[None])
+    assert r.top_ids.tolist() == [[[3, 17, 0]]]
