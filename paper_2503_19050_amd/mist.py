@@ -1154,6 +1154,8 @@ def token_part(logits, targets, *, vocab_begin: int, scale: float = 1.0, top: in
     new) and its `top` alternatives.  targets are ids of the whole vocabulary."""
     torch = _torch()
     L = _lib or load()
+    if targets is None:
+        _need(False, "token log probabilities: a part needs targets")
     _no_graph(torch, "token log probabilities", logits)
     d = _token_desc(torch, logits, targets, None, vocab_begin, scale, top)
     device, shape = logits.device, tuple(logits.shape[:-1])
@@ -1238,6 +1240,8 @@ def token_loss(logits, targets, weights=1.0, *, scale: float = 1.0, dlogits=None
     torch = _torch()
     L = _lib or load()
     what = "token loss"
+    if targets is None:
+        _need(False, "token loss: needs targets")
     _no_graph(torch, what, logits)
     _here(what, logits, targets, dlogits)
     if not (logits.dim() in (2, 3)):

@@ -1,6 +1,8 @@
 """Calls of the loss, the norms around a block and the kept activations that end on the host, without a GPU: nothing to do, and refusals."""
 import ctypes
 
+import pytest
+
 from paper_2503_19050_amd import mist
 
 r = ctypes.byref
@@ -87,3 +89,12 @@ def test_gates_beside_their_gradients():
     back = lambda dgate, d=d: L.mist_block_backward(r(d), A[4], A[5], A[6], A[7], None, None, A[8], r(grads(dgate)), A[9], 1 << 20, None)  # noqa: E731
     assert back(A[8] + 252) == -1 and b"overlap" in L.mist_last_error()
     assert back(A[8] - 252) == -1 and b"overlap" in L.mist_last_error()
+
+
+def test_calls_without_targets():
+    torch = mist._torch()
+    x = torch.zeros(2, 3, 8)
+    for call in (lambda: mist.token_part(x, None, vocab_begin=0), lambda: mist.token_loss(x, None)):
+        with pytest.raises(mist.MistError, match="targets") as e:
+            call()
+        assert e.value.status == mist.E_INVALID
