@@ -1406,7 +1406,7 @@ def block_norm_grad(y, stats, dh=None, *, block=None, dy=None, weight=None, post
 
 class Checkpoint:
     """A tensor kept in 8 bits (mist_kept_store): int8 values and uint8 exponents, a byte for each 128 values of a row, both plain tensors
-    that a program can offload or send.  shape and dtype are the tensor's."""
+    that a program can offload or send.  shape and dtype are the tensor's; stream: the one that it is used on (None: the current one)."""
 
     def __init__(self, shape, dtype, device="cuda", stream=None):
         torch = _torch()
@@ -1420,7 +1420,10 @@ class Checkpoint:
             _need(False, "checkpoint: the last dimension must be at least 1")
         self.rows, self.width = math.prod(self.shape[:-1]), self.shape[-1]
         groups = self.groups = -(-self.width // KEPT_GROUP)
-        with _pool(torch, stream):
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        _, other = _stream_of(torch, stream, device)
+        with _pool(torch, other):
             self.values = torch.empty(self.rows, groups * KEPT_GROUP, dtype=torch.int8, device=device)
             self.exponents = torch.empty(self.rows, groups, dtype=torch.uint8, device=device)
 

@@ -43,3 +43,19 @@ def test_f16_at_its_largest_value(torch, form, width):
         for got, w in zip([again, dup] + ([] if g is None else [dgate]), want):
             assert bool(got.isfinite().all())
             assert bool(((got.double() - w).abs() <= (2.0 ** -11 + 2.0 ** -20) * w.abs() + 2.0 ** -24).all())
+
+
+def test_a_checkpoint_of_a_stream(torch):
+    """A checkpoint made for another stream, given as a torch stream or as its handle, and for the default one."""
+    from paper_2503_19050_amd import mist
+    side = torch.cuda.Stream()
+    x = torch.randn(5, 300, device="cuda").bfloat16()
+    want = mist.checkpoint_store(x)
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream, 0, None):
+        for device in ("cuda", x.device):
+            c = mist.Checkpoint((5, 300), torch.bfloat16, device, stream=stream)
+            assert c.values.device == x.device
+            assert mist.checkpoint_store(x, c, stream=stream) is c
+            torch.cuda.synchronize()
+            assert torch.equal(c.values, want.values) and torch.equal(c.exponents, want.exponents)
