@@ -1005,6 +1005,11 @@ MlpAct = collections.namedtuple("MlpAct", "out up gate")
 
 
 def _no_graph(torch, what, *tensors) -> None:
+    forward = torch.autograd.forward_ad
+    if forward._current_level >= 0:   # forward mode, also under no_grad
+        for t in tensors:
+            if t is not None and forward.unpack_dual(t).tangent is not None:
+                _need(False, "%s: has no forward-mode gradient; a tensor with a tangent is given" % what)
     if not torch.is_grad_enabled():
         return
     for t in tensors:

@@ -98,3 +98,18 @@ def test_calls_without_targets():
         with pytest.raises(mist.MistError, match="targets") as e:
             call()
         assert e.value.status == mist.E_INVALID
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_tangents_are_not_dropped(grad):
+    torch = mist._torch()
+    t = torch.zeros(2, 3, dtype=torch.int64)
+    with torch.autograd.forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        plain = torch.zeros(2, 3, 8)
+        x = torch.autograd.forward_ad.make_dual(plain, torch.ones(2, 3, 8))
+        for call in (lambda: mist.token_logprob(x, t), lambda: mist.token_loss(x, t), lambda: mist.token_part(x, t, vocab_begin=0), lambda: mist.block_norm(x, weight=plain[0, 0]),
+                     lambda: mist.block_norm(plain, weight=x[0, 0]), lambda: mist.checkpoint_store(x), lambda: mist.mlp_act(plain, x)):
+            with pytest.raises(mist.MistError, match="tangent"):
+                call()
+        with pytest.raises(mist.MistError, match="GPU"):   # without one they go on to the next check
+            mist.token_logprob(plain, t)
