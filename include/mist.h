@@ -698,7 +698,7 @@ mist_status mist_token_loss(const mist_token_desc* d, const void* logits, const 
  * n = x / sqrt(mean x^2 + eps) (RMS) or n = (x - mean x) / sqrt(var x + eps) (LAYER).
  *     v = N(block) post_weight + post_bias   (block itself without post_weight)
  *     y = res_scale x + block_scale gate v   (gate: one value a column, or a row of them for each sequence; none: 1)
- *     h = N(y) weight + bias                 (of y as stored; biases may be NULL)
+ *     h = N(y) weight + bias                 (of y as stored, or with of_sum of the sum before its rounding; biases may be NULL)
  * Row strides are in elements, tokens of all sequences at one stride; columns are contiguous.  Those of gradients are
  * with the backward call. */
 typedef struct mist_block_desc {
@@ -712,6 +712,7 @@ typedef struct mist_block_desc {
   int32_t weight_type;     /* of weights, biases and gates, and their gradients */
   float eps;               /* >= 0, finite */
   float res_scale, block_scale; /* finite */
+  int32_t of_sum;          /* 0: a later norm of the stored y gives h bit for bit; 1: h of a 16-bit residual is rounded once, not twice */
 } mist_block_desc;
 
 /* y and h, and fp32 stats[tokens * 4] for the backward pass: mean and 1 / sqrt(var + eps) of block and of y (0 and 1 where there is
@@ -738,7 +739,7 @@ typedef struct mist_block_grads {
 /* Scratch bytes that mist_block_backward needs.  Errors: MIST_E_INVALID. */
 mist_status mist_block_workspace(const mist_block_desc* d, const mist_block_grads* g, size_t* bytes);
 
-/* From y (as stored), block and stats of the forward call.  dx may be dy, and dblock dh or block (each with the other's
+/* From y (as stored: with of_sum N(y) is formed from it and the sum's statistics), block and stats of the forward call.  dx may be dy, and dblock dh or block (each with the other's
  * stride).  workspace: at least mist_block_workspace bytes, aligned to 256.  Errors: MIST_E_INVALID, MIST_E_RANGE
  * (workspace too small), MIST_E_DEVICE. */
 mist_status mist_block_backward(const mist_block_desc* d, const void* y, const void* block, const float* stats, const void* weight,

@@ -34,7 +34,7 @@ constexpr int kJoinThreads = 1024;
 
 struct BlockArgs {
   int64_t n, seq, hidden, x_stride, block_stride, y_stride, h_stride, gate_stride;
-  int32_t layer, weight_type;
+  int32_t layer, weight_type, of_sum;
   float eps, res_scale, block_scale, inv_hidden;
   const void *weight, *bias, *post_weight, *post_bias, *gate;
 };
@@ -239,8 +239,9 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(B
         if (MORE) b[u] *= a.gate_stride ? load_weight(a.gate, a.weight_type, gate_row, c.e[u]) : shared_gate(u);
         v[u] = a.res_scale * v[u] + a.block_scale * b[u];
         if (there) store8(y + t * a.y_stride, c.e[u], v[u]);
-        // the norm is of y as it is stored: formed again from it, h has the same bits
-        v[u] = masked(__builtin_convertvector(__builtin_convertvector(v[u], mist::Raw8<R>), Float8), c.e[u]);
+        // of y as it is stored: formed again from it, h has the same bits
+        if (!a.of_sum) v[u] = __builtin_convertvector(__builtin_convertvector(v[u], mist::Raw8<R>), Float8);
+        v[u] = masked(v[u], c.e[u]);
       });
     }
     if (h) {
@@ -458,6 +459,7 @@ mist_status check(const mist_block_desc* d) {
     return lib_fail(MIST_E_INVALID, "block norm: the residual must be of the block's type or fp32");
   if (!(d->eps >= 0.0f) || !std::isfinite(d->eps) || !std::isfinite(d->res_scale) || !std::isfinite(d->block_scale))
     return lib_fail(MIST_E_INVALID, "block norm: eps must be >= 0, scales finite");
+  if (d->of_sum != 0 && d->of_sum != 1) return lib_fail(MIST_E_INVALID, "block norm: of_sum must be 0 or 1");
   for (int64_t x : {d->x_stride, d->block_stride, d->y_stride, d->h_stride, d->gate_stride})
     if (!mist::stride_ok(x)) return lib_fail(MIST_E_INVALID, "block norm: strides must be in 0..2^40");
   return MIST_OK;
@@ -503,7 +505,7 @@ mist_status not_shared(bool shared) { return shared ? lib_fail(MIST_E_INVALID, "
 
 BlockArgs args(const mist_block_desc* d, const void* weight, const void* bias, const void* post_weight, const void* post_bias, const void* gate) {
   return BlockArgs{d->batch * d->seq, std::max<int64_t>(d->seq, 1), d->hidden, d->x_stride, d->block_stride, d->y_stride, d->h_stride,
-                   gate && d->batch > 1 ? d->gate_stride : 0, d->kind == MIST_BLOCK_LAYER, d->weight_type, d->eps, d->res_scale, d->block_scale,
+                   gate && d->batch > 1 ? d->gate_stride : 0, d->kind == MIST_BLOCK_LAYER, d->weight_type, d->of_sum, d->eps, d->res_scale, d->block_scale,
                    (float)(1.0 / (double)d->hidden), weight, bias, post_weight, post_bias, gate};
 }
 

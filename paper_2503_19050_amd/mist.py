@@ -160,7 +160,7 @@ class BlockDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in
                 ["batch", "seq", "hidden", "x_stride", "block_stride", "y_stride", "h_stride", "gate_stride"]] + \
                [(n, ctypes.c_int32) for n in ["kind", "type", "res_type", "weight_type"]] + \
-               [(n, ctypes.c_float) for n in ["eps", "res_scale", "block_scale"]]
+               [(n, ctypes.c_float) for n in ["eps", "res_scale", "block_scale"]] + [("of_sum", ctypes.c_int32)]
 
 
 class BlockGrads(ctypes.Structure):
@@ -1285,7 +1285,7 @@ def _block_gate(what, x, gate, dtype) -> int:
     return gate.stride(0) if gate.dim() == 2 else 0
 
 
-def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale):
+def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale, of_sum=0):
     shape = x.shape
     dims, hidden = len(shape), shape[-1] if len(shape) else 0
     if dims != 3 and dims != 2:
@@ -1314,15 +1314,16 @@ def _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate
         _need(False, "%s: h must have the block's type" % what)
     return BlockDesc(shape[0] if dims == 3 else 1, shape[-2], hidden, strides[0], strides[1], strides[2], strides[3],
                      0 if gate is None else _block_gate(what, x, gate, wtype), code, _type(like, what), _type(x, what), _TYPES.get(wtype, -1),
-                     eps, res_scale, block_scale)
+                     eps, res_scale, block_scale, of_sum)
 
 
 def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, kind: str = "rms", eps: float = 1e-6,
-               res_scale: float = 1.0, block_scale: float = 1.0, y=None, h=None, dtype=None, stream=None) -> BlockNorm:
+               res_scale: float = 1.0, block_scale: float = 1.0, stored: bool = True, y=None, h=None, dtype=None, stream=None) -> BlockNorm:
     """mist_block_forward: y = res_scale * x + block_scale * gate * N(block), h = N(y) * weight + bias, and the stats that
     block_norm_grad takes.  x: [tokens, hidden] or [batch, seq, hidden], the residual, of the block's type or float32; gate: [hidden]
     or [batch, hidden].  Without post_weight the block's output is not normed; without weight there is no h (None); without
-    block, y is x and h its norm (of dtype, default x's).  y may be x or block."""
+    block, y is x and h its norm (of dtype, default x's).  stored: N(y) is of y as it is stored, so that block_norm of y alone gives h bit
+    for bit; False: of the sum before its rounding, so that h of a 16-bit residual has one rounding, not two.  y may be x or block."""
     torch = _torch()
     L = _lib or load()
     what = "block norm"
@@ -1341,7 +1342,7 @@ def block_norm(x, block=None, *, weight=None, bias=None, post_weight=None, post_
         if weight is not None and h is None:
             h = _like(torch, x, dtype if block is None else block.dtype)
         stats = torch.empty((*x.shape[:-1], 4), dtype=torch.float32, device=x.device)
-    d = _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale)
+    d = _block_desc(what, x, block, y, h, weight, bias, post_weight, post_bias, gate, kind, eps, res_scale, block_scale, 0 if stored else 1)
     _on_device(torch, x.device, L.mist_block_forward, ctypes.byref(d), x.data_ptr(), _ptr(block), _ptr(weight), _ptr(bias), _ptr(post_weight),
                _ptr(post_bias), _ptr(gate), _ptr(y), _ptr(h), stats.data_ptr(), handle)
     if other is not None:

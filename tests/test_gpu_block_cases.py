@@ -4,7 +4,7 @@ import sys
 
 import pytest
 
-from test_gpu_block import EPS, make
+from test_gpu_block import EPS, TINY, UNIT, V, back, forward_truth, make, norm, within
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,42 @@ def test_gates_beside_their_gradients(torch):
     for gate, dgate in ((w["gate"], want), (both[:, 1:65], both[:, 65:129])):
         mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], gate=gate, dgate=dgate, **how)
     assert torch.equal(both[:, 65:129], want) and torch.equal(both[:, 1:65], w["gate"]) and bool((both[:, [0, 129]] == 7).all())
+
+
+@pytest.mark.parametrize("act, res, wt", [("bf16", "bf16", "bf16"), ("f16", "f16", "f32"), ("bf16", "f32", "f32")])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("shape, post, gate", [((2, 5, 7), True, "sequence"), ((3, 70, 512), False, ""), ((2, 37, 200), False, "all"), ((1, 9, 2561), True, ""),
+                                               ((2, 3, 9000), True, "sequence"), ((1, 3, 8192), False, "")], ids=str)
+def test_the_norm_of_the_sum(torch, shape, post, gate, kind, act, res, wt):
+    """h of the sum before its rounding, its statistics, and the gradients, which take the norm from the stored sum: off by its rounding."""
+    from paper_2503_19050_amd import mist
+    say("norm of the sum", shape, post, gate, kind, act, res, wt)
+    s, w, gr = make(torch, *shape, act, res, wt, post, True, gate)
+    form = dict(kind=kind, res_scale=0.75, block_scale=1.5)
+    r, other = (mist.block_norm(s["x"], s["block"], eps=EPS, stored=k, **form, **w) for k in (False, True))
+    assert torch.equal(r.y, other.y) and torch.equal(r.stats[..., :2], other.stats[..., :2])
+    if res == "f32":
+        assert torch.equal(r.h, other.h) and torch.equal(r.stats, other.stats)
+    y, v, n2, r2, gate_, wide, one = forward_truth(torch, s, w, kind, 0.75, 1.5)
+    within(r.y, y, res, "y")
+    n1, r1 = norm(torch, y, kind)
+    within(r.h, n1 * wide["weight"] + wide["bias"], act, "h")
+    assert bool(((r.stats[..., 3:].double() - r1.x).abs() <= r1.e + 2.0 ** -24 * r1.x).all())
+    n1 = V(n1.x, n1.e + r1.x * (UNIT[res] * (y.x.abs() + y.e) + TINY[res]))   # from y as it is stored
+    how = {k: t for k, t in w.items() if k != "bias"}
+    dweight = torch.empty_like(w["weight"])
+    dx, db = mist.block_norm_grad(r.y, r.stats, gr["dh"], block=s["block"], dy=gr["dy"], dweight=dweight, **form, **how)
+    dh = V(gr["dh"].double())
+    within(dweight, (dh * n1).sum((0, 1)), wt, "dweight")
+    d = V(gr["dy"].double()) + back(dh * wide["weight"], n1, r1, kind)
+    within(dx, one(0.75) * d, res, "dx")
+    d = one(1.5) * d
+    d = d * gate_ if gate else d
+    within(db, back(d * wide["post_weight"], n2, r2, kind) if post else d, act, "dblock")
+
+
+def test_a_norm_alone_has_no_sum(torch):
+    from paper_2503_19050_amd import mist
+    s, w, _ = make(torch, 2, 5, 300, "bf16", "bf16", "bf16", False, True, "")
+    a, b = (mist.block_norm(s["x"], stored=k, **w) for k in (False, True))
+    assert torch.equal(a.h, b.h) and torch.equal(a.stats, b.stats)

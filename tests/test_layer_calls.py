@@ -113,3 +113,10 @@ def test_tangents_are_not_dropped(grad):
                 call()
         with pytest.raises(mist.MistError, match="GPU"):   # without one they go on to the next check
             mist.token_logprob(plain, t)
+
+
+def test_what_the_norm_is_of():
+    L = mist.load()
+    for bad in (2, -1):
+        d = mist.BlockDesc(2, 3, 16, 16, 16, 16, 16, 0, 0, 1, 0, 1, 1e-5, 1.0, 1.0, bad)
+        assert L.mist_block_forward(r(d), *A[:3], None, None, None, None, *A[3:6], None) == -1 and b"of_sum" in L.mist_last_error()
