@@ -402,7 +402,7 @@ def _block_own(s, mist):
     c = s["c"]
     how = dict(weight=s["weight"], post_weight=s["post_weight"], post_bias=s["post_bias"], gate=s["gate"], kind=c["kind"],
                res_scale=c["res_scale"], block_scale=c["block_scale"])
-    r = mist.block_norm(s["x"], s["block"], bias=s["bias"], eps=EPS, **how)
+    r = mist.block_norm(s["x"], s["block"], bias=s["bias"], eps=EPS, stored=False, **how)  # of the sum, as the plain form has it
     out = dict(y=r.y, h=r.h)
     if c["op"] == "norm":
         return out
