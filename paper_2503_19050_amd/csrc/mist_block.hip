@@ -34,7 +34,7 @@ constexpr int kJoinThreads = 1024;
 
 struct BlockArgs {
   int64_t n, seq, hidden, x_stride, block_stride, y_stride, h_stride, gate_stride;
-  int32_t layer, weight_type, of_sum;
+  int32_t layer, weight_type;
   float eps, res_scale, block_scale, inv_hidden;
   const void *weight, *bias, *post_weight, *post_bias, *gate;
 };
@@ -191,7 +191,7 @@ constexpr int most_waves(int u, int l, bool wide, bool more) { return l < 64 ? 1
 // The next row is read before the sums of this one are waited for, where the registers are there.
 // MORE: a norm before, or a gate.
 template <class A, class R, int U, int L, bool WIDE, bool WHOLE, bool MORE>
-__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats) {
+__global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(BlockArgs a, const R* x, const A* block, R* y, A* h, float* stats, int32_t of_sum) {
   constexpr int kRows = 64 / L;  // of a block at a time
   __shared__ float2 part[3 * kMostWaves];
   Join<L> join{part, part + 2 * kMostWaves, (int)blockDim.x / 64, 0};
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(most_waves(U, L, WIDE, MORE) * 64) void k_forward(B
         v[u] = a.res_scale * v[u] + a.block_scale * b[u];
         if (there) store8(y + t * a.y_stride, c.e[u], v[u]);
         // of y as it is stored: formed again from it, h has the same bits
-        if (!a.of_sum) v[u] = __builtin_convertvector(__builtin_convertvector(v[u], mist::Raw8<R>), Float8);
+        if (!of_sum) v[u] = __builtin_convertvector(__builtin_convertvector(v[u], mist::Raw8<R>), Float8);
         v[u] = masked(v[u], c.e[u]);
       });
     }
@@ -505,7 +505,7 @@ mist_status not_shared(bool shared) { return shared ? lib_fail(MIST_E_INVALID, "
 
 BlockArgs args(const mist_block_desc* d, const void* weight, const void* bias, const void* post_weight, const void* post_bias, const void* gate) {
   return BlockArgs{d->batch * d->seq, std::max<int64_t>(d->seq, 1), d->hidden, d->x_stride, d->block_stride, d->y_stride, d->h_stride,
-                   gate && d->batch > 1 ? d->gate_stride : 0, d->kind == MIST_BLOCK_LAYER, d->weight_type, d->of_sum, d->eps, d->res_scale, d->block_scale,
+                   gate && d->batch > 1 ? d->gate_stride : 0, d->kind == MIST_BLOCK_LAYER, d->weight_type, d->eps, d->res_scale, d->block_scale,
                    (float)(1.0 / (double)d->hidden), weight, bias, post_weight, post_bias, gate};
 }
 
@@ -636,7 +636,7 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
     constexpr bool kWide = l.value == 64;  // its registers are the same for all
     const auto kernel = post_weight || gate ? k_forward<A, R, u.value, l.value, kWide, whole.value, true> : k_forward<A, R, u.value, l.value, kWide, whole.value, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((a.n * l.value + 63) / 64, kMostBlocks)), dim3(threads(d->hidden)), 0, (hipStream_t)stream, a,
-                       (const R*)x, (const A*)block, (R*)y, (A*)h, stats);
+                       (const R*)x, (const A*)block, (R*)y, (A*)h, stats, d->of_sum);
   });
   return launched("block norm");
 }
