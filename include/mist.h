@@ -726,7 +726,8 @@ mist_status mist_block_forward(const mist_block_desc* d, const void* x, const vo
 /* Gradients: dh of h (NULL iff weight is) and dy of y by its other uses (NULL: none) give dx and dblock (each may be
  * NULL: not wanted), and, where their addresses are given, those of the weights, biases and gates, overwritten or
  * (accumulate = 1) added to.  Sums over tokens are in fp32 in an order that depends on
- * *d and on whether there is a norm before or a gate, not on which gradients are wanted. */
+ * *d and on whether there is a norm before or a gate, not on which gradients are wanted: up to 2^21 tokens in chains of at
+ * most 512. */
 typedef struct mist_block_grads {
   const void *dh, *dy;
   void *dx, *dblock;

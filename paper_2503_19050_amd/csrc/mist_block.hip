@@ -29,6 +29,8 @@ constexpr int kMostWaves = 16;
 constexpr int64_t kMostTokens = (int64_t)1 << 30;
 constexpr int64_t kMostBlocks = 4096;  // of the forward pass; they take rows in turn
 constexpr int64_t kPartRows = 4;       // a part has at least, where there are as many
+constexpr int64_t kMostRows = 512;     // added one after another in fp32, as long as kMostParts parts are enough
+constexpr int64_t kMostParts = 4096;
 constexpr int kSlots = 5;              // gradients summed over tokens
 constexpr int kJoinThreads = 1024;
 
@@ -549,7 +551,8 @@ mist_status launched(const char* what) {
   return e == hipSuccess ? MIST_OK : hip_failed(e, what);
 }
 
-// Waves of the backward pass that a CU holds: one round of blocks of the same work (two to four rounds took 0-5 % more).
+// Waves of the backward pass that a CU holds: one round of blocks of the same work (two to four rounds took 0-5 % more), or as many rounds as
+// keep the sums' chains short.
 int64_t resident_waves(const mist_block_desc* d, int64_t waves, bool more) {
   const bool wide = waves == 1 || waves > narrow_waves(more);
   return more && !wide ? 12 : more ? 16 : 4 * back_waves(units(d->hidden), lanes(d->hidden), wide, (size_t)mist::type_bytes(d->res_type));
@@ -560,7 +563,8 @@ Parts parts_of(const mist_block_desc* d, bool by_sequence, bool more) {
   p.batch = by_sequence ? d->batch : 1;
   p.seq = by_sequence ? d->seq : d->batch * d->seq;
   if (!p.batch || !p.seq) return p;
-  const int64_t waves = threads(d->hidden) / 64, parts = 256 * std::max<int64_t>(1, resident_waves(d, waves, more) / waves), least = kPartRows * 64 / lanes(d->hidden);
+  const int64_t waves = threads(d->hidden) / 64, round = 256 * std::max<int64_t>(1, resident_waves(d, waves, more) / waves), least = kPartRows * 64 / lanes(d->hidden);
+  const int64_t parts = round * std::clamp<int64_t>((p.batch * p.seq + round * kMostRows - 1) / (round * kMostRows), 1, std::max<int64_t>(1, kMostParts / round));
   p.pieces = std::clamp<int64_t>(parts / p.batch, 1, (p.seq + least - 1) / least);
   p.rows = (p.seq + p.pieces - 1) / p.pieces;
   p.pieces = (p.seq + p.rows - 1) / p.rows;

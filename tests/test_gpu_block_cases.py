@@ -148,3 +148,32 @@ def test_a_norm_alone_has_no_sum(torch):
     s, w, _ = make(torch, 2, 5, 300, "bf16", "bf16", "bf16", False, True, "")
     a, b = (mist.block_norm(s["x"], stored=k, **w) for k in (False, True))
     assert torch.equal(a.h, b.h) and torch.equal(a.stats, b.stats)
+
+
+@pytest.mark.parametrize("hidden", [4096, 8192, 9000, 16384])
+@pytest.mark.parametrize("batch", [1, 1 << 10])
+def test_sums_of_many_tokens(torch, hidden, batch):
+    """2^21 tokens that share a row, in the C call (no outputs but the sums): a part adds 512 rows one after another, the parts' sums are
+    added in 32 chains of 128 and those in one: 700 roundings of 2^-24.  The value is one of which a long chain loses the same at each step."""
+    from paper_2503_19050_amd import mist
+    say("many tokens", hidden, batch)
+    L = mist.load()
+    n = 1 << 21
+    value = 1 + 0.4 * 2.0 ** -12
+    dh, y = torch.full((hidden,), value, device="cuda"), torch.zeros(hidden, device="cuda")
+    y[0] = 1.0
+    stats = torch.tensor([0.0, 1.0, 0.0, 1.0], device="cuda").repeat(n, 1)
+    w, gate = torch.ones(hidden, device="cuda"), torch.ones(batch, hidden, device="cuda")
+    dw, db, dgate = torch.empty(hidden, device="cuda"), torch.empty(hidden, device="cuda"), torch.empty(batch, hidden, device="cuda")
+    stride = hidden if batch > 1 else 0
+    d = mist.BlockDesc(batch, n // batch, hidden, 0, 0, 0, 0, stride, 0, 0, 0, 0, 0.0, 1.0, 1.0)
+    for more in (False, True):   # with a gate: its gradient is the sum of dy times the block, here of dh alone
+        g = mist.BlockGrads(dh.data_ptr(), None, None, None, dw.data_ptr(), db.data_ptr(), None, None, dgate.data_ptr() if more else None, 0, 0, 0, 0, stride, 0)
+        need = ctypes.c_size_t()
+        assert L.mist_block_workspace(ctypes.byref(d), ctypes.byref(g), ctypes.byref(need)) == 0
+        ws = torch.empty(need.value, device="cuda", dtype=torch.uint8)
+        assert L.mist_block_backward(ctypes.byref(d), y.data_ptr(), dh.data_ptr(), stats.data_ptr(), w.data_ptr(), None, None, gate.data_ptr() if more else None,
+                                     ctypes.byref(g), ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+        exact = n * float(dh[0])
+        assert float((db.double() - exact).abs().max()) <= 700 * 2.0 ** -24 * exact, more
+        assert abs(float(dw[0]) - exact) <= 700 * 2.0 ** -24 * exact and not bool(dw[1:].any()), more
