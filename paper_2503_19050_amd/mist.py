@@ -1529,6 +1529,8 @@ def mlp_act(up, gate=None, *, kind: str = "silu", save=False, out=None, stream=N
         pair = (None, None) if save is True else save
         if not (len(pair) == 2):
             _need(False, "activation: save must be a bool or (up's checkpoint, gate's or None)")
+        if gate is None and pair[1] is not None:
+            _need(False, "activation: a gate to keep that is not there")
         keep = (_checkpoint_for(torch, what, up, pair[0], other), None if gate is None else _checkpoint_for(torch, what, gate, pair[1], other))
     rows, stride = _flat(what, up)
     d = ActDesc(rows, up.shape[-1], stride, 0 if gate is None else _flat(what, gate)[1], _flat(what, out)[1], 0, _type(up, what), _ACTS[kind])

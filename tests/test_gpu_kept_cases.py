@@ -59,3 +59,13 @@ def test_a_checkpoint_of_a_stream(torch):
             assert mist.checkpoint_store(x, c, stream=stream) is c
             torch.cuda.synchronize()
             assert torch.equal(c.values, want.values) and torch.equal(c.exponents, want.exponents)
+
+
+def test_a_place_for_a_gate_that_is_not_there(torch):
+    from paper_2503_19050_amd import mist
+    x = torch.zeros(4, 200, device="cuda", dtype=torch.bfloat16)
+    a, b = (mist.Checkpoint((4, 200), torch.bfloat16) for _ in range(2))
+    with pytest.raises(mist.MistError, match="gate"):
+        mist.mlp_act(x, save=(a, b))
+    r = mist.mlp_act(x, save=(a, None))
+    assert r.up is a and r.gate is None
