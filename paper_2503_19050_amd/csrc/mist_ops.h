@@ -1,4 +1,5 @@
-// Element types and host helpers shared by the training-step operators (mist_embed.hip, mist_step.hip).
+// Element types, vectors, lane exchanges and host helpers shared by the operators of a training step, its last stage and a layer
+// (mist_embed.hip, mist_step.hip, mist_token.hip, mist_block.hip, mist_kept.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>

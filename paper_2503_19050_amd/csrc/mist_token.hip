@@ -5,11 +5,11 @@
 // the logits are (a fused product less a rounded largest one is off by up to half a step of that: past any exponential from 2^31 on).  A row stays in the registers of its block from its one reading to the
 // last pass over it (of 16-bit values up to 65536, of fp32 32768; longer ones by chunks, whose sums are rescaled); the loss writes the
 // gradient from there.  Measured on one MI355X, where a large copy reads and writes 4.9 TB/s:
-//   loss        32768 x 50257 bf16  1310 us, 5.0 TB/s: memory
-//   gradient    8192 x 50257 bf16   293 us, 5.6 TB/s: memory
-//   statistics  8192 x 32000 fp32   170 us, 6.2 TB/s: memory;  8192 x 50256 bf16  162 us, 5.1 TB/s: vector instructions, 11.7 a
-//               logit (a conversion and the maximum, then a conversion, the exponential and four more)
-//   with 8 alternatives  16376 x 50257 bf16  456 us
+//   loss        32768 x 50257 bf16  1265 us, 5.2 TB/s: memory
+//   gradient    8192 x 50257 bf16   306 us, 5.4 TB/s: memory
+//   statistics  8192 x 32000 fp32   171 us, 6.1 TB/s: memory;  8192 x 50256 bf16  158 us, 5.2 TB/s: vector instructions, 12.0 a
+//               logit (a conversion and the maximum, then a conversion, the exponential and five more)
+//   with 8 alternatives  16376 x 50257 bf16  461-470 us
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
