@@ -3,10 +3,9 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 #include <stdio.h>
-
-#include <initializer_list>
 
 #include "mist.h"
 
@@ -197,20 +196,29 @@ struct Use {
   R at;
   bool out;
 };
-inline bool empty(const Range& x) { return x.lo == x.hi; }
-inline bool empty(const Rows& x) { return !x.p || x.rows <= 0 || x.width <= 0; }
+inline Range span_of(const Range& x) { return x; }
+inline Range span_of(const Rows& x) { return range_of(x.p, x.rows, x.stride, x.width, x.bytes); }
 // Whether an output of the first list shares memory with another tensor of it, or one of the first list with one of the second where
 // either is an output.
-template <class R>
-bool shared(std::initializer_list<Use<R>> all, std::initializer_list<Use<R>> others = {}) {
-  for (auto a = all.begin(); a != all.end(); ++a) {
-    if (empty(a->at)) continue;
-    for (auto b = all.begin(); b != a; ++b)
-      if ((a->out || b->out) && !empty(b->at) && overlap(a->at, b->at)) return true;
-    for (const Use<R>& b : others)
-      if ((a->out || b.out) && !empty(b.at) && overlap(a->at, b.at)) return true;
+template <class R, size_t N, size_t M>
+bool shared(const Use<R> (&all)[N], const Use<R> (&others)[M]) {
+  Range a[N], b[M];
+  for (size_t i = 0; i < N; ++i) a[i] = span_of(all[i].at);
+  for (size_t i = 0; i < M; ++i) b[i] = span_of(others[i].at);
+  auto meet = [](const Use<R>& x, Range p, const Use<R>& y, Range q) {
+    return (x.out || y.out) && p.lo != p.hi && q.lo != q.hi && overlap(p, q) && overlap(x.at, y.at);
+  };
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t k = 0; k < i; ++k)
+      if (meet(all[i], a[i], all[k], a[k])) return true;
+    for (size_t k = 0; k < M; ++k)
+      if (meet(all[i], a[i], others[k], b[k])) return true;
   }
   return false;
+}
+template <class R, size_t N>
+bool shared(const Use<R> (&all)[N]) {
+  return shared<R>(all, {Use<R>{R{}, false}});
 }
 
 inline bool is_aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
