@@ -6,7 +6,7 @@
 // Bound by memory; what it takes is enough rows in flight, so the next row is read ahead and registers decide.  Measured on one MI355X, where
 // a large copy reads and writes 4.9 TB/s, forward and backward: 65536 x 2560 bf16 268 and 364 us (5.0 and 4.6 TB/s), 65536 x 5120
 // 536 and 675 (5.0, 5.0), 32768 x 8192 398-441 and 528 (4.9-5.4, 5.1), 65536 x 512 45 and 82 (5.9, 4.1), 65536 x 2559 326 and 541
-// (4.1, 3.1), 32768 x 4096 with a norm before and gates by sequence 229 and 323 (4.7, 5.0).
+// (4.1, 3.1), 32768 x 4096 with a norm before and gates by sequence 231 and 324 (4.7, 5.0).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
